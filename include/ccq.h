@@ -271,6 +271,157 @@ int ccq_probe_stream_read(const void *src, int64_t bytes, int32_t loads_per_thre
                           void *hip_stream);
 int ccq_probe_mfma_bf16(const void *operands, int32_t workgroups, int32_t iters, void *sink, void *hip_stream, double *flop_out);
 
+/* ---- The rest of a decoder layer, in 8 bits -------------------------------------------------------------------------------------------
+ *
+ * The operators between the quantized products: norm, 8-bit products for the layers that are not quantized further, rotary
+ * positions, a paged cache of keys and values, and the attention that reads it.  The conventions above hold (DEVICE
+ * pointers 16-byte aligned where nothing else is said, work enqueued on hip_stream, nothing allocated or synchronised).
+ *
+ * 8-bit values are e4m3 (1 sign, 4 exponent, 3 mantissa bits, largest 448, no infinities, 0x7F and 0xFF are NaN), rounded to
+ * nearest even.  Scales that the library computes are powers of two, held as a byte e + 127 that stands for 2^e: the least e
+ * with (largest magnitude) <= 448 * 2^e.  A power of two costs e4m3 no precision (its steps are relative), scaling by it is exact, and
+ * the byte is the scale operand of the scaled matrix instructions. */
+
+/* M rows of N 8-bit values, one scale per row and block of 128 columns (the last block may be shorter). */
+typedef struct {
+  void *codes;       /* DEVICE e4m3 [M][ld], ld >= N, a multiple of 16                                */
+  int64_t ld;
+  uint8_t *scales;   /* DEVICE [M][ld_scales], ld_scales >= ceil(N / 128); any alignment              */
+  int64_t ld_scales;
+} ccq_rows8;
+
+typedef enum { CCQ_BF16 = 0, CCQ_FP32 = 1 } ccq_type;
+
+/* h = x + residual;  sum = h;  y = h / sqrt(mean(h^2) + eps) * weight, per row, in fp32 (sums and statistics included; h is not
+ * rounded before it is normalised).  Strides are in elements and free (any alignment of rows; multiples of 8 elements on 16-byte
+ * aligned arrays are read and written 16 bytes at a time). */
+typedef struct {
+  int32_t M, N;            /* M = 0 is a no-op; N >= 1                                                   */
+  float eps;               /* >= 0                                                                       */
+  const void *x;           /* DEVICE bf16 [M][ldx]                                                       */
+  int64_t ldx;
+  const void *residual;    /* DEVICE [M][ld_residual] of residual_type, or NULL                          */
+  int64_t ld_residual;
+  void *sum;               /* DEVICE [M][ld_sum] of residual_type, may be `residual` itself (with the same stride), or NULL */
+  int64_t ld_sum;
+  int32_t residual_type;   /* ccq_type                                                                   */
+  const void *weight;      /* DEVICE [N] of weight_type, or NULL (ones)                                  */
+  int32_t weight_type;
+  void *y;                 /* DEVICE bf16 [M][ldy], or NULL; may be x (with the same stride)             */
+  int64_t ldy;
+  ccq_rows8 y8;            /* or codes = NULL.  y, y8 or both                                            */
+} ccq_norm;
+/* A row that holds NaN is NaN in all outputs (in y8: codes and scales).  A row with an infinity is so where h is not finite and
+ * zero elsewhere; a block of y8 with a NaN in it has NaN codes and a NaN scale (255). */
+int ccq_rms_norm(const ccq_norm *n, void *hip_stream);
+
+/* Rows of bf16 [M][ldx] as 8-bit rows: what ccq_rms_norm does to its result.  A block that holds NaN or an infinity becomes NaN
+ * (codes and scale). */
+int ccq_quantize8(const void *x, int64_t ldx, int32_t M, int32_t N, const ccq_rows8 *out, void *hip_stream);
+
+/* 8-bit weights [N][K] with a scale per block of 128 x 128 (blocks at the ends may be smaller). */
+typedef struct {
+  int32_t K, N;            /* K a multiple of 16                                                         */
+  const void *codes;       /* DEVICE e4m3 [N][ldw], ldw >= K, a multiple of 16                           */
+  int64_t ldw;
+  const float *scales;     /* DEVICE fp32 [ceil(N / 128)][ld_scales], ld_scales >= ceil(K / 128); any finite values */
+  int64_t ld_scales;
+} ccq_weight8;
+
+/* y[m][n] = sum over blocks b of 2^(e[m][b]) s[n / 128][b] sum over k in b of x[m][k] w[n][k], fp32 accumulation.
+ *   x: 8-bit rows [M][K]; y DEVICE bf16 [M][ldy], ldy >= N, a multiple of 8; columns N.. of y are not written.
+ *   workspace DEVICE, at least ccq_gemm8_workspace_bytes(w, M) bytes (may be NULL if that is 0; -1: invalid arguments).
+ *   M = 0 is a no-op. */
+int64_t ccq_gemm8_workspace_bytes(const ccq_weight8 *w, int32_t M);
+int ccq_gemm8(const ccq_weight8 *w, const ccq_rows8 *x, int32_t M, void *y, int64_t ldy, void *workspace, int64_t workspace_bytes,
+              void *hip_stream);
+
+/* A paged cache.  A page holds page_tokens tokens of one sequence, for every key head:
+ *   k DEVICE e4m3 [pages][kv_heads][page_tokens][head_dim],  v DEVICE e4m3 [pages][kv_heads][head_dim][page_tokens]
+ *   (values of neighbouring tokens side by side: a matrix operand of the products with the softmax weights is one load),
+ *   k_scales, v_scales DEVICE bytes [pages][kv_heads], exponents -60 .. 60 (larger magnitudes saturate at 448 * 2^60). */
+typedef struct {
+  int32_t pages;
+  int32_t page_tokens;     /* 16, 32, 64, 128 or 256                                                     */
+  int32_t kv_heads;
+  int32_t head_dim;        /* 64 or 128                                                                  */
+  void *k, *v;
+  uint8_t *k_scales, *v_scales;
+} ccq_cache;
+
+/* The sequences of a call.  Sequence b has the new tokens offsets[b] .. offsets[b + 1] - 1 of the call's token rows (none, one or
+ * many) and lens[b] tokens with them: its new tokens are at positions lens[b] - new .. lens[b] - 1, position p lies in
+ * slot p % page_tokens of page table[b][p / page_tokens].  Device data are not read back; max_new and max_len are
+ * upper bounds that shape the launch and must hold: new tokens past max_new and positions past max_len or the table are left
+ * out.  An entry of the table outside 0 .. pages - 1 stands for a page that is not there: its tokens are not written
+ * and not attended to.  Offsets must be monotone within 0 .. tokens. */
+typedef struct {
+  int32_t batch;           /* sequences; 0 is a no-op                                                    */
+  int32_t tokens;          /* token rows of the call                                                     */
+  int32_t max_new;         /* the most new tokens of a sequence                                          */
+  int32_t max_len;         /* the greatest length (new tokens included)                                  */
+  const int32_t *offsets;  /* DEVICE int32 [batch + 1]                                                   */
+  const int32_t *lens;     /* DEVICE int32 [batch]                                                       */
+  const int32_t *table;    /* DEVICE int32 [batch][ld_table]                                             */
+  int64_t ld_table;        /* entries between rows, >= table_width                                       */
+  int32_t table_width;     /* entries of a row                                                           */
+} ccq_batch;
+
+/* bf16 [tokens][heads][head_dim]: strides in elements, multiples of 8, the head_dim values of a head side by side. */
+typedef struct {
+  void *data;              /* DEVICE                                                                     */
+  int64_t token_stride, head_stride;
+} ccq_heads;
+
+/* Rotary positions: dimensions 0 .. dims - 1 of a head in pairs (i, i + dims / 2), or (2 i, 2 i + 1) with `interleaved`, pair i turned by
+ * the angle whose cosine is table[p][i] and whose sine is table[p][dims / 2 + i]; the other dimensions stay.  p is the token's position in
+ * its sequence, or positions[token row]; past the table's ends its first or last row is taken.  Products and sums in fp32, each
+ * rounded on its own. */
+typedef struct {
+  const float *table;        /* DEVICE fp32 [rows][dims]                                                 */
+  int32_t rows, dims;        /* dims even, <= head_dim                                                   */
+  int32_t interleaved;
+  const int32_t *positions;  /* DEVICE int32 [tokens], or NULL                                           */
+} ccq_rope;
+
+/* Fills such a table: angle of pair i at position p is p * base^(-2 i / dims), in 64 bits, for kind
+ *   0: as it is;  1: divided by `factor`;  2: with base * factor^(dims / (dims - 2)) (dims >= 4);
+ *   3: by parts: f = base^(-2 i / dims) makes r = original_length f / (2 pi) turns over the original length; f stays where r >= fast,
+ *      is divided by factor where r <= slow, and between them is mixed linearly in i (i of a number of turns r is
+ *      dims ln(original_length / (2 pi r)) / (2 ln base), the ends rounded outwards to whole pairs); cosines and sines are
+ *      multiplied by `magnitude`.
+ * magnitude is applied for every kind (0 stands for 1). */
+typedef struct {
+  int32_t kind;
+  double base, factor, original_length, fast, slow, magnitude;
+} ccq_rope_scaling;
+int ccq_rope_table(const ccq_rope_scaling *s, int32_t rows, int32_t dims, float *table, void *hip_stream);
+
+/* Writes the new tokens' keys (rotated when rope is given) and values to the cache, and rotated queries to q_out.
+ *   k, v: kv_heads heads each; q, q_out: q_heads heads (both NULL: keys and values only; k and v both NULL: queries only; q_out may be q).
+ * A page's scale for a head covers its tokens so far: a page whose first slots hold older tokens takes the larger of its old scale and
+ * what the new tokens need, and where that grows the older tokens are brought to it (exact but for results below e4m3's smallest normal
+ * number); a page that the call begins takes what its new tokens need.  NaN and infinities do not count for the scale: in k they become NaN; a token
+ * with one in v has zeros there and NaN for its whole key, so that the rows that see the token are NaN, and no others.
+ * The pages of the new tokens must belong to their sequence alone, and no page may occur twice in the call's new tokens. */
+int ccq_cache_append(const ccq_cache *c, const ccq_batch *b, const ccq_rope *rope, const ccq_heads *k, const ccq_heads *v, const ccq_heads *q,
+                     const ccq_heads *q_out, int32_t q_heads, void *hip_stream);
+
+/* out[t][h] = sum over tokens j of softmax_j(scale q[t][h] . k[j][h / g]) v[j][h / g], g = q_heads / kv_heads, over the cached tokens j < lens that
+ * the row at position p sees: j <= p when causal, j > p - window when window > 0.  A row that sees none is zero.  Scores, softmax and sums in
+ * fp32; the softmax weights enter the second product as fp16, the cached values as they are.  `v` of the tokens that are seen holds no NaN
+ * (ccq_cache_append writes none); slots that are not written, and pages outside the window, may hold anything.
+ *   workspace DEVICE, at least ccq_attention_workspace_bytes(...) bytes (may be NULL if that is 0; -1: invalid arguments). */
+typedef struct {
+  int32_t q_heads;         /* a multiple of kv_heads                                                     */
+  int32_t causal;
+  int32_t window;          /* 0: none; needs causal                                                      */
+  float scale;             /* > 0                                                                        */
+} ccq_attn;
+int64_t ccq_attention_workspace_bytes(const ccq_cache *c, const ccq_batch *b, const ccq_attn *a);
+int ccq_attention(const ccq_cache *c, const ccq_batch *b, const ccq_attn *a, const ccq_heads *q, const ccq_heads *out, void *workspace,
+                  int64_t workspace_bytes, void *hip_stream);
+
 /* Human-readable name of a status code. */
 const char *ccq_status_string(int status);
 

@@ -1,0 +1,82 @@
+// What the attention kernels share: arguments, the sequences' ranges, and how rows are cut.
+//
+// The rows of a sequence and key head are its new tokens times the g query heads that share the key head, row r being token r / g,
+// head r % g, so that cached keys and values are read once for all of them.  The cached tokens of a sequence start at the first
+// that any of its rows sees, rounded down to 64, and may be cut into splits of `chunk` tokens, each with its own softmax statistics; a
+// second kernel joins them.
+//
+// Statistics are kept in units that take the scale of the values along: with x = log2(e) scale q k + e_v (e_v: exponent of the scale of v
+// in j's page) the accumulators hold  o = sum 2^(x - m) v8,  l = sum 2^(x - m - e_v),  so that a page's scale costs no work on
+// the accumulators, and the weights, fp16 for the second product, are largest where their product with v is.  The reference m
+// only moves when a tile's largest x is more than 8 above it (weights reach 2^8, far from fp16's largest number); the result is o / l.
+#pragma once
+#include "ccq_layer.h"
+
+namespace ccq {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8_t;
+typedef __attribute__((ext_vector_type(16))) float f32x16_t;
+
+struct AttnArgs {
+  const uint8_t *k, *v, *ks, *vs;
+  const uint16_t* q;
+  uint16_t* out;
+  int64_t q_token, q_head, o_token, o_head;
+  const int32_t *offsets, *lens, *table;
+  int64_t ld_table;
+  float* part_o;    // [split][token row][q head][D]
+  float* part_ml;   // [split][token row][q head][2]
+  int32_t pages, page_shift, kv_heads, q_heads, group, table_width, batch, tokens, max_new, max_len;
+  int32_t causal, window;
+  int32_t chunk, splits;
+  int32_t row_tiles;
+  float c;          // scale * log2(e)
+};
+
+constexpr float kLowest = -3.0e38f;   // the reference before any token is seen
+constexpr float kRise = 8.f;
+
+struct AttnSequence {
+  int first, n, old, len;   // first token row, new tokens, tokens before them, cached tokens with them
+  int begin;                // first cached token that a row sees, rounded down to 64
+};
+__device__ __forceinline__ int first_seen(const AttnArgs& a, int p) { return a.window > 0 ? max(0, p - a.window + 1) : 0; }
+__device__ __forceinline__ AttnSequence attn_sequence(const AttnArgs& a, int b) {
+  AttnSequence s;
+  s.first = max(a.offsets[b], 0);
+  s.n = min(a.offsets[b + 1], a.tokens) - s.first;
+  s.len = a.lens[b];
+  s.old = s.len - s.n;
+  s.n = min(s.n, a.max_new);
+  s.len = min(min(s.len, a.max_len), (int)min((int64_t)a.table_width << a.page_shift, (int64_t)0x7FFFFFFF));
+  s.begin = min(first_seen(a, s.old), max(s.len, 0)) & ~63;
+  return s;
+}
+// Cached tokens [first, second) that the row at position p sees.
+__device__ __forceinline__ int seen_end(const AttnArgs& a, const AttnSequence& s, int p) { return a.causal ? min(max(p + 1, 0), s.len) : s.len; }
+
+__device__ __forceinline__ f16x8_t values_f16(uint32_t lo, uint32_t hi) {
+  typedef __attribute__((ext_vector_type(2))) _Float16 pair;
+  const pair a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)lo, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)lo, 1.f, true);
+  const pair c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, 1.f, true);
+  return f16x8_t{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
+}
+__device__ __forceinline__ bf16x8_t values_bf16(uint32_t lo, uint32_t hi, float scale) {
+  typedef __attribute__((ext_vector_type(2))) __bf16 pair;
+  const pair a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)lo, scale, true);
+  const pair c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, scale, true);
+  return bf16x8_t{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
+}
+// The bytes of 16 neighbouring slots from token t0 on whose tokens lie in [lo, hi); the others become zero.
+__device__ __forceinline__ u32x4_t keep_tokens(u32x4_t v, int t0, int lo, int hi) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const int from = min(max(lo - t0 - 4 * w, 0), 4), to = min(max(hi - t0 - 4 * w, 0), 4);
+    const uint32_t below_to = (uint32_t)((1ull << (8 * to)) - 1), below_from = (uint32_t)((1ull << (8 * from)) - 1);
+    v[w] &= below_to & ~below_from;
+  }
+  return v;
+}
+
+}  // namespace ccq

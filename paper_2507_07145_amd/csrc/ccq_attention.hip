@@ -1,0 +1,314 @@
+// Attention over the paged 8-bit cache for few rows: single new tokens, and the join of splits.
+//
+// A wavefront walks tiles of 64 cached tokens on its own (the four of a workgroup take them in turn) and holds up to 16 or 32 rows:
+//   scores^T = K q^T   MFMA 16x16x32 bf16, cached tokens as rows: e4m3 is exact in bf16
+//   out^T    = V^T p^T MFMA 16x16x32 f16, dimensions as rows: e4m3 is exact in fp16
+// Tokens are dealt to the first product's rows so that a lane's 16 scores are those of 16 neighbouring tokens, in the order in which
+// the second product wants its operand: the weights go from one to the other in registers, and the values of a dimension, stored
+// token after token, are 16-byte loads that need no transposition either.  Nothing passes LDS until the wavefronts' results
+// are joined.  A lane's 16 tokens lie in one page (pages hold multiples of 16): its scales are one value each.
+// Bound by memory: 16 KB a tile (128 dimensions) against 32 MFMAs; keys are asked for a tile ahead, values while the scores are formed.
+#include <algorithm>
+
+#include "ccq_attention.h"
+
+namespace ccq {
+
+namespace {
+
+constexpr int kTile = 64, kWaves = 4;
+
+template <int D, int NT>
+__global__ __launch_bounds__(64 * kWaves) void ccq_attention_few_kernel(AttnArgs a) {
+  constexpr int KP = D / 64;     // 16-byte pieces of a key in a lane: dimensions 64 p + 16 g .. + 15
+  constexpr int DT = D / 16;     // tiles of dimensions
+  constexpr int STEPS = D / 32;
+  constexpr int kPitch = D + 4;
+  __shared__ __align__(16) float joined[kWaves * 16 * NT * kPitch];
+  __shared__ float stats[kWaves * 16 * NT * 2];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
+  const int h = blockIdx.x % a.kv_heads, tile = (blockIdx.x / a.kv_heads) % a.row_tiles, split = blockIdx.x / (a.kv_heads * a.row_tiles), b = blockIdx.y;
+  const AttnSequence s = attn_sequence(a, b);
+  const int rows = s.n * a.group, row0 = tile * (16 * NT);
+  if (row0 >= rows) return;
+  const int last_row = min(row0 + 16 * NT, rows) - 1;
+  const int p_first = s.old + row0 / a.group, p_last = s.old + last_row / a.group;   // positions of the tile's rows
+  // tokens that all rows see, and that any sees
+  const int all_lo = first_seen(a, p_last), all_hi = seen_end(a, s, p_first), any_lo = first_seen(a, p_first), any_hi = seen_end(a, s, p_last);
+  const int begin = s.begin + split * a.chunk, end = begin + min(a.chunk, s.len - begin);
+  if (split > 0 && begin >= s.len) return;   // (the first one answers for rows that see nothing)
+  const int from = max(begin, any_lo & ~(kTile - 1)), to = min(end, any_hi);
+
+  // queries: the same dimensions as a lane's pieces of the keys
+  bf16x8_t q[NT][STEPS];
+  int lo[NT], hi[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int row = min(row0 + nt * 16 + r16, last_row), token = row / a.group;
+    const uint16_t* at = a.q + (int64_t)(s.first + token) * a.q_token + (int64_t)(h * a.group + row % a.group) * a.q_head;
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i)
+      q[nt][i] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t*>(at + 64 * (i >> 1) + 16 * g + 8 * (i & 1)));
+    lo[nt] = first_seen(a, s.old + token);
+    hi[nt] = seen_end(a, s, s.old + token);
+  }
+
+  f32x4_t o[NT][DT];
+  float m[NT], l[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    m[nt] = kLowest;
+    l[nt] = 0.f;
+#pragma unroll
+    for (int i = 0; i < DT; ++i) o[nt][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+
+  const int32_t* pages = a.table + b * a.ld_table;
+  const int in_page = (1 << a.page_shift) - 1;
+  // page of a quarter of the tile at t0, -1 where there is none
+  auto page_at = [&](int t0, int quarter) {
+    const int t = t0 + 16 * quarter;
+    const int p = t < to ? pages[t >> a.page_shift] : -1;
+    return p < a.pages ? p : -1;
+  };
+  const int quarter_k = r16 >> 2;
+  u32x4_t kr[4][KP], vr[DT];
+  auto load_keys = [&](int t0, int page) {
+    const int slot = ((t0 + 16 * quarter_k) & in_page) + (r16 & 3);
+    const uint8_t* at = a.k + ((((int64_t)max(page, 0) * a.kv_heads + h) << a.page_shift) + slot) * D + 16 * g;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int p = 0; p < KP; ++p) kr[i][p] = *reinterpret_cast<const u32x4_t*>(at + (8 * (i >> 1) + 4 * (i & 1)) * D + 64 * p);
+  };
+  auto load_values = [&](int t0, int page) {
+    const int slot = (t0 + 16 * g) & in_page;
+    const uint8_t* at = a.v + ((((int64_t)max(page, 0) * a.kv_heads + h) * D + r16) << a.page_shift) + slot;
+#pragma unroll
+    for (int i = 0; i < DT; ++i) vr[i] = *reinterpret_cast<const u32x4_t*>(at + ((int64_t)(16 * i) << a.page_shift));
+  };
+
+  int t0 = from + wave * kTile;
+  const int stride = kWaves * kTile;
+  if (t0 < to) {
+    int pk = page_at(t0, quarter_k), pv = page_at(t0, g);
+    load_keys(t0, pk);
+    for (; t0 < to; t0 += stride) {
+      const int pk_next = page_at(t0 + stride, quarter_k), pv_next = page_at(t0 + stride, g);
+      const int64_t at = (int64_t)max(pv, 0) * a.kv_heads + h;
+      const int kb = a.ks[at], vb = a.vs[at];
+      load_values(t0, pv);
+      f32x4_t sc[NT][4];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sc[nt][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int step = 0; step < STEPS; ++step) {
+          const u32x4_t w = kr[i][step >> 1];
+          const bf16x8_t key = values_bf16(w[2 * (step & 1)], w[2 * (step & 1) + 1], 1.f);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) sc[nt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q[nt][step], sc[nt][i], 0, 0, 0);
+        }
+      load_keys(t0 + stride, pk_next);   // (past the end: page 0, never used)
+      const float ck = a.c * pow2_of_byte(kb), ev = (float)(vb - 127), inv_v = inverse_of_byte(vb);
+      const bool whole = t0 >= all_lo && t0 + kTile <= min(all_hi, to) && __all(pv >= 0);
+      if (!whole) {
+        const int token0 = t0 + 16 * g;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const int first = pv >= 0 ? lo[nt] : 0x7FFFFFFF, last = min(hi[nt], to);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int token = token0 + 4 * i + e;
+              if (token < first || token >= last) sc[nt][i][e] = -__builtin_inff();
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < DT; ++i) vr[i] = keep_tokens(vr[i], token0, pv >= 0 ? any_lo : 0x7FFFFFFF, to);
+      }
+      f16x8_t w[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float top = sc[nt][0][0];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) top = fmaxf(top, sc[nt][i][e]);
+        top = fmaf(top, ck, ev);
+        top = fmaxf(top, xor16(top));
+        top = fmaxf(top, xor32(top));
+        if (__any(top > m[nt] + kRise)) {
+          const float next = top > m[nt] + kRise ? top : m[nt];
+          const float f = __builtin_amdgcn_exp2f(m[nt] - next);
+          m[nt] = next;
+          l[nt] *= f;
+#pragma unroll
+          for (int i = 0; i < DT; ++i) o[nt][i] *= f;
+        }
+        const float bias = ev - m[nt];
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float p = __builtin_amdgcn_exp2f(fmaf(sc[nt][i][e], ck, bias));
+            sum += p;
+            w[nt][i >> 1][4 * (i & 1) + e] = (_Float16)p;
+          }
+        l[nt] = fmaf(sum, inv_v, l[nt]);
+      }
+#pragma unroll
+      for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const f16x8_t val = values_f16(vr[i][2 * half], vr[i][2 * half + 1]);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) o[nt][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(val, w[nt][half], o[nt][i], 0, 0, 0);
+        }
+      pk = pk_next;
+      pv = pv_next;
+    }
+  }
+
+  // join the wavefronts
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    l[nt] += xor16(l[nt]);
+    l[nt] += xor32(l[nt]);
+    float* at = joined + ((wave * NT + nt) * 16 + r16) * kPitch + 4 * g;
+#pragma unroll
+    for (int i = 0; i < DT; ++i) *reinterpret_cast<f32x4_t*>(at + 16 * i) = o[nt][i];
+    if (g == 0) {
+      stats[((wave * NT + nt) * 16 + r16) * 2] = m[nt];
+      stats[((wave * NT + nt) * 16 + r16) * 2 + 1] = l[nt];
+    }
+  }
+  __syncthreads();
+  constexpr int kQuads = D / 4;   // four dimensions to a thread
+  for (int i = threadIdx.x; i < 16 * NT * kQuads; i += 64 * kWaves) {
+    const int r = i / kQuads, d = i % kQuads * 4, row = row0 + r;
+    if (row >= rows) continue;
+    float top = kLowest;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, stats[(w * 16 * NT + r) * 2]);
+    f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+    float total = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = __builtin_amdgcn_exp2f(stats[(w * 16 * NT + r) * 2] - top);
+      total = fmaf(f, stats[(w * 16 * NT + r) * 2 + 1], total);
+      const f32x4_t part = *reinterpret_cast<const f32x4_t*>(joined + (w * 16 * NT + r) * kPitch + d);
+      sum += part * f;
+    }
+    const int64_t token = s.first + row / a.group;
+    const int head = h * a.group + row % a.group;
+    if (a.splits > 1) {
+      const int64_t at = ((int64_t)split * a.tokens + token) * a.q_heads + head;
+      *reinterpret_cast<f32x4_t*>(a.part_o + at * D + d) = sum;
+      if (d == 0) {
+        a.part_ml[at * 2] = top;
+        a.part_ml[at * 2 + 1] = total;
+      }
+    } else {
+      const float inv = total == 0.f ? 0.f : 1.f / total;
+      const u32x2_t v = {pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv)};
+      *reinterpret_cast<u32x2_t*>(a.out + token * a.o_token + head * a.o_head + d) = v;
+    }
+  }
+}
+
+// out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s, splits in index order; a wavefront to a row.
+template <int D>
+__global__ __launch_bounds__(256) void ccq_attention_join_kernel(AttnArgs a) {
+  constexpr int kPer = D / 64;
+  const int b = blockIdx.y, rows = a.max_new * a.q_heads, lane = threadIdx.x & 63;
+  const int r = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const AttnSequence s = attn_sequence(a, b);
+  if (r >= rows || r / a.q_heads >= s.n) return;
+  const int64_t row = (int64_t)s.first * a.q_heads + r, rows_all = (int64_t)a.tokens * a.q_heads;
+  const int splits = max(1, min(a.splits, (s.len - s.begin + a.chunk - 1) / a.chunk));
+  float top = kLowest;
+  for (int i = lane; i < splits; i += 64) top = fmaxf(top, a.part_ml[(i * rows_all + row) * 2]);
+  for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+  float total = 0.f, sum[kPer] = {};
+  for (int i = 0; i < splits; ++i) {
+    const int64_t at = i * rows_all + row;
+    const float f = __builtin_amdgcn_exp2f(a.part_ml[at * 2] - top);
+    total = fmaf(f, a.part_ml[at * 2 + 1], total);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) sum[j] = fmaf(f, a.part_o[at * D + lane * kPer + j], sum[j]);
+  }
+  const float inv = total == 0.f ? 0.f : 1.f / total;
+  uint16_t* out = a.out + (s.first + r / a.q_heads) * a.o_token + (int64_t)(r % a.q_heads) * a.o_head + lane * kPer;
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) out[j] = to_bf16(sum[j] * inv);
+}
+
+// How a call is cut.
+struct Plan {
+  int nt, row_tiles, chunk, splits;
+};
+Plan plan_of(const ccq_cache* c, const ccq_batch* b, const ccq_attn* at) {
+  Plan p;
+  const int64_t rows = (int64_t)b->max_new * (at->q_heads / c->kv_heads);
+  p.nt = rows <= 16 ? 1 : 2;
+  p.row_tiles = (int)((rows + 16 * p.nt - 1) / (16 * p.nt));
+  int64_t range = b->max_len;
+  if (at->window > 0) range = std::min<int64_t>(range, (int64_t)at->window + b->max_new + 63);
+  const int64_t unit = kWaves * kTile, units = std::max<int64_t>(1, (range + unit - 1) / unit), groups = (int64_t)b->batch * c->kv_heads * p.row_tiles;
+  const int64_t at_once = 3 * 256;   // workgroups that the chip holds
+  int64_t per = (units * groups + at_once - 1) / at_once;
+  per = groups >= 4 * at_once ? units : std::min<int64_t>(std::min<int64_t>(per, 8), units);
+  p.splits = (int)((units + per - 1) / per);
+  p.chunk = p.splits == 1 ? 1 << 30 : (int)(per * unit);
+  return p;
+}
+
+template <int D>
+int launch_few(const AttnArgs& a, const Plan& p, hipStream_t s) {
+  const dim3 grid((unsigned)(a.kv_heads * a.row_tiles * a.splits), (unsigned)a.batch);
+  if (p.nt == 1) hipLaunchKernelGGL((ccq_attention_few_kernel<D, 1>), grid, dim3(64 * kWaves), 0, s, a);
+  else hipLaunchKernelGGL((ccq_attention_few_kernel<D, 2>), grid, dim3(64 * kWaves), 0, s, a);
+  if (hipGetLastError() != hipSuccess) return CCQ_ERR_HIP;
+  if (a.splits > 1) {
+    const int64_t rows = (int64_t)a.max_new * a.q_heads;
+    hipLaunchKernelGGL((ccq_attention_join_kernel<D>), dim3((unsigned)((rows + 3) / 4), (unsigned)a.batch), dim3(256), 0, s, a);
+  }
+  return hipGetLastError() == hipSuccess ? CCQ_OK : CCQ_ERR_HIP;
+}
+
+}  // namespace
+
+int64_t attention_workspace(const ccq_cache* c, const ccq_batch* b, const ccq_attn* at) {
+  if (b->batch == 0 || b->max_new == 0) return 0;
+  const Plan p = plan_of(c, b, at);
+  return p.splits > 1 ? (int64_t)p.splits * b->tokens * at->q_heads * (c->head_dim + 2) * 4 : 0;
+}
+
+int launch_attention(const ccq_cache* c, const ccq_batch* b, const ccq_attn* at, const ccq_heads* q, const ccq_heads* out, void* workspace, void* stream) {
+  if (b->batch == 0 || b->max_new == 0) return CCQ_OK;
+  const Plan p = plan_of(c, b, at);
+  AttnArgs a = {};
+  a.k = static_cast<const uint8_t*>(c->k), a.v = static_cast<const uint8_t*>(c->v), a.ks = c->k_scales, a.vs = c->v_scales;
+  a.q = static_cast<const uint16_t*>(q->data), a.q_token = q->token_stride, a.q_head = q->head_stride;
+  a.out = static_cast<uint16_t*>(out->data), a.o_token = out->token_stride, a.o_head = out->head_stride;
+  a.offsets = b->offsets, a.lens = b->lens, a.table = b->table, a.ld_table = b->ld_table;
+  a.pages = c->pages, a.page_shift = __builtin_ctz((unsigned)c->page_tokens), a.kv_heads = c->kv_heads, a.q_heads = at->q_heads;
+  a.group = at->q_heads / c->kv_heads, a.table_width = b->table_width, a.batch = b->batch, a.tokens = b->tokens, a.max_new = b->max_new, a.max_len = b->max_len;
+  a.causal = at->causal, a.window = at->window, a.c = at->scale * 1.4426950408889634f;
+  a.chunk = p.chunk, a.splits = p.splits, a.row_tiles = p.row_tiles;
+  if (p.splits > 1) {
+    a.part_o = static_cast<float*>(workspace);
+    a.part_ml = a.part_o + (int64_t)p.splits * b->tokens * at->q_heads * c->head_dim;
+  }
+  if ((int64_t)a.kv_heads * a.row_tiles * a.splits > 0x7FFFFFFF || b->batch > 65535) return CCQ_ERR_BAD_PARAM;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return c->head_dim == 64 ? launch_few<64>(a, p, s) : launch_few<128>(a, p, s);
+}
+
+}  // namespace ccq

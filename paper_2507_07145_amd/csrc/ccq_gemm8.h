@@ -1,0 +1,35 @@
+// What the 8-bit product's kernels share.
+//
+//   y[m][n] = sum_b 2^ex[m][b] s[n / 128][b] sum_{k in b} x[m][k] w[n][k],   b: blocks of 128 of K
+//
+// One scaled MFMA, 16x16x128, covers a block of K: it starts from zero, takes the activations' power-of-two scale as its scale operand, and
+// its result goes into the fp32 accumulators with one multiply-add by the weights' scale, which is one number for the whole
+// tile.  The weights are the first operand: a lane then holds four neighbouring outputs of a row.
+#pragma once
+#include "ccq_layer.h"
+
+namespace ccq {
+
+typedef __attribute__((ext_vector_type(8))) int i32x8_t;
+
+struct Gemm8Args {
+  const uint8_t* w;
+  const float* ws;
+  const uint8_t* x;
+  const uint8_t* xs;
+  uint16_t* y;
+  float* partial;
+  int64_t ldw, ld_ws, ldx, ld_xs, ldy;
+  int32_t M, N, K, blocks;   // blocks: of K, the last one possibly shorter
+};
+
+__device__ __forceinline__ i32x8_t operand8(u32x4_t a, u32x4_t b) {
+  return i32x8_t{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
+}
+// A block of K: weights times activations, scaled by the activations' scale byte (the low byte of `x_scale`).
+__device__ __forceinline__ f32x4_t multiply8(i32x8_t w, i32x8_t x, int x_scale) {
+  const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, zero, 0, 0, 0, 0x7F7F7F7F, 0, x_scale);
+}
+
+}  // namespace ccq
