@@ -16,7 +16,6 @@ namespace ccq {
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8_t;
-typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 
 struct AttnArgs {
   const uint8_t *k, *v, *ks, *vs;

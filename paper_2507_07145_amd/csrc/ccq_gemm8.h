@@ -18,8 +18,8 @@ struct Gemm8Args {
   const uint8_t* x;
   const uint8_t* xs;
   uint16_t* y;
-  float* partial;
-  int64_t ldw, ld_ws, ldx, ld_xs, ldy;
+  float* partial;       // fp32 [shares][M][ld_partial]
+  int64_t ldw, ld_ws, ldx, ld_xs, ldy, ld_partial;   // ld_partial: N rounded up to a multiple of 4
   int32_t M, N, K, blocks;   // blocks: of K, the last one possibly shorter
 };
 
@@ -31,5 +31,24 @@ __device__ __forceinline__ f32x4_t multiply8(i32x8_t w, i32x8_t x, int x_scale) 
   const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, zero, 0, 0, 0, 0x7F7F7F7F, 0, x_scale);
 }
+
+// At most n of the wavefront's loads (copies to LDS among them) are still under way.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4 << 14) | 0x0F70);
+}
+// All wavefronts' LDS reads and writes before it are done, their copies from memory not: those are waited for by wait_loads.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
+  asm volatile("s_barrier" ::: "memory");
+}
+
+// Blocks of 64 mi rows (mi 1, 2, 4) and 256 columns over columns n_first .. n_first + n_count - 1, K in `shares` (more than one: all columns, fp32
+// partial results in a.partial).
+int launch_gemm8_block(const Gemm8Args& a, int mi, int n_first, int n_count, int shares, void* stream);
+
+// Tiles of 16 mt rows (mt 1, 2, 3, 4, 6) and 128 columns.
+int launch_gemm8_stream(const Gemm8Args& a, int mt, int shares, void* stream);
+int launch_gemm8_add(const Gemm8Args& a, int shares, void* stream);   // y = sum of the shares
 
 }  // namespace ccq

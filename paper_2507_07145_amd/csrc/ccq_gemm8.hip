@@ -2,6 +2,9 @@
 //
 // A workgroup owns 16 outputs (of all rows of a tile of 16 MT rows); its wavefronts take the blocks of K in turn and their
 // accumulators are added through LDS at the end, in a fixed order.  Bound by memory: the weights' bytes.
+#include <algorithm>
+#include <cmath>
+
 #include "ccq_gemm8.h"
 
 namespace ccq {
@@ -32,7 +35,6 @@ __global__ __launch_bounds__(64 * W) void ccq_gemm8_few_kernel(Gemm8Args a) {
     if (k >= a.K) v = u32x4_t{0, 0, 0, 0};
     return v;
   };
-#pragma unroll 4
   for (int kb = wave; kb < a.blocks; kb += W) {
     const int k = kb * kScaleBlock + 16 * g;
     const i32x8_t wv = operand8(piece(w, k), piece(w, k + 64));
@@ -58,19 +60,163 @@ __global__ __launch_bounds__(64 * W) void ccq_gemm8_few_kernel(Gemm8Args a) {
 
 }  // namespace
 
-int64_t gemm8_workspace(const ccq_weight8*, int) { return 0; }
+namespace {
 
-int launch_gemm8(const ccq_weight8* w, const ccq_rows8* x, int M, void* y, int64_t ldy, void* workspace, void* stream) {
+Gemm8Args args_of(const ccq_weight8* w, const ccq_rows8* x, int M, void* y, int64_t ldy, void* workspace) {
   Gemm8Args a;
   a.w = static_cast<const uint8_t*>(w->codes), a.ws = w->scales, a.ldw = w->ldw, a.ld_ws = w->ld_scales;
   a.x = static_cast<const uint8_t*>(x->codes), a.xs = x->scales, a.ldx = x->ld, a.ld_xs = x->ld_scales;
   a.y = static_cast<uint16_t*>(y), a.ldy = ldy, a.partial = static_cast<float*>(workspace);
   a.M = M, a.N = w->N, a.K = w->K, a.blocks = (w->K + kScaleBlock - 1) / kScaleBlock;
-  hipStream_t s = static_cast<hipStream_t>(stream);
-  const unsigned nt = (unsigned)((a.N + 15) / 16);
-  if (M <= 16) hipLaunchKernelGGL((ccq_gemm8_few_kernel<1, 4>), dim3(nt, 1), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((ccq_gemm8_few_kernel<4, 4>), dim3(nt, (unsigned)((M + 63) / 64)), dim3(256), 0, s, a);
+  a.ld_partial = (int64_t)(a.N + 3) / 4 * 4;
+  return a;
+}
+
+template <int MT, int W>
+int launch_few(const Gemm8Args& a, hipStream_t s) {
+  hipLaunchKernelGGL((ccq_gemm8_few_kernel<MT, W>), dim3((unsigned)((a.N + 15) / 16), (unsigned)((a.M + 16 * MT - 1) / (16 * MT))), dim3(64 * W), 0, s, a);
   return hipGetLastError() == hipSuccess ? CCQ_OK : CCQ_ERR_HIP;
+}
+
+// How a call is served: `kind` few rows (mt: 16-row tiles of a workgroup, waves), stream (mt, shares), block (mt: 64-row units, shares; columns
+// from n_rest on, if any are left out, in blocks of mt_rest).
+enum Kind8 { kFew = 0, kStream = 1, kBlock = 2 };
+struct Plan8 {
+  int kind = kFew, mt = 1, shares = 1, waves = 4, n_rest = 0, mt_rest = 0;
+  double time = 1e30;   // estimate, microseconds
+};
+
+int run(const Gemm8Args& a, const Plan8& p, void* stream) {
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (p.kind == kFew) return p.mt == 4 ? launch_few<4, 4>(a, s) : p.waves == 16 ? launch_few<1, 16>(a, s) : launch_few<1, 4>(a, s);
+  if (p.kind == kStream) return launch_gemm8_stream(a, p.mt, p.shares, stream);
+  const int n = p.n_rest > 0 ? p.n_rest : a.N;
+  const int rc = launch_gemm8_block(a, p.mt, 0, n, p.shares, stream);
+  return rc != CCQ_OK || n == a.N ? rc : launch_gemm8_block(a, p.mt_rest, n, a.N - n, 1, stream);
+}
+
+// The kernels' times as they were measured on K = 8192, N = 8192 and 28672, M = 1 .. 2048 (and short and narrow products), as lines in the steps of a
+// workgroup and the share of the chip that is busy: within about 15 % of all of them, which are further apart than that where the choice matters.
+constexpr double kCus = 256.0;
+double rounds_of(double groups) { return std::ceil(groups / kCus); }
+double busy(double groups) { return std::min(1.0, groups / (kCus * rounds_of(groups))); }
+double add_time(double shares, double M, double N) { return shares > 1 ? 2.0 + shares * M * N * 4.0 / 5e6 : 0.0; }
+double few_time(int mt, int waves, int M, int N, int blocks) {
+  const double tiles = (N + 15) / 16, its = (blocks + waves - 1) / waves;
+  if (mt == 4) return 4.0 + its * std::ceil(M / 64.0) * (1.2 + 2.3 * std::min(4.0, tiles / 512.0));
+  return std::max(2.5 + (double)N * blocks * kScaleBlock / 5.7e6 * (1.0 + 0.04 * (M - 1)), 4.0 + its * (waves == 16 ? 1.0 : 0.4));
+}
+double stream_time(int mt, int shares, int M, int N, int blocks) {
+  const double groups = (double)((N + 127) / 128) * shares * ((M + 16 * mt - 1) / (16 * mt)), steps = std::ceil(std::ceil((double)blocks / shares) / 2.0);
+  return 4.0 + rounds_of(groups) * (1.0 + steps * (0.75 + 0.1 * mt + 0.6 * busy(groups))) + add_time(shares, M, N);
+}
+// `alone`: one block of rows, whose weights come from memory and not from a neighbour's reading
+double block_rounds_time(int mi, double groups, double steps, bool alone) {
+  const double full = busy(groups);
+  const double per = mi == 4 ? 1.75 + 0.55 * full : mi == 2 ? (alone ? 1.1 + 0.6 * full : 0.9 + 0.3 * full) : alone ? 1.0 + 0.45 * full : 0.75 + 0.3 * full;
+  return rounds_of(groups) * ((alone ? 5.0 : 2.0) + steps * per);
+}
+double block_groups(int mi, int M, int n, int shares) { return (double)((M + 64 * mi - 1) / (64 * mi)) * ((n + 255) / 256) * shares; }
+
+Plan8 find_plan(int M, int N, int K) {
+  const int blocks = (K + kScaleBlock - 1) / kScaleBlock;
+  Plan8 best;
+  auto offer = [&](const Plan8& p) {
+    if (p.time < best.time) best = p;
+  };
+  auto few = [&](int mt, int waves) {
+    Plan8 p;
+    p.kind = kFew, p.mt = mt, p.waves = waves, p.time = few_time(mt, waves, M, N, blocks);
+    offer(p);
+  };
+  if (M <= 16) {
+    few(1, 16);
+    if (M > 4) few(1, 4);
+  }
+  if (M <= 64) few(4, 4);
+  static const int kShares[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 16, 24, 32};
+  if (M <= 192) {
+    for (const int mt : {1, 2, 3, 4, 6}) {
+      if (mt > 1 && 16 * (mt - 1) >= M) break;   // (rows of nothing)
+      if (M > 16 * mt && mt < 4) continue;       // (a tile of all rows, or the larger ones)
+      for (const int shares : kShares) {
+        if (shares > 1 && shares * 2 > blocks) break;
+        Plan8 p;
+        p.kind = kStream, p.mt = mt, p.shares = shares, p.time = stream_time(mt, shares, M, N, blocks);
+        offer(p);
+      }
+    }
+  }
+  if (M > 32) {
+    const double bytes = 4.0 + ((double)N * K + (double)M * K + 2.0 * M * N) / 4.9e6;
+    for (const int mi : {1, 2, 4}) {
+      if (mi > 1 && M <= 32 * mi) break;
+      for (const int shares : kShares) {
+        if (shares > 1 && (shares * 4 > blocks || (double)shares * M * N * 4 > 256e6)) break;
+        Plan8 p;
+        p.kind = kBlock, p.mt = mi, p.shares = shares;
+        p.time = std::max(bytes, 4.0 + block_rounds_time(mi, block_groups(mi, M, N, shares), std::ceil((double)blocks / shares), M <= 64 * mi)) + add_time(shares, M, N);
+        offer(p);
+      }
+      // whole rounds of the chip in these blocks, the columns that are left in smaller ones
+      const int m_tiles = (M + 64 * mi - 1) / (64 * mi), n_tiles = (N + 255) / 256, full = (int)((int64_t)m_tiles * n_tiles / 256) * 256 / m_tiles;
+      if (mi > 1 && full > 0 && full < n_tiles) {
+        for (const int rest : {1, 2}) {
+          if (rest >= mi) break;
+          Plan8 p;
+          p.kind = kBlock, p.mt = mi, p.n_rest = full * 256, p.mt_rest = rest;
+          p.time = 6.0 + block_rounds_time(mi, block_groups(mi, M, p.n_rest, 1), blocks, M <= 64 * mi) +
+                   block_rounds_time(rest, block_groups(rest, M, N - p.n_rest, 1), blocks, false);
+          offer(p);
+        }
+      }
+    }
+  }
+  return best;
+}
+
+// The plans of the sizes that a thread asked for last: finding one takes up to 5 us of host time.
+Plan8 plan_of(int M, int N, int K) {
+  struct Known {
+    int M = 0, N = 0, K = 0;
+    Plan8 plan;
+  };
+  static thread_local Known known[64];
+  Known& k = known[((unsigned)M * 31 + (unsigned)N * 7 + (unsigned)K / 16) % 64];
+  if (k.M != M || k.N != N || k.K != K) {
+    k.plan = find_plan(M, N, K);
+    k.M = M, k.N = N, k.K = K;
+  }
+  return k.plan;
+}
+
+}  // namespace
+
+int64_t gemm8_workspace(const ccq_weight8* w, int M) {
+  if (M <= 0) return 0;
+  const Plan8 p = plan_of(M, w->N, w->K);
+  return p.shares > 1 ? (int64_t)p.shares * M * (((int64_t)w->N + 3) / 4 * 4) * 4 : 0;
+}
+
+int launch_gemm8(const ccq_weight8* w, const ccq_rows8* x, int M, void* y, int64_t ldy, void* workspace, void* stream) {
+  const Gemm8Args a = args_of(w, x, M, y, ldy, workspace);
+  Plan8 p = plan_of(M, a.N, a.K);
+  if (a.ldw > (1 << 23) || a.ldx > (1 << 23)) p = Plan8{kFew, 4, 1, 4, 0, 0, 0.0};   // too far apart for 32-bit offsets within the block kernel's 256 rows
+  return run(a, p, stream);
+}
+
+// For tests, no part of the interface: how a call of these sizes is served (six numbers of the plan, and the estimate), and a call as a named plan, whose
+// arguments are not checked.
+extern "C" void ccq_gemm8_plan(int32_t M, int32_t N, int32_t K, int32_t* out, double* time) {
+  const Plan8 p = plan_of(M, N, K);
+  const int v[6] = {p.kind, p.mt, p.shares, p.waves, p.n_rest, p.mt_rest};
+  for (int i = 0; i < 6; ++i) out[i] = v[i];
+  *time = p.time;
+}
+extern "C" int ccq_gemm8_as(const ccq_weight8* w, const ccq_rows8* x, int32_t M, void* y, int64_t ldy, void* workspace, const int32_t* plan, void* stream) {
+  Plan8 p;
+  p.kind = plan[0], p.mt = plan[1], p.shares = plan[2], p.waves = plan[3], p.n_rest = plan[4], p.mt_rest = plan[5];
+  return run(args_of(w, x, M, y, ldy, workspace), p, stream);
 }
 
 }  // namespace ccq

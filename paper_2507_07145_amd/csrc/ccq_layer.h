@@ -14,6 +14,7 @@ constexpr int kCacheExp = 60;      // exponents of the cache's scales lie in [-6
 
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
 typedef __attribute__((ext_vector_type(4))) float f32x4_t;
+typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
 
 // The least e with amax <= 448 * 2^e, as e + 127: 448 = 1.75 * 2^8.  `bits`: amax's fp32 bits, finite.
