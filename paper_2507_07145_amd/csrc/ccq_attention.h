@@ -78,4 +78,7 @@ __device__ __forceinline__ u32x4_t keep_tokens(u32x4_t v, int t0, int lo, int hi
   return v;
 }
 
+// The kernel for many rows: workgroups of `waves` (4 or 8) times 32 rows; a.row_tiles counts them.
+int launch_attention_rows(const AttnArgs& a, int head_dim, int waves, void* stream);
+
 }  // namespace ccq

@@ -251,22 +251,38 @@ __global__ __launch_bounds__(256) void ccq_attention_join_kernel(AttnArgs a) {
 
 // How a call is cut.
 struct Plan {
-  int nt, row_tiles, chunk, splits;
+  int nt = 0;      // 16-row tiles of a workgroup of the kernel for few rows, or
+  int waves = 0;   // wavefronts of 32 rows of the kernel for many
+  int row_tiles = 0, chunk = 0, splits = 0;
 };
+int forced_waves = -1;   // (tests: the kernel for many rows with so many wavefronts, 0: the other)
 Plan plan_of(const ccq_cache* c, const ccq_batch* b, const ccq_attn* at) {
   Plan p;
-  const int64_t rows = (int64_t)b->max_new * (at->q_heads / c->kv_heads);
-  p.nt = rows <= 16 ? 1 : 2;
-  p.row_tiles = (int)((rows + 16 * p.nt - 1) / (16 * p.nt));
+  const int64_t rows = (int64_t)b->max_new * (at->q_heads / c->kv_heads), pairs = (int64_t)b->batch * c->kv_heads;
   int64_t range = b->max_len;
   if (at->window > 0) range = std::min<int64_t>(range, (int64_t)at->window + b->max_new + 63);
-  const int64_t unit = kWaves * kTile, units = std::max<int64_t>(1, (range + unit - 1) / unit), groups = (int64_t)b->batch * c->kv_heads * p.row_tiles;
-  const int64_t at_once = 3 * 256;   // workgroups that the chip holds
+  // up to 32 rows the tile of the kernel for many would be less than full
+  if (forced_waves >= 0 ? forced_waves > 0 : rows > 32) {
+    p.waves = forced_waves > 0 ? forced_waves : 8;
+    p.row_tiles = (int)((rows + 32 * p.waves - 1) / (32 * p.waves));
+  } else {
+    p.nt = rows <= 16 ? 1 : 2;
+    p.row_tiles = (int)((rows + 16 * p.nt - 1) / (16 * p.nt));
+  }
+  const int64_t unit = kWaves * kTile, units = std::max<int64_t>(1, (range + unit - 1) / unit), groups = pairs * p.row_tiles;
+  const int64_t at_once = p.waves ? 256 : 3 * 256;   // workgroups that the chip holds
   int64_t per = (units * groups + at_once - 1) / at_once;
-  per = groups >= 4 * at_once ? units : std::min<int64_t>(std::min<int64_t>(per, 8), units);
+  per = groups >= 4 * at_once || (p.waves && groups >= at_once) ? units : std::min<int64_t>(std::min<int64_t>(per, 8), units);
   p.splits = (int)((units + per - 1) / per);
   p.chunk = p.splits == 1 ? 1 << 30 : (int)(per * unit);
   return p;
+}
+
+template <int D>
+int launch_join(const AttnArgs& a, hipStream_t s) {
+  const int64_t rows = (int64_t)a.max_new * a.q_heads;
+  hipLaunchKernelGGL((ccq_attention_join_kernel<D>), dim3((unsigned)((rows + 3) / 4), (unsigned)a.batch), dim3(256), 0, s, a);
+  return hipGetLastError() == hipSuccess ? CCQ_OK : CCQ_ERR_HIP;
 }
 
 template <int D>
@@ -274,11 +290,6 @@ int launch_few(const AttnArgs& a, const Plan& p, hipStream_t s) {
   const dim3 grid((unsigned)(a.kv_heads * a.row_tiles * a.splits), (unsigned)a.batch);
   if (p.nt == 1) hipLaunchKernelGGL((ccq_attention_few_kernel<D, 1>), grid, dim3(64 * kWaves), 0, s, a);
   else hipLaunchKernelGGL((ccq_attention_few_kernel<D, 2>), grid, dim3(64 * kWaves), 0, s, a);
-  if (hipGetLastError() != hipSuccess) return CCQ_ERR_HIP;
-  if (a.splits > 1) {
-    const int64_t rows = (int64_t)a.max_new * a.q_heads;
-    hipLaunchKernelGGL((ccq_attention_join_kernel<D>), dim3((unsigned)((rows + 3) / 4), (unsigned)a.batch), dim3(256), 0, s, a);
-  }
   return hipGetLastError() == hipSuccess ? CCQ_OK : CCQ_ERR_HIP;
 }
 
@@ -308,7 +319,13 @@ int launch_attention(const ccq_cache* c, const ccq_batch* b, const ccq_attn* at,
   }
   if ((int64_t)a.kv_heads * a.row_tiles * a.splits > 0x7FFFFFFF || b->batch > 65535) return CCQ_ERR_BAD_PARAM;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  return c->head_dim == 64 ? launch_few<64>(a, p, s) : launch_few<128>(a, p, s);
+  const int rc = p.waves ? launch_attention_rows(a, c->head_dim, p.waves, stream) : c->head_dim == 64 ? launch_few<64>(a, p, s) : launch_few<128>(a, p, s);
+  if (rc != CCQ_OK || p.splits == 1) return rc;
+  return c->head_dim == 64 ? launch_join<64>(a, s) : launch_join<128>(a, s);
 }
+
+// For tests, no part of the interface: all calls from now on take the kernel for many rows with 4 or 8 wavefronts, or (0) the one for few, or (-1)
+// what the rule says.
+extern "C" void ccq_attention_force(int32_t waves) { forced_waves = waves; }
 
 }  // namespace ccq
