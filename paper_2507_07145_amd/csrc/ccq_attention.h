@@ -29,7 +29,7 @@ struct AttnArgs {
   int32_t pages, page_shift, kv_heads, q_heads, group, table_width, batch, tokens, max_new, max_len;
   int32_t causal, window;
   int32_t chunk, splits;
-  int32_t row_tiles;
+  int32_t row_tiles, tile_rows;
   float c;          // scale * log2(e)
 };
 
@@ -38,7 +38,6 @@ constexpr float kRise = 8.f;
 
 struct AttnSequence {
   int first, n, old, len;   // first token row, new tokens, tokens before them, cached tokens with them
-  int begin;                // first cached token that a row sees, rounded down to 64
 };
 __device__ __forceinline__ int first_seen(const AttnArgs& a, int p) { return a.window > 0 ? max(0, p - a.window + 1) : 0; }
 __device__ __forceinline__ AttnSequence attn_sequence(const AttnArgs& a, int b) {
@@ -49,11 +48,29 @@ __device__ __forceinline__ AttnSequence attn_sequence(const AttnArgs& a, int b) 
   s.old = s.len - s.n;
   s.n = min(s.n, a.max_new);
   s.len = min(min(s.len, a.max_len), (int)min((int64_t)a.table_width << a.page_shift, (int64_t)0x7FFFFFFF));
-  s.begin = min(first_seen(a, s.old), max(s.len, 0)) & ~63;
   return s;
 }
 // Cached tokens [first, second) that the row at position p sees.
 __device__ __forceinline__ int seen_end(const AttnArgs& a, const AttnSequence& s, int p) { return a.causal ? min(max(p + 1, 0), s.len) : s.len; }
+
+// Rows [first_row, last_row] of a tile and what they see: any of them, all of them; the tile's splits begin at `begin`, every a.chunk tokens.
+struct AttnTile {
+  int first_row, last_row;
+  int any_lo, any_hi, all_lo, all_hi, begin;
+  __device__ __forceinline__ int splits(const AttnArgs& a) const { return max(1, min(a.splits, (any_hi - begin - 1) / a.chunk + 1)); }
+};
+__device__ __forceinline__ AttnTile attn_tile(const AttnArgs& a, const AttnSequence& s, int first_row, int rows) {
+  AttnTile t;
+  t.first_row = first_row;
+  t.last_row = min(first_row + rows, s.n * a.group) - 1;
+  const int p_first = s.old + t.first_row / a.group, p_last = s.old + t.last_row / a.group;
+  t.any_lo = first_seen(a, p_first);
+  t.any_hi = seen_end(a, s, p_last);
+  t.all_lo = first_seen(a, p_last);
+  t.all_hi = seen_end(a, s, p_first);
+  t.begin = min(t.any_lo, max(s.len, 0)) & ~63;
+  return t;
+}
 
 __device__ __forceinline__ f16x8_t values_f16(uint32_t lo, uint32_t hi) {
   typedef __attribute__((ext_vector_type(2))) _Float16 pair;
@@ -78,7 +95,8 @@ __device__ __forceinline__ u32x4_t keep_tokens(u32x4_t v, int t0, int lo, int hi
   return v;
 }
 
-// The kernel for many rows: workgroups of `waves` (4 or 8) times 32 rows; a.row_tiles counts them.
-int launch_attention_rows(const AttnArgs& a, int head_dim, int waves, void* stream);
+// The kernel for many rows: workgroups of kManyRows; a.row_tiles counts them.
+constexpr int kManyRows = 256;
+int launch_attention_rows(const AttnArgs& a, int head_dim, void* stream);
 
 }  // namespace ccq

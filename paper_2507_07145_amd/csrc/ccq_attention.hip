@@ -19,7 +19,7 @@ namespace {
 constexpr int kTile = 64, kWaves = 4;
 
 template <int D, int NT>
-__global__ __launch_bounds__(64 * kWaves) void ccq_attention_few_kernel(AttnArgs a) {
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))) void ccq_attention_few_kernel(AttnArgs a) {
   constexpr int KP = D / 64;     // 16-byte pieces of a key in a lane: dimensions 64 p + 16 g .. + 15
   constexpr int DT = D / 16;     // tiles of dimensions
   constexpr int STEPS = D / 32;
@@ -31,20 +31,16 @@ __global__ __launch_bounds__(64 * kWaves) void ccq_attention_few_kernel(AttnArgs
   const AttnSequence s = attn_sequence(a, b);
   const int rows = s.n * a.group, row0 = tile * (16 * NT);
   if (row0 >= rows) return;
-  const int last_row = min(row0 + 16 * NT, rows) - 1;
-  const int p_first = s.old + row0 / a.group, p_last = s.old + last_row / a.group;   // positions of the tile's rows
-  // tokens that all rows see, and that any sees
-  const int all_lo = first_seen(a, p_last), all_hi = seen_end(a, s, p_first), any_lo = first_seen(a, p_first), any_hi = seen_end(a, s, p_last);
-  const int begin = s.begin + split * a.chunk, end = begin + min(a.chunk, s.len - begin);
-  if (split > 0 && begin >= s.len) return;   // (the first one answers for rows that see nothing)
-  const int from = max(begin, any_lo & ~(kTile - 1)), to = min(end, any_hi);
+  const AttnTile t = attn_tile(a, s, row0, 16 * NT);
+  if (split >= t.splits(a)) return;
+  const int begin = t.begin + split * a.chunk, from = begin, to = begin + min(a.chunk, t.any_hi - begin);
 
   // queries: the same dimensions as a lane's pieces of the keys
   bf16x8_t q[NT][STEPS];
   int lo[NT], hi[NT];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    const int row = min(row0 + nt * 16 + r16, last_row), token = row / a.group;
+    const int row = min(row0 + nt * 16 + r16, t.last_row), token = row / a.group;
     const uint16_t* at = a.q + (int64_t)(s.first + token) * a.q_token + (int64_t)(h * a.group + row % a.group) * a.q_head;
 #pragma unroll
     for (int i = 0; i < STEPS; ++i)
@@ -65,12 +61,9 @@ __global__ __launch_bounds__(64 * kWaves) void ccq_attention_few_kernel(AttnArgs
 
   const int32_t* pages = a.table + b * a.ld_table;
   const int in_page = (1 << a.page_shift) - 1;
-  // page of a quarter of the tile at t0, -1 where there is none
-  auto page_at = [&](int t0, int quarter) {
-    const int t = t0 + 16 * quarter;
-    const int p = t < to ? pages[t >> a.page_shift] : -1;
-    return p < a.pages ? p : -1;
-  };
+  // Table entry of a quarter of the tile at t0; looked at a tile later (its page, -1 where there is none), so that nothing waits for it.
+  auto entry_at = [&](int t0, int quarter) { return pages[min(t0 + 16 * quarter, to - 1) >> a.page_shift]; };
+  auto page_of = [&](int entry) { return entry < a.pages ? entry : -1; };
   const int quarter_k = r16 >> 2;
   u32x4_t kr[4][KP], vr[DT];
   auto load_keys = [&](int t0, int page) {
@@ -91,12 +84,11 @@ __global__ __launch_bounds__(64 * kWaves) void ccq_attention_few_kernel(AttnArgs
   int t0 = from + wave * kTile;
   const int stride = kWaves * kTile;
   if (t0 < to) {
-    int pk = page_at(t0, quarter_k), pv = page_at(t0, g);
-    load_keys(t0, pk);
+    int pv = page_of(entry_at(t0, g)), next_k = entry_at(t0 + stride, quarter_k), next_v = entry_at(t0 + stride, g);
+    load_keys(t0, page_of(entry_at(t0, quarter_k)));
+    int64_t scale_at = (int64_t)max(pv, 0) * a.kv_heads + h;
+    int k_byte = a.ks[scale_at], v_byte = a.vs[scale_at];
     for (; t0 < to; t0 += stride) {
-      const int pk_next = page_at(t0 + stride, quarter_k), pv_next = page_at(t0 + stride, g);
-      const int64_t at = (int64_t)max(pv, 0) * a.kv_heads + h;
-      const int kb = a.ks[at], vb = a.vs[at];
       load_values(t0, pv);
       f32x4_t sc[NT][4];
 #pragma unroll
@@ -112,9 +104,15 @@ __global__ __launch_bounds__(64 * kWaves) void ccq_attention_few_kernel(AttnArgs
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) sc[nt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q[nt][step], sc[nt][i], 0, 0, 0);
         }
-      load_keys(t0 + stride, pk_next);   // (past the end: page 0, never used)
-      const float ck = a.c * pow2_of_byte(kb), ev = (float)(vb - 127), inv_v = inverse_of_byte(vb);
-      const bool whole = t0 >= all_lo && t0 + kTile <= min(all_hi, to) && __all(pv >= 0);
+      const float ck = a.c * pow2_of_byte(k_byte), ev = (float)(v_byte - 127), inv_v = inverse_of_byte(v_byte);
+      const int pv_next = page_of(next_v);
+      load_keys(t0 + stride, page_of(next_k));   // (past the end the last page's, never used)
+      scale_at = (int64_t)max(pv_next, 0) * a.kv_heads + h;
+      k_byte = a.ks[scale_at];
+      v_byte = a.vs[scale_at];
+      next_k = entry_at(t0 + 2 * stride, quarter_k);
+      next_v = entry_at(t0 + 2 * stride, g);
+      const bool whole = t0 >= t.all_lo && t0 + kTile <= min(t.all_hi, to) && __all(pv >= 0);
       if (!whole) {
         const int token0 = t0 + 16 * g;
 #pragma unroll
@@ -129,7 +127,7 @@ __global__ __launch_bounds__(64 * kWaves) void ccq_attention_few_kernel(AttnArgs
             }
         }
 #pragma unroll
-        for (int i = 0; i < DT; ++i) vr[i] = keep_tokens(vr[i], token0, pv >= 0 ? any_lo : 0x7FFFFFFF, to);
+        for (int i = 0; i < DT; ++i) vr[i] = keep_tokens(vr[i], token0, pv >= 0 ? t.any_lo : 0x7FFFFFFF, to);
       }
       f16x8_t w[NT][2];
 #pragma unroll
@@ -170,7 +168,6 @@ __global__ __launch_bounds__(64 * kWaves) void ccq_attention_few_kernel(AttnArgs
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) o[nt][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(val, w[nt][half], o[nt][i], 0, 0, 0);
         }
-      pk = pk_next;
       pv = pv_next;
     }
   }
@@ -222,66 +219,121 @@ __global__ __launch_bounds__(64 * kWaves) void ccq_attention_few_kernel(AttnArgs
   }
 }
 
-// out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s, splits in index order; a wavefront to a row.
+// out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s, splits in a fixed order.  Of up to kFewSplits a thread adds four dimensions of a row, split
+// after split (2 splits of 16384 rows: TODO us, with a workgroup to a row 20).
+constexpr int kFewSplits = 8;
+__device__ __forceinline__ int splits_of(const AttnArgs& a, const AttnSequence& s, int r) {   // r: new token * q_heads + q head
+  const int row = r / a.q_heads * a.group + r % a.q_heads % a.group;
+  return attn_tile(a, s, row / a.tile_rows * a.tile_rows, a.tile_rows).splits(a);
+}
 template <int D>
-__global__ __launch_bounds__(256) void ccq_attention_join_kernel(AttnArgs a) {
-  constexpr int kPer = D / 64;
-  const int b = blockIdx.y, rows = a.max_new * a.q_heads, lane = threadIdx.x & 63;
-  const int r = blockIdx.x * 4 + (threadIdx.x >> 6);
+__global__ __launch_bounds__(256) void ccq_attention_join_few_kernel(AttnArgs a) {
+  constexpr int kQuads = D / 4;
+  const int b = blockIdx.y, r = blockIdx.x * (256 / kQuads) + threadIdx.x / kQuads, quad = threadIdx.x % kQuads;
   const AttnSequence s = attn_sequence(a, b);
-  if (r >= rows || r / a.q_heads >= s.n) return;
+  if (r / a.q_heads >= s.n) return;
   const int64_t row = (int64_t)s.first * a.q_heads + r, rows_all = (int64_t)a.tokens * a.q_heads;
-  const int splits = max(1, min(a.splits, (s.len - s.begin + a.chunk - 1) / a.chunk));
+  const int splits = splits_of(a, s, r);
+  float m[kFewSplits], l[kFewSplits];
+  f32x4_t o[kFewSplits];
   float top = kLowest;
-  for (int i = lane; i < splits; i += 64) top = fmaxf(top, a.part_ml[(i * rows_all + row) * 2]);
-  for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-  float total = 0.f, sum[kPer] = {};
-  for (int i = 0; i < splits; ++i) {
-    const int64_t at = i * rows_all + row;
-    const float f = __builtin_amdgcn_exp2f(a.part_ml[at * 2] - top);
-    total = fmaf(f, a.part_ml[at * 2 + 1], total);
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) sum[j] = fmaf(f, a.part_o[at * D + lane * kPer + j], sum[j]);
+  for (int i = 0; i < kFewSplits; ++i) {   // (of splits that there are not: the last one's, not added)
+    const int64_t at = min(i, splits - 1) * rows_all + row;
+    m[i] = a.part_ml[at * 2];
+    l[i] = a.part_ml[at * 2 + 1];
+    o[i] = *reinterpret_cast<const f32x4_t*>(a.part_o + at * D + 4 * quad);
+    top = fmaxf(top, m[i]);
+  }
+  f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+  float total = 0.f;
+#pragma unroll
+  for (int i = 0; i < kFewSplits; ++i) {
+    if (i >= splits) continue;
+    const float f = __builtin_amdgcn_exp2f(m[i] - top);
+    total = fmaf(f, l[i], total);
+    sum += o[i] * f;
   }
   const float inv = total == 0.f ? 0.f : 1.f / total;
-  uint16_t* out = a.out + (s.first + r / a.q_heads) * a.o_token + (int64_t)(r % a.q_heads) * a.o_head + lane * kPer;
-#pragma unroll
-  for (int j = 0; j < kPer; ++j) out[j] = to_bf16(sum[j] * inv);
+  uint16_t* out = a.out + (s.first + r / a.q_heads) * a.o_token + (int64_t)(r % a.q_heads) * a.o_head + 4 * quad;
+  *reinterpret_cast<u32x2_t*>(out) = u32x2_t{pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv)};
+}
+
+// Of more, a workgroup has a row, its threads side by side over four dimensions each and over the splits (86 splits of one long sequence: 5.5 us, with a
+// wavefront to a row, one split after the other, 27).
+constexpr int kMostSplits = 1024;
+template <int D>
+__global__ __launch_bounds__(256) void ccq_attention_join_kernel(AttnArgs a) {
+  constexpr int kQuads = D / 4, kGroups = 256 / kQuads;
+  __shared__ float weight[kMostSplits], tops[4], totals[4];
+  __shared__ __align__(16) float sums[kGroups * D];
+  const int b = blockIdx.y, r = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const AttnSequence s = attn_sequence(a, b);
+  if (r / a.q_heads >= s.n) return;
+  const int64_t row = (int64_t)s.first * a.q_heads + r, rows_all = (int64_t)a.tokens * a.q_heads;
+  const int splits = splits_of(a, s, r);
+  float top = kLowest;
+  for (int i = threadIdx.x; i < splits; i += 256) top = fmaxf(top, a.part_ml[(i * rows_all + row) * 2]);
+  for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+  if (lane == 0) tops[wave] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+  float total = 0.f;
+  for (int i = threadIdx.x; i < splits; i += 256) {
+    const float f = __builtin_amdgcn_exp2f(a.part_ml[(i * rows_all + row) * 2] - top);
+    weight[i] = f;
+    total = fmaf(f, a.part_ml[(i * rows_all + row) * 2 + 1], total);
+  }
+  for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d);
+  if (lane == 0) totals[wave] = total;
+  __syncthreads();
+  total = (totals[0] + totals[1]) + (totals[2] + totals[3]);
+  const int group = threadIdx.x / kQuads, quad = threadIdx.x % kQuads;
+  f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int i = group; i < splits; i += kGroups) sum += *reinterpret_cast<const f32x4_t*>(a.part_o + (i * rows_all + row) * D + 4 * quad) * weight[i];
+  *reinterpret_cast<f32x4_t*>(sums + group * D + 4 * quad) = sum;
+  __syncthreads();
+  if (group > 0) return;
+  for (int i = 1; i < kGroups; ++i) sum += *reinterpret_cast<const f32x4_t*>(sums + i * D + 4 * quad);
+  const float inv = total == 0.f ? 0.f : 1.f / total;
+  uint16_t* out = a.out + (s.first + r / a.q_heads) * a.o_token + (int64_t)(r % a.q_heads) * a.o_head + 4 * quad;
+  *reinterpret_cast<u32x2_t*>(out) = u32x2_t{pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv)};
 }
 
 // How a call is cut.
 struct Plan {
-  int nt = 0;      // 16-row tiles of a workgroup of the kernel for few rows, or
-  int waves = 0;   // wavefronts of 32 rows of the kernel for many
-  int row_tiles = 0, chunk = 0, splits = 0;
+  bool many = false;   // the kernel for many rows
+  int nt = 0;          // the one for few: 16-row tiles of a workgroup
+  int tile_rows = 0, row_tiles = 0, chunk = 0, splits = 0;
 };
-int forced_waves = -1;   // (tests: the kernel for many rows with so many wavefronts, 0: the other)
+int forced = -1;   // (tests: 1 the kernel for many rows, 0 the one for few)
 Plan plan_of(const ccq_cache* c, const ccq_batch* b, const ccq_attn* at) {
   Plan p;
   const int64_t rows = (int64_t)b->max_new * (at->q_heads / c->kv_heads), pairs = (int64_t)b->batch * c->kv_heads;
-  int64_t range = b->max_len;
-  if (at->window > 0) range = std::min<int64_t>(range, (int64_t)at->window + b->max_new + 63);
   // up to 32 rows the tile of the kernel for many would be less than full
-  if (forced_waves >= 0 ? forced_waves > 0 : rows > 32) {
-    p.waves = forced_waves > 0 ? forced_waves : 8;
-    p.row_tiles = (int)((rows + 32 * p.waves - 1) / (32 * p.waves));
-  } else {
-    p.nt = rows <= 16 ? 1 : 2;
-    p.row_tiles = (int)((rows + 16 * p.nt - 1) / (16 * p.nt));
-  }
+  p.many = forced >= 0 ? forced == 1 : rows > 32;
+  if (!p.many) p.nt = rows <= 16 ? 1 : 2;
+  p.tile_rows = p.many ? kManyRows : 16 * p.nt;
+  p.row_tiles = (int)((rows + p.tile_rows - 1) / p.tile_rows);
+  // tokens that a tile of rows can see
+  int64_t range = b->max_len;
+  if (at->window > 0) range = std::min<int64_t>(range, (int64_t)at->window + std::min<int64_t>(b->max_new, p.tile_rows / (at->q_heads / c->kv_heads) + 1) + 63);
   const int64_t unit = kWaves * kTile, units = std::max<int64_t>(1, (range + unit - 1) / unit), groups = pairs * p.row_tiles;
-  const int64_t at_once = p.waves ? 256 : 3 * 256;   // workgroups that the chip holds
+  const int64_t at_once = p.many ? 256 : 3 * 256;   // workgroups that the chip holds
   int64_t per = (units * groups + at_once - 1) / at_once;
-  per = groups >= 4 * at_once || (p.waves && groups >= at_once) ? units : std::min<int64_t>(std::min<int64_t>(per, 8), units);
+  const int64_t least = (units + kMostSplits - 1) / kMostSplits;
+  per = groups >= 4 * at_once || (p.many && groups >= at_once) ? units : std::max(least, std::min<int64_t>(std::min<int64_t>(per, 8), units));
   p.splits = (int)((units + per - 1) / per);
-  p.chunk = p.splits == 1 ? 1 << 30 : (int)(per * unit);
+  p.chunk = p.splits == 1 ? 0x7FFFFFFF : (int)(per * unit);
   return p;
 }
 
 template <int D>
 int launch_join(const AttnArgs& a, hipStream_t s) {
-  const int64_t rows = (int64_t)a.max_new * a.q_heads;
-  hipLaunchKernelGGL((ccq_attention_join_kernel<D>), dim3((unsigned)((rows + 3) / 4), (unsigned)a.batch), dim3(256), 0, s, a);
+  const unsigned rows = (unsigned)(a.max_new * a.q_heads), at_once = 256 / (D / 4);
+  if (a.splits <= kFewSplits) hipLaunchKernelGGL((ccq_attention_join_few_kernel<D>), dim3((rows + at_once - 1) / at_once, (unsigned)a.batch), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((ccq_attention_join_kernel<D>), dim3(rows, (unsigned)a.batch), dim3(256), 0, s, a);
   return hipGetLastError() == hipSuccess ? CCQ_OK : CCQ_ERR_HIP;
 }
 
@@ -312,20 +364,19 @@ int launch_attention(const ccq_cache* c, const ccq_batch* b, const ccq_attn* at,
   a.pages = c->pages, a.page_shift = __builtin_ctz((unsigned)c->page_tokens), a.kv_heads = c->kv_heads, a.q_heads = at->q_heads;
   a.group = at->q_heads / c->kv_heads, a.table_width = b->table_width, a.batch = b->batch, a.tokens = b->tokens, a.max_new = b->max_new, a.max_len = b->max_len;
   a.causal = at->causal, a.window = at->window, a.c = at->scale * 1.4426950408889634f;
-  a.chunk = p.chunk, a.splits = p.splits, a.row_tiles = p.row_tiles;
+  a.chunk = p.chunk, a.splits = p.splits, a.row_tiles = p.row_tiles, a.tile_rows = p.tile_rows;
   if (p.splits > 1) {
     a.part_o = static_cast<float*>(workspace);
     a.part_ml = a.part_o + (int64_t)p.splits * b->tokens * at->q_heads * c->head_dim;
   }
   if ((int64_t)a.kv_heads * a.row_tiles * a.splits > 0x7FFFFFFF || b->batch > 65535) return CCQ_ERR_BAD_PARAM;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const int rc = p.waves ? launch_attention_rows(a, c->head_dim, p.waves, stream) : c->head_dim == 64 ? launch_few<64>(a, p, s) : launch_few<128>(a, p, s);
+  const int rc = p.many ? launch_attention_rows(a, c->head_dim, stream) : c->head_dim == 64 ? launch_few<64>(a, p, s) : launch_few<128>(a, p, s);
   if (rc != CCQ_OK || p.splits == 1) return rc;
   return c->head_dim == 64 ? launch_join<64>(a, s) : launch_join<128>(a, s);
 }
 
-// For tests, no part of the interface: all calls from now on take the kernel for many rows with 4 or 8 wavefronts, or (0) the one for few, or (-1)
-// what the rule says.
-extern "C" void ccq_attention_force(int32_t waves) { forced_waves = waves; }
+// For tests, no part of the interface: all calls from now on take the kernel for many rows (1), the one for few (0), or (-1) what the rule says.
+extern "C" void ccq_attention_force(int32_t kernel) { forced = kernel; }
 
 }  // namespace ccq

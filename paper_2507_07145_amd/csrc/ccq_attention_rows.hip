@@ -1,6 +1,6 @@
 // Attention over the paged 8-bit cache for many rows: chunks of prompts.
 //
-// A wavefront holds 32 rows, a workgroup W of them; the workgroup walks the cached tokens that its rows see in tiles of 64.  Keys and values of
+// A wavefront holds 32 rows, a workgroup eight of them; the workgroup walks the cached tokens that its rows see in tiles of 64.  Keys and values of
 // the next tile are converted on their way to LDS (keys to bf16 with their scale, values to fp16), once for all rows:
 //   scores^T = K q^T   MFMA 32x32x16 bf16, cached tokens as rows
 //   out^T    = V^T p^T MFMA 32x32x16 f16, dimensions as rows
@@ -17,28 +17,24 @@ namespace {
 
 constexpr int kTile = 64;
 
-template <int D, int W>
-__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2, 2))) void ccq_attention_rows_kernel(AttnArgs a) {
+template <int D>
+__global__ __launch_bounds__(2 * kManyRows) __attribute__((amdgpu_waves_per_eu(2, 2))) void ccq_attention_rows_kernel(AttnArgs a) {
   constexpr int DT = D / 32, STEPS = D / 16;
   constexpr int kKeyRow = 2 * D, kKeys = kTile * kKeyRow, kValues = D * kTile * 2, kStage = kKeys + kValues;
-  constexpr int kPieces = kTile * D / 16 / (64 * W) > 0 ? kTile * D / 16 / (64 * W) : 1;   // 16-byte pieces of keys, and of values, to a thread
-  constexpr int kThreads = kTile * D / 16 / kPieces;                                       // threads that have any
+  constexpr int kPieces = kTile * D / 16;   // 16-byte pieces of a tile's keys, and of its values: at most one to a thread
+  static_assert(kPieces <= 2 * kManyRows, "a piece to a thread");
   __shared__ __align__(256) uint8_t lds[2 * kStage];
   __shared__ float exponents[2][4], inverses[2][4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, h = lane >> 5;
   const int head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, tile = a.row_tiles - 1 - rest % a.row_tiles, split = rest / a.row_tiles, b = blockIdx.y;
   const AttnSequence s = attn_sequence(a, b);
-  const int rows = s.n * a.group, row0 = tile * (32 * W);
+  const int rows = s.n * a.group, row0 = tile * kManyRows;
   if (row0 >= rows) return;
-  const int begin = s.begin + split * a.chunk, end = begin + min(a.chunk, s.len - begin);
-  if (split > 0 && begin >= s.len) return;   // (the first one answers for rows that see nothing)
-  // what the workgroup's rows see, and what the wavefront's do
-  const int last_row = min(row0 + 32 * W, rows) - 1;
-  const int any_lo = first_seen(a, s.old + row0 / a.group), any_hi = seen_end(a, s, s.old + last_row / a.group);
-  const int from = max(begin, any_lo & ~(kTile - 1)), to = min(end, any_hi);
-  const int w_first = min(row0 + wave * 32, last_row), w_last = min(row0 + wave * 32 + 31, last_row);
-  const int all_lo = first_seen(a, s.old + w_last / a.group), all_hi = seen_end(a, s, s.old + w_first / a.group);
-  const int wave_lo = first_seen(a, s.old + w_first / a.group), wave_hi = min(to, seen_end(a, s, s.old + w_last / a.group));
+  const AttnTile w = attn_tile(a, s, row0, kManyRows);   // of the workgroup
+  if (split >= w.splits(a)) return;
+  const int from = w.begin + split * a.chunk, to = from + min(a.chunk, w.any_hi - from);
+  const AttnTile own = attn_tile(a, s, min(row0 + wave * 32, w.last_row), 32);   // of the wavefront
+  const int all_lo = own.all_lo, all_hi = own.all_hi, any_lo = w.any_lo, wave_lo = own.any_lo, wave_hi = min(to, own.any_hi), last_row = w.last_row;
 
   const int row = min(row0 + wave * 32 + l32, last_row), token = row / a.group, q_head = head * a.group + row % a.group;
   const int lo = first_seen(a, s.old + token), hi = min(to, seen_end(a, s, s.old + token));
@@ -53,57 +49,41 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2, 2))) 
   const int32_t* pages = a.table + b * a.ld_table;
   const int in_page = (1 << a.page_shift) - 1;
   constexpr int kTokenPieces = D / 16;
-  auto page_at = [&](int t) {
-    const int p = t < to ? pages[t >> a.page_shift] : -1;
-    return p < a.pages ? p : -1;
+  const int piece = threadIdx.x & (kPieces - 1), key_piece_token = piece / kTokenPieces;
+  const bool stages = (int)threadIdx.x < kPieces;
+  u32x4_t kr, vr;
+  int k_page, v_page, k_byte, v_byte, k_next, v_next;   // of what kr and vr hold; pages of the tile after it
+  auto find_pages = [&](int t0) {   // looked at a tile later: no wait for memory here
+    k_next = pages[min(t0 + key_piece_token, to - 1) >> a.page_shift];
+    v_next = pages[min(t0 + 16 * (piece & 3), to - 1) >> a.page_shift];
   };
-  const bool stages = (int)threadIdx.x < kThreads;
-  u32x4_t kr[kPieces], vr[kPieces];
-  int kp[kPieces], vp[kPieces], kb[kPieces], vb[kPieces];
-  auto find_pages = [&](int t0) {
-#pragma unroll
-    for (int i = 0; i < kPieces; ++i) {
-      const int p = threadIdx.x + i * 64 * W;
-      kp[i] = stages ? page_at(t0 + p / kTokenPieces) : -1;
-      vp[i] = stages ? page_at(t0 + 16 * (p & 3)) : -1;
-    }
-  };
-  int kp_of[kPieces], vp_of[kPieces];   // pages of what kr and vr hold
-  auto load = [&](int t0) {
-#pragma unroll
-    for (int i = 0; i < kPieces; ++i) {
-      const int p = (threadIdx.x + i * 64 * W) & (kTile * D / 16 - 1);
-      const int64_t k_tile = (int64_t)max(kp[i], 0) * a.kv_heads + head, v_tile = (int64_t)max(vp[i], 0) * a.kv_heads + head;
-      kr[i] = *reinterpret_cast<const u32x4_t*>(a.k + ((k_tile << a.page_shift) + ((t0 + p / kTokenPieces) & in_page)) * D + p % kTokenPieces * 16);
-      vr[i] = *reinterpret_cast<const u32x4_t*>(a.v + ((v_tile * D + (p >> 2)) << a.page_shift) + ((t0 + 16 * (p & 3)) & in_page));
-      kb[i] = a.ks[k_tile];
-      vb[i] = a.vs[v_tile];
-      kp_of[i] = kp[i];
-      vp_of[i] = vp[i];
-    }
+  const uint32_t page_bytes = (uint32_t)D << a.page_shift;   // of a head
+  const uint32_t k_inner = piece % kTokenPieces * 16, v_inner = (uint32_t)(piece >> 2) << a.page_shift;
+  auto load = [&](int t0) {   // of pages found before; past the end page 0, never stored
+    k_page = k_next < a.pages ? k_next : -1, v_page = v_next < a.pages ? v_next : -1;
+    const uint32_t k_tile = (uint32_t)max(k_page, 0) * a.kv_heads + head, v_tile = (uint32_t)max(v_page, 0) * a.kv_heads + head;
+    kr = *reinterpret_cast<const u32x4_t*>(a.k + ((uint64_t)k_tile * page_bytes + (((t0 + key_piece_token) & in_page) * D + k_inner)));
+    vr = *reinterpret_cast<const u32x4_t*>(a.v + ((uint64_t)v_tile * page_bytes + (((t0 + 16 * (piece & 3)) & in_page) + v_inner)));
+    k_byte = a.ks[k_tile];
+    v_byte = a.vs[v_tile];
   };
   auto store = [&](int t0, int stage) {   // what kr and vr hold, the tile at t0
-    uint8_t* keys = lds + stage * kStage;
-    uint8_t* values = keys + kKeys;
     if (!stages) return;
-#pragma unroll
-    for (int i = 0; i < kPieces; ++i) {
-      const int p = threadIdx.x + i * 64 * W, t = p / kTokenPieces, c = p % kTokenPieces * 2, d = p >> 2, v = (p & 3) * 2;
-      u32x4_t k = kr[i];
-      if (kp_of[i] < 0) k = u32x4_t{0, 0, 0, 0};
-      const float scale = pow2_of_byte(kb[i]);
-      const int k_swizzle = D == 128 ? t & 15 : (t ^ (t >> 3 & 1)) & 7, v_swizzle = (d ^ (d >> 3 & 1)) & 7;
-      *reinterpret_cast<bf16x8_t*>(keys + t * kKeyRow + ((c ^ k_swizzle) * 16)) = values_bf16(k[0], k[1], scale);
-      *reinterpret_cast<bf16x8_t*>(keys + t * kKeyRow + (((c + 1) ^ k_swizzle) * 16)) = values_bf16(k[2], k[3], scale);
-      const int v0 = t0 + 16 * (p & 3);
-      u32x4_t x = vr[i];
-      if (t0 < any_lo || t0 + kTile > to || vp_of[i] < 0) x = keep_tokens(x, v0, vp_of[i] < 0 ? 0x7FFFFFFF : any_lo, to);
-      *reinterpret_cast<f16x8_t*>(values + d * (2 * kTile) + ((v ^ v_swizzle) * 16)) = values_f16(x[0], x[1]);
-      *reinterpret_cast<f16x8_t*>(values + d * (2 * kTile) + (((v + 1) ^ v_swizzle) * 16)) = values_f16(x[2], x[3]);
-      if (p < 4) {
-        exponents[stage][p] = vp_of[i] < 0 ? -__builtin_inff() : (float)(vb[i] - 127);
-        inverses[stage][p] = vp_of[i] < 0 ? 0.f : inverse_of_byte(vb[i]);
-      }
+    const int t = key_piece_token, c = piece % kTokenPieces * 2, d = piece >> 2, v = (piece & 3) * 2;
+    uint8_t* keys = lds + stage * kStage + t * kKeyRow;
+    uint8_t* values = lds + stage * kStage + kKeys + d * (2 * kTile);
+    u32x4_t k = kr, x = vr;
+    if (__any(k_page < 0)) k = k_page < 0 ? u32x4_t{0, 0, 0, 0} : k;
+    const float scale = pow2_of_byte(k_byte);
+    const int k_swizzle = D == 128 ? t & 15 : (t ^ (t >> 3 & 1)) & 7, v_swizzle = (d ^ (d >> 3 & 1)) & 7;
+    *reinterpret_cast<bf16x8_t*>(keys + ((c ^ k_swizzle) * 16)) = values_bf16(k[0], k[1], scale);
+    *reinterpret_cast<bf16x8_t*>(keys + (((c + 1) ^ k_swizzle) * 16)) = values_bf16(k[2], k[3], scale);
+    if (t0 < any_lo || t0 + kTile > to || __any(v_page < 0)) x = keep_tokens(x, t0 + 16 * (piece & 3), v_page < 0 ? 0x7FFFFFFF : any_lo, to);
+    *reinterpret_cast<f16x8_t*>(values + ((v ^ v_swizzle) * 16)) = values_f16(x[0], x[1]);
+    *reinterpret_cast<f16x8_t*>(values + (((v + 1) ^ v_swizzle) * 16)) = values_f16(x[2], x[3]);
+    if (threadIdx.x < 4) {
+      exponents[stage][piece] = v_page < 0 ? -__builtin_inff() : (float)(v_byte - 127);
+      inverses[stage][piece] = v_page < 0 ? 0.f : inverse_of_byte(v_byte);
     }
   };
 
@@ -227,16 +207,11 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2, 2))) 
 
 }  // namespace
 
-int launch_attention_rows(const AttnArgs& a, int head_dim, int waves, void* stream) {
-  const dim3 grid((unsigned)(a.kv_heads * a.row_tiles * a.splits), (unsigned)a.batch);
+int launch_attention_rows(const AttnArgs& a, int head_dim, void* stream) {
+  const dim3 grid((unsigned)(a.kv_heads * a.row_tiles * a.splits), (unsigned)a.batch), block(kManyRows * 2);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (head_dim == 64) {
-    if (waves == 8) hipLaunchKernelGGL((ccq_attention_rows_kernel<64, 8>), grid, dim3(512), 0, s, a);
-    else hipLaunchKernelGGL((ccq_attention_rows_kernel<64, 4>), grid, dim3(256), 0, s, a);
-  } else {
-    if (waves == 8) hipLaunchKernelGGL((ccq_attention_rows_kernel<128, 8>), grid, dim3(512), 0, s, a);
-    else hipLaunchKernelGGL((ccq_attention_rows_kernel<128, 4>), grid, dim3(256), 0, s, a);
-  }
+  if (head_dim == 64) hipLaunchKernelGGL((ccq_attention_rows_kernel<64>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((ccq_attention_rows_kernel<128>), grid, block, 0, s, a);
   return hipGetLastError() == hipSuccess ? CCQ_OK : CCQ_ERR_HIP;
 }
 

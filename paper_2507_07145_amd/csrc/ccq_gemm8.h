@@ -43,9 +43,8 @@ __device__ __forceinline__ void lds_barrier() {
   asm volatile("s_barrier" ::: "memory");
 }
 
-// Blocks of 64 mi rows (mi 1, 2, 4) and 256 columns over columns n_first .. n_first + n_count - 1, K in `shares` (more than one: all columns, fp32
-// partial results in a.partial).
-int launch_gemm8_block(const Gemm8Args& a, int mi, int n_first, int n_count, int shares, void* stream);
+// Blocks of 64 mi rows (mi 1, 2, 4) and 256 columns, K in `shares` (more than one: fp32 partial results in a.partial).
+int launch_gemm8_block(const Gemm8Args& a, int mi, int shares, void* stream);
 
 // Tiles of 16 mt rows (mt 1, 2, 3, 4, 6) and 128 columns.
 int launch_gemm8_stream(const Gemm8Args& a, int mt, int shares, void* stream);

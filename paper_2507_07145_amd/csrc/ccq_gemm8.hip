@@ -68,7 +68,7 @@ Gemm8Args args_of(const ccq_weight8* w, const ccq_rows8* x, int M, void* y, int6
   a.x = static_cast<const uint8_t*>(x->codes), a.xs = x->scales, a.ldx = x->ld, a.ld_xs = x->ld_scales;
   a.y = static_cast<uint16_t*>(y), a.ldy = ldy, a.partial = static_cast<float*>(workspace);
   a.M = M, a.N = w->N, a.K = w->K, a.blocks = (w->K + kScaleBlock - 1) / kScaleBlock;
-  a.ld_partial = (int64_t)(a.N + 3) / 4 * 4;
+  a.ld_partial = ((int64_t)a.N + 3) / 4 * 4;
   return a;
 }
 
@@ -78,21 +78,32 @@ int launch_few(const Gemm8Args& a, hipStream_t s) {
   return hipGetLastError() == hipSuccess ? CCQ_OK : CCQ_ERR_HIP;
 }
 
-// How a call is served: `kind` few rows (mt: 16-row tiles of a workgroup, waves), stream (mt, shares), block (mt: 64-row units, shares; columns
-// from n_rest on, if any are left out, in blocks of mt_rest).
+// How a call is served: `kind` few rows (mt: 16-row tiles of a workgroup, waves), stream (mt, shares), block (mt: 64-row units, shares); a block plan
+// may end at column n_rest, the columns from there on are a product of their own in blocks of mt_rest and shares_rest.
 enum Kind8 { kFew = 0, kStream = 1, kBlock = 2 };
 struct Plan8 {
-  int kind = kFew, mt = 1, shares = 1, waves = 4, n_rest = 0, mt_rest = 0;
+  int kind = kFew, mt = 1, shares = 1, waves = 4, n_rest = 0, mt_rest = 0, shares_rest = 1;
   double time = 1e30;   // estimate, microseconds
 };
+
+int64_t columns_of_partial(int64_t n) { return (n + 3) / 4 * 4; }
+int64_t workspace_of(const Plan8& p, int64_t M, int64_t N) {
+  if (p.n_rest > 0) return p.shares_rest > 1 ? p.shares_rest * M * columns_of_partial(N - p.n_rest) * 4 : 0;
+  return p.shares > 1 ? p.shares * M * columns_of_partial(N) * 4 : 0;
+}
 
 int run(const Gemm8Args& a, const Plan8& p, void* stream) {
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (p.kind == kFew) return p.mt == 4 ? launch_few<4, 4>(a, s) : p.waves == 16 ? launch_few<1, 16>(a, s) : launch_few<1, 4>(a, s);
   if (p.kind == kStream) return launch_gemm8_stream(a, p.mt, p.shares, stream);
-  const int n = p.n_rest > 0 ? p.n_rest : a.N;
-  const int rc = launch_gemm8_block(a, p.mt, 0, n, p.shares, stream);
-  return rc != CCQ_OK || n == a.N ? rc : launch_gemm8_block(a, p.mt_rest, n, a.N - n, 1, stream);
+  if (p.n_rest == 0) return launch_gemm8_block(a, p.mt, p.shares, stream);
+  Gemm8Args left = a, rest = a;
+  left.N = p.n_rest;
+  rest.N = a.N - p.n_rest;   // (n_rest is a multiple of 256: whole blocks of scales, aligned outputs)
+  rest.w += (int64_t)p.n_rest * a.ldw, rest.ws += (int64_t)(p.n_rest / kScaleBlock) * a.ld_ws, rest.y += p.n_rest;
+  rest.ld_partial = columns_of_partial(rest.N);
+  const int rc = launch_gemm8_block(left, p.mt, 1, stream);
+  return rc != CCQ_OK ? rc : launch_gemm8_block(rest, p.mt_rest, p.shares_rest, stream);
 }
 
 // The kernels' times as they were measured on K = 8192, N = 8192 and 28672, M = 1 .. 2048 (and short and narrow products), as lines in the steps of a
@@ -161,13 +172,15 @@ Plan8 find_plan(int M, int N, int K) {
       // whole rounds of the chip in these blocks, the columns that are left in smaller ones
       const int m_tiles = (M + 64 * mi - 1) / (64 * mi), n_tiles = (N + 255) / 256, full = (int)((int64_t)m_tiles * n_tiles / 256) * 256 / m_tiles;
       if (mi > 1 && full > 0 && full < n_tiles) {
-        for (const int rest : {1, 2}) {
-          if (rest >= mi) break;
-          Plan8 p;
-          p.kind = kBlock, p.mt = mi, p.n_rest = full * 256, p.mt_rest = rest;
-          p.time = 6.0 + block_rounds_time(mi, block_groups(mi, M, p.n_rest, 1), blocks, M <= 64 * mi) +
-                   block_rounds_time(rest, block_groups(rest, M, N - p.n_rest, 1), blocks, false);
-          offer(p);
+        for (const int rest : {1, 2, 4}) {
+          for (const int shares : kShares) {
+            if (shares > 8 || (shares > 1 && shares * 4 > blocks)) break;
+            Plan8 p;
+            p.kind = kBlock, p.mt = mi, p.n_rest = full * 256, p.mt_rest = rest, p.shares_rest = shares;
+            p.time = 6.0 + block_rounds_time(mi, block_groups(mi, M, p.n_rest, 1), blocks, M <= 64 * mi) +
+                     block_rounds_time(rest, block_groups(rest, M, N - p.n_rest, shares), std::ceil((double)blocks / shares), false) + add_time(shares, M, N - p.n_rest);
+            offer(p);
+          }
         }
       }
     }
@@ -195,27 +208,27 @@ Plan8 plan_of(int M, int N, int K) {
 int64_t gemm8_workspace(const ccq_weight8* w, int M) {
   if (M <= 0) return 0;
   const Plan8 p = plan_of(M, w->N, w->K);
-  return p.shares > 1 ? (int64_t)p.shares * M * (((int64_t)w->N + 3) / 4 * 4) * 4 : 0;
+  return workspace_of(p, M, w->N);
 }
 
 int launch_gemm8(const ccq_weight8* w, const ccq_rows8* x, int M, void* y, int64_t ldy, void* workspace, void* stream) {
   const Gemm8Args a = args_of(w, x, M, y, ldy, workspace);
   Plan8 p = plan_of(M, a.N, a.K);
-  if (a.ldw > (1 << 23) || a.ldx > (1 << 23)) p = Plan8{kFew, 4, 1, 4, 0, 0, 0.0};   // too far apart for 32-bit offsets within the block kernel's 256 rows
+  if (a.ldw > (1 << 23) || a.ldx > (1 << 23)) p = Plan8{kFew, 4, 1, 4, 0, 0, 1, 0.0};   // too far apart for 32-bit offsets within the block kernel's 256 rows
   return run(a, p, stream);
 }
 
-// For tests, no part of the interface: how a call of these sizes is served (six numbers of the plan, and the estimate), and a call as a named plan, whose
+// For tests, no part of the interface: how a call of these sizes is served (the numbers of the plan, and the estimate), and a call as a named plan, whose
 // arguments are not checked.
 extern "C" void ccq_gemm8_plan(int32_t M, int32_t N, int32_t K, int32_t* out, double* time) {
   const Plan8 p = plan_of(M, N, K);
-  const int v[6] = {p.kind, p.mt, p.shares, p.waves, p.n_rest, p.mt_rest};
-  for (int i = 0; i < 6; ++i) out[i] = v[i];
+  const int v[7] = {p.kind, p.mt, p.shares, p.waves, p.n_rest, p.mt_rest, p.shares_rest};
+  for (int i = 0; i < 7; ++i) out[i] = v[i];
   *time = p.time;
 }
 extern "C" int ccq_gemm8_as(const ccq_weight8* w, const ccq_rows8* x, int32_t M, void* y, int64_t ldy, void* workspace, const int32_t* plan, void* stream) {
   Plan8 p;
-  p.kind = plan[0], p.mt = plan[1], p.shares = plan[2], p.waves = plan[3], p.n_rest = plan[4], p.mt_rest = plan[5];
+  p.kind = plan[0], p.mt = plan[1], p.shares = plan[2], p.waves = plan[3], p.n_rest = plan[4], p.mt_rest = plan[5], p.shares_rest = plan[6];
   return run(args_of(w, x, M, y, ldy, workspace), p, stream);
 }
 

@@ -21,7 +21,7 @@ constexpr int kScaleSteps = 64, kScalePitch = kScaleSteps + 4;   // steps whose 
 
 struct Gemm8Block {
   Gemm8Args a;
-  int32_t n_first, m_tiles, n_tiles, shares, steps_per_share;
+  int32_t m_tiles, n_tiles, shares, steps_per_share;
 };
 
 __device__ const uint4 kZeros = {0, 0, 0, 0};
@@ -45,7 +45,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   const int share = blockIdx.x / (8 * per), at = blockIdx.x % (8 * per), t = at % 8 * per + at / 8;
   if (t >= tiles) return;
   const int panel = t / (8 * p.n_tiles), in_panel = t - panel * 8 * p.n_tiles, high = min(8, p.m_tiles - 8 * panel);
-  const int m0 = (8 * panel + in_panel % high) * kRows, n0 = p.n_first + in_panel / high * kCols;
+  const int m0 = (8 * panel + in_panel % high) * kRows, n0 = in_panel / high * kCols;
   const int first = share * p.steps_per_share, last = min(first + p.steps_per_share, a.blocks);
 
   // A copy moves eight rows; lane l fills position l % 8 of row l / 8 with the chunk that belongs there.  Uniform bases and 32-bit lane offsets:
@@ -273,12 +273,11 @@ int launch(const Gemm8Block& p, hipStream_t s) {
 
 }  // namespace
 
-int launch_gemm8_block(const Gemm8Args& a, int mi, int n_first, int n_count, int shares, void* stream) {
+int launch_gemm8_block(const Gemm8Args& a, int mi, int shares, void* stream) {
   Gemm8Block p;
   p.a = a;
-  p.n_first = n_first;
   p.m_tiles = (a.M + 64 * mi - 1) / (64 * mi);
-  p.n_tiles = (n_count + kCols - 1) / kCols;
+  p.n_tiles = (a.N + kCols - 1) / kCols;
   p.steps_per_share = (a.blocks + shares - 1) / shares;
   p.shares = (a.blocks + p.steps_per_share - 1) / p.steps_per_share;
   hipStream_t s = static_cast<hipStream_t>(stream);

@@ -16,22 +16,22 @@ def _as(weight, rows, M, N, plan):
     f = layer._load().ccq_gemm8_as
     f.restype, f.argtypes = ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]
     y = torch.full((M, (N + 15) // 8 * 8), 7.0, dtype=torch.bfloat16, device=r.DEV)
-    ws = torch.full((plan[2] * M * ((N + 3) // 4 * 4) * 4 + 64,), 0xFF, dtype=torch.uint8, device=r.DEV)   # NaN
+    ws = torch.full((max(plan[2], plan[6]) * M * ((N + 3) // 4 * 4) * 4 + 64,), 0xFF, dtype=torch.uint8, device=r.DEV)   # NaN
     d = rows.desc()
-    rc = f(ctypes.byref(weight.desc), ctypes.byref(d), M, y.data_ptr(), y.stride(0), ws.data_ptr(), (ctypes.c_int32 * 6)(*plan), torch.cuda.current_stream().cuda_stream)
+    rc = f(ctypes.byref(weight.desc), ctypes.byref(d), M, y.data_ptr(), y.stride(0), ws.data_ptr(), (ctypes.c_int32 * 7)(*plan), torch.cuda.current_stream().cuda_stream)
     assert rc == 0
     assert bool((y[:, N:] == 7).all()) and bool((ws[-64:] == 0xFF).all())
     return y[:, :N]
 
 
 def plan(M, N, K):
-    out, time = (ctypes.c_int32 * 6)(), ctypes.c_double()
+    out, time = (ctypes.c_int32 * 7)(), ctypes.c_double()
     layer._load().ccq_gemm8_plan(M, N, K, out, ctypes.byref(time))
     return list(out)
 
 
-PLANS = ([[FEW, 1, 1, 4, 0, 0], [FEW, 1, 1, 16, 0, 0], [FEW, 4, 1, 4, 0, 0]] + [[STREAM, mt, s, 4, 0, 0] for mt in (1, 2, 3, 4, 6) for s in (1, 2, 5)] +
-         [[BLOCK, mi, s, 4, 0, 0] for mi in (1, 2, 4) for s in (1, 3)] + [[BLOCK, 4, 1, 4, 256, 1], [BLOCK, 4, 1, 4, 256, 2], [BLOCK, 2, 1, 4, 512, 1]])
+PLANS = ([[FEW, 1, 1, 4, 0, 0, 1], [FEW, 1, 1, 16, 0, 0, 1], [FEW, 4, 1, 4, 0, 0, 1]] + [[STREAM, mt, s, 4, 0, 0, 1] for mt in (1, 2, 3, 4, 6) for s in (1, 2, 5)] +
+         [[BLOCK, mi, s, 4, 0, 0, 1] for mi in (1, 2, 4) for s in (1, 3)] + [[BLOCK, 4, 1, 4, 256, 1, 1], [BLOCK, 4, 1, 4, 256, 2, 3], [BLOCK, 2, 1, 4, 512, 4, 2]])
 
 
 @pytest.mark.parametrize("M,N,K", [(1, 16, 16), (5, 130, 384), (37, 601, 1936), (64, 333, 768), (100, 129, 144), (129, 1100, 1552), (257, 513, 1040)])
@@ -45,7 +45,7 @@ def test_shape(M, N, K, p):
     t._check(got, want, lost, K)
 
 
-@pytest.mark.parametrize("p", [[BLOCK, 1, 1, 4, 0, 0], [BLOCK, 2, 1, 4, 0, 0], [BLOCK, 4, 1, 4, 0, 0], [STREAM, 4, 1, 4, 0, 0], [FEW, 1, 1, 16, 0, 0]], ids=str)
+@pytest.mark.parametrize("p", [[BLOCK, 1, 1, 4, 0, 0, 1], [BLOCK, 2, 1, 4, 0, 0, 1], [BLOCK, 4, 1, 4, 0, 0, 1], [STREAM, 4, 1, 4, 0, 0, 1], [FEW, 1, 1, 16, 0, 0, 1]], ids=str)
 def test_long_k(p):
     """More steps than the scales of 64 that lie in LDS at a time, and a ragged last one."""
     M, N, K = 70, 300, 128 * 131 + 48
