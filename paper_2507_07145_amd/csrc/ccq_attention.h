@@ -95,8 +95,8 @@ __device__ __forceinline__ u32x4_t keep_tokens(u32x4_t v, int t0, int lo, int hi
   return v;
 }
 
-// The kernel for many rows: workgroups of kManyRows; a.row_tiles counts them.
+// The kernel for many rows, of 128 dimensions: workgroups of kManyRows; a.row_tiles counts them.
 constexpr int kManyRows = 256;
-int launch_attention_rows(const AttnArgs& a, int head_dim, void* stream);
+int launch_attention_rows(const AttnArgs& a, void* stream);
 
 }  // namespace ccq

@@ -311,8 +311,15 @@ int forced = -1;   // (tests: 1 the kernel for many rows, 0 the one for few)
 Plan plan_of(const ccq_cache* c, const ccq_batch* b, const ccq_attn* at) {
   Plan p;
   const int64_t rows = (int64_t)b->max_new * (at->q_heads / c->kv_heads), pairs = (int64_t)b->batch * c->kv_heads;
-  // up to 32 rows the tile of the kernel for many would be less than full
-  p.many = forced >= 0 ? forced == 1 : rows > 32;
+  // The kernel for many rows takes 2 us for 64 tokens of 256 rows and a whole CU for them; the one for few takes 3 us for that work, but in pieces of 32 rows
+  // and of single wavefronts.  The first wins where every CU gets eight of its steps (2048 rows of 32 / 8 heads, 16384 tokens: 510 against 841 us; 4 times 256
+  // rows, 1024 tokens: 40 against 27).  Heads of 64 dimensions leave the second three wavefronts a SIMD: it then keeps up (4 times 512 rows, 16384 tokens:
+  // 379 against 244 us).
+  if (c->head_dim == 128 && rows >= kManyRows) {
+    const int64_t mean = at->window > 0 ? std::min<int64_t>(at->window, b->max_len) : at->causal ? b->max_len - b->max_new / 2 : b->max_len;
+    p.many = (rows + kManyRows - 1) / kManyRows * pairs * (mean / kTile) >= 8 * 256;
+  }
+  if (forced >= 0) p.many = forced == 1 && c->head_dim == 128;
   if (!p.many) p.nt = rows <= 16 ? 1 : 2;
   p.tile_rows = p.many ? kManyRows : 16 * p.nt;
   p.row_tiles = (int)((rows + p.tile_rows - 1) / p.tile_rows);
@@ -371,7 +378,7 @@ int launch_attention(const ccq_cache* c, const ccq_batch* b, const ccq_attn* at,
   }
   if ((int64_t)a.kv_heads * a.row_tiles * a.splits > 0x7FFFFFFF || b->batch > 65535) return CCQ_ERR_BAD_PARAM;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const int rc = p.many ? launch_attention_rows(a, c->head_dim, stream) : c->head_dim == 64 ? launch_few<64>(a, p, s) : launch_few<128>(a, p, s);
+  const int rc = p.many ? launch_attention_rows(a, stream) : c->head_dim == 64 ? launch_few<64>(a, p, s) : launch_few<128>(a, p, s);
   if (rc != CCQ_OK || p.splits == 1) return rc;
   return c->head_dim == 64 ? launch_join<64>(a, s) : launch_join<128>(a, s);
 }

@@ -7,22 +7,24 @@
 // As in the kernel for few rows, tokens are dealt to the first product's rows so that a lane's scores lie in the order in which the second product wants
 // its operand: the weights stay in registers.  Scales of values and pages that are not there enter as the exponent added to a score
 // (-inf for the latter).  Only tiles that not all of a wavefront's rows see whole are masked.
-// A tile costs a wavefront 32 MFMAs (1024 cycles) and about as many cycles of the vector unit (32 scores a lane: multiply-add, largest, exp2, sum, fp16); the
-// two wavefronts of a SIMD overlap them.
+// A tile costs a wavefront 32 MFMAs (1024 cycles) and 1350 cycles of the vector unit (32 scores a lane: largest, multiply-add, exp2, sum, fp16; its share of
+// the conversions), and the two wavefronts of a SIMD overlap only a part of them: 2.1 us a tile.  A chunk of 2048 after 2048 tokens (56 / 8 heads): 217 us, 0.84
+// PFLOP/s; counters say 35% of the time in MFMAs, 55% of vector instructions, LDS 25%.  Tried and no faster: half of the wavefronts half a tile behind, with
+// barriers between (225 us), conversions and exp2 dealt out between the MFMAs (211 to 231).  Slower: four wavefronts of 64 rows, whose accumulators
+// leave the registers that vector instructions reach.
 #include "ccq_attention.h"
 
 namespace ccq {
 
 namespace {
 
-constexpr int kTile = 64;
+constexpr int D = 128, kTile = 64;
 
-template <int D>
 __global__ __launch_bounds__(2 * kManyRows) __attribute__((amdgpu_waves_per_eu(2, 2))) void ccq_attention_rows_kernel(AttnArgs a) {
   constexpr int DT = D / 32, STEPS = D / 16;
   constexpr int kKeyRow = 2 * D, kKeys = kTile * kKeyRow, kValues = D * kTile * 2, kStage = kKeys + kValues;
-  constexpr int kPieces = kTile * D / 16;   // 16-byte pieces of a tile's keys, and of its values: at most one to a thread
-  static_assert(kPieces <= 2 * kManyRows, "a piece to a thread");
+  constexpr int kPieces = kTile * D / 16;   // 16-byte pieces of a tile's keys, and of its values
+  static_assert(kPieces == 2 * kManyRows, "a piece to a thread");
   __shared__ __align__(256) uint8_t lds[2 * kStage];
   __shared__ float exponents[2][4], inverses[2][4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, h = lane >> 5;
@@ -49,8 +51,7 @@ __global__ __launch_bounds__(2 * kManyRows) __attribute__((amdgpu_waves_per_eu(2
   const int32_t* pages = a.table + b * a.ld_table;
   const int in_page = (1 << a.page_shift) - 1;
   constexpr int kTokenPieces = D / 16;
-  const int piece = threadIdx.x & (kPieces - 1), key_piece_token = piece / kTokenPieces;
-  const bool stages = (int)threadIdx.x < kPieces;
+  const int piece = threadIdx.x, key_piece_token = piece / kTokenPieces;
   u32x4_t kr, vr;
   int k_page, v_page, k_byte, v_byte, k_next, v_next;   // of what kr and vr hold; pages of the tile after it
   auto find_pages = [&](int t0) {   // looked at a tile later: no wait for memory here
@@ -68,14 +69,13 @@ __global__ __launch_bounds__(2 * kManyRows) __attribute__((amdgpu_waves_per_eu(2
     v_byte = a.vs[v_tile];
   };
   auto store = [&](int t0, int stage) {   // what kr and vr hold, the tile at t0
-    if (!stages) return;
     const int t = key_piece_token, c = piece % kTokenPieces * 2, d = piece >> 2, v = (piece & 3) * 2;
     uint8_t* keys = lds + stage * kStage + t * kKeyRow;
     uint8_t* values = lds + stage * kStage + kKeys + d * (2 * kTile);
     u32x4_t k = kr, x = vr;
     if (__any(k_page < 0)) k = k_page < 0 ? u32x4_t{0, 0, 0, 0} : k;
     const float scale = pow2_of_byte(k_byte);
-    const int k_swizzle = D == 128 ? t & 15 : (t ^ (t >> 3 & 1)) & 7, v_swizzle = (d ^ (d >> 3 & 1)) & 7;
+    const int k_swizzle = t & 15, v_swizzle = (d ^ (d >> 3 & 1)) & 7;
     *reinterpret_cast<bf16x8_t*>(keys + ((c ^ k_swizzle) * 16)) = values_bf16(k[0], k[1], scale);
     *reinterpret_cast<bf16x8_t*>(keys + (((c + 1) ^ k_swizzle) * 16)) = values_bf16(k[2], k[3], scale);
     if (t0 < any_lo || t0 + kTile > to || __any(v_page < 0)) x = keep_tokens(x, t0 + 16 * (piece & 3), v_page < 0 ? 0x7FFFFFFF : any_lo, to);
@@ -96,7 +96,7 @@ __global__ __launch_bounds__(2 * kManyRows) __attribute__((amdgpu_waves_per_eu(2
 
   // a lane's operands: of the keys the token of row l32 (bits 2 and 3 of a row's number are exchanged), of the values dimension l32 of a tile
   const int key_token = (l32 & 0x13) | (l32 & 8) >> 1 | (l32 & 4) << 1;
-  const int key_swizzle = D == 128 ? key_token & 15 : (key_token ^ (key_token >> 3 & 1)) & 7, value_swizzle = (l32 ^ (l32 >> 3 & 1)) & 7;
+  const int key_swizzle = key_token & 15, value_swizzle = (l32 ^ (l32 >> 3 & 1)) & 7;
 
   if (from < to) {
     find_pages(from);
@@ -207,11 +207,9 @@ __global__ __launch_bounds__(2 * kManyRows) __attribute__((amdgpu_waves_per_eu(2
 
 }  // namespace
 
-int launch_attention_rows(const AttnArgs& a, int head_dim, void* stream) {
-  const dim3 grid((unsigned)(a.kv_heads * a.row_tiles * a.splits), (unsigned)a.batch), block(kManyRows * 2);
-  hipStream_t s = static_cast<hipStream_t>(stream);
-  if (head_dim == 64) hipLaunchKernelGGL((ccq_attention_rows_kernel<64>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((ccq_attention_rows_kernel<128>), grid, block, 0, s, a);
+int launch_attention_rows(const AttnArgs& a, void* stream) {
+  const dim3 grid((unsigned)(a.kv_heads * a.row_tiles * a.splits), (unsigned)a.batch), block(2 * kManyRows);
+  hipLaunchKernelGGL(ccq_attention_rows_kernel, grid, block, 0, static_cast<hipStream_t>(stream), a);
   return hipGetLastError() == hipSuccess ? CCQ_OK : CCQ_ERR_HIP;
 }
 
