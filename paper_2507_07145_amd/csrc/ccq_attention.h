@@ -26,10 +26,12 @@ struct AttnArgs {
   int64_t ld_table;
   float* part_o;    // [split][token row][q head][D]
   float* part_ml;   // [split][token row][q head][2]
+  uint8_t* images;        // [batch][kv head][image_tiles], for the kernel for many rows
+  float* image_scales;    // the same, eight numbers each
   int32_t pages, page_shift, kv_heads, q_heads, group, table_width, batch, tokens, max_new, max_len;
   int32_t causal, window;
   int32_t chunk, splits;
-  int32_t row_tiles, tile_rows;
+  int32_t row_tiles, tile_rows, image_tiles;
   float c;          // scale * log2(e)
 };
 
@@ -95,8 +97,10 @@ __device__ __forceinline__ u32x4_t keep_tokens(u32x4_t v, int t0, int lo, int hi
   return v;
 }
 
-// The kernel for many rows, of 128 dimensions: workgroups of kManyRows; a.row_tiles counts them.
-constexpr int kManyRows = 256;
+// The kernels for many rows, of 128 dimensions: workgroups of kManyRows; a.row_tiles counts them.  Before it the tiles of 64 cached tokens that a sequence's
+// rows see, from image_begin on, are converted to images of kImageBytes.
+constexpr int kManyRows = 256, kImageBytes = 64 * 128 * 4;
+__device__ __forceinline__ int image_begin(const AttnArgs& a, const AttnSequence& s) { return min(first_seen(a, s.old), max(s.len, 0)) & ~63; }
 int launch_attention_rows(const AttnArgs& a, void* stream);
 
 }  // namespace ccq

@@ -306,18 +306,24 @@ struct Plan {
   bool many = false;   // the kernel for many rows
   int nt = 0;          // the one for few: 16-row tiles of a workgroup
   int tile_rows = 0, row_tiles = 0, chunk = 0, splits = 0;
+  int image_tiles = 0;   // of a sequence
 };
+constexpr int64_t kMostImages = int64_t(4) << 30;   // bytes of workspace; past it the kernel for few rows
+int64_t image_tiles(const ccq_batch* b, const ccq_attn* at) {   // of a sequence
+  return (at->window > 0 ? std::min<int64_t>(b->max_len, (int64_t)at->window + b->max_new) : b->max_len) / kTile + 2;
+}
 int forced = -1;   // (tests: 1 the kernel for many rows, 0 the one for few)
 Plan plan_of(const ccq_cache* c, const ccq_batch* b, const ccq_attn* at) {
   Plan p;
   const int64_t rows = (int64_t)b->max_new * (at->q_heads / c->kv_heads), pairs = (int64_t)b->batch * c->kv_heads;
-  // The kernel for many rows takes 2 us for 64 tokens of 256 rows and a whole CU for them; the one for few takes 3 us for that work, but in pieces of 32 rows
-  // and of single wavefronts.  The first wins where every CU gets eight of its steps (2048 rows of 32 / 8 heads, 16384 tokens: 510 against 841 us; 4 times 256
-  // rows, 1024 tokens: 40 against 27).  Heads of 64 dimensions leave the second three wavefronts a SIMD: it then keeps up (4 times 512 rows, 16384 tokens:
-  // 379 against 244 us).
-  if (c->head_dim == 128 && rows >= kManyRows) {
+  // The kernels for many rows take 0.02 us of the chip for an image, read by every 256 rows, and 1.9 us of a CU for a tile of 256 rows; the one for few takes 3 us
+  // for that, but in pieces of 32 rows and of single wavefronts.  The first win where an image is read six times and every CU gets six tiles (2048 rows of
+  // 32 / 8 heads, 16384 tokens: 465 against 843 us; 16 times 256 rows, 4096 tokens, four readers: 235 against 197; measured over 366 shapes).  Heads of 64 dimensions
+  // leave the kernel for few three wavefronts a SIMD: it then keeps up (4 times 512 rows, 16384 tokens: 244 us against 379).
+  if (c->head_dim == 128) {
     const int64_t mean = at->window > 0 ? std::min<int64_t>(at->window, b->max_len) : at->causal ? b->max_len - b->max_new / 2 : b->max_len;
-    p.many = (rows + kManyRows - 1) / kManyRows * pairs * (mean / kTile) >= 8 * 256;
+    const int64_t tiles = (rows + kManyRows - 1) / kManyRows;
+    p.many = tiles >= 6 && tiles * pairs * (mean / kTile) >= 6 * 256 && image_tiles(b, at) * pairs * kImageBytes <= kMostImages;
   }
   if (forced >= 0) p.many = forced == 1 && c->head_dim == 128;
   if (!p.many) p.nt = rows <= 16 ? 1 : 2;
@@ -332,6 +338,7 @@ Plan plan_of(const ccq_cache* c, const ccq_batch* b, const ccq_attn* at) {
   const int64_t least = (units + kMostSplits - 1) / kMostSplits;
   per = groups >= 4 * at_once || (p.many && groups >= at_once) ? units : std::max(least, std::min<int64_t>(std::min<int64_t>(per, 8), units));
   p.splits = (int)((units + per - 1) / per);
+  if (p.many) p.image_tiles = (int)image_tiles(b, at);
   p.chunk = p.splits == 1 ? 0x7FFFFFFF : (int)(per * unit);
   return p;
 }
@@ -352,12 +359,17 @@ int launch_few(const AttnArgs& a, const Plan& p, hipStream_t s) {
   return hipGetLastError() == hipSuccess ? CCQ_OK : CCQ_ERR_HIP;
 }
 
+// Partial results of the splits.
+int64_t parts_bytes(const Plan& p, const ccq_cache* c, const ccq_batch* b, const ccq_attn* at) {
+  return p.splits > 1 ? ((int64_t)p.splits * b->tokens * at->q_heads * (c->head_dim + 2) * 4 + 255) / 256 * 256 : 0;
+}
+
 }  // namespace
 
 int64_t attention_workspace(const ccq_cache* c, const ccq_batch* b, const ccq_attn* at) {
   if (b->batch == 0 || b->max_new == 0) return 0;
   const Plan p = plan_of(c, b, at);
-  return p.splits > 1 ? (int64_t)p.splits * b->tokens * at->q_heads * (c->head_dim + 2) * 4 : 0;
+  return parts_bytes(p, c, b, at) + (int64_t)p.image_tiles * b->batch * c->kv_heads * (kImageBytes + 32);
 }
 
 int launch_attention(const ccq_cache* c, const ccq_batch* b, const ccq_attn* at, const ccq_heads* q, const ccq_heads* out, void* workspace, void* stream) {
@@ -376,7 +388,12 @@ int launch_attention(const ccq_cache* c, const ccq_batch* b, const ccq_attn* at,
     a.part_o = static_cast<float*>(workspace);
     a.part_ml = a.part_o + (int64_t)p.splits * b->tokens * at->q_heads * c->head_dim;
   }
-  if ((int64_t)a.kv_heads * a.row_tiles * a.splits > 0x7FFFFFFF || b->batch > 65535) return CCQ_ERR_BAD_PARAM;
+  if (p.many) {
+    a.images = static_cast<uint8_t*>(workspace) + parts_bytes(p, c, b, at);
+    a.image_tiles = p.image_tiles;
+    a.image_scales = reinterpret_cast<float*>(a.images + (int64_t)p.image_tiles * b->batch * c->kv_heads * kImageBytes);
+  }
+  if ((int64_t)a.kv_heads * a.image_tiles > 0x7FFFFFFF || (int64_t)a.kv_heads * a.row_tiles * a.splits > 0x7FFFFFFF || b->batch > 65535) return CCQ_ERR_BAD_PARAM;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int rc = p.many ? launch_attention_rows(a, stream) : c->head_dim == 64 ? launch_few<64>(a, p, s) : launch_few<128>(a, p, s);
   if (rc != CCQ_OK || p.splits == 1) return rc;

@@ -1,42 +1,82 @@
 // Attention over the paged 8-bit cache for many rows: chunks of prompts.
 //
-// A wavefront holds 32 rows, a workgroup eight of them; the workgroup walks the cached tokens that its rows see in tiles of 64.  Keys and values of
-// the next tile are converted on their way to LDS (keys to bf16 with their scale, values to fp16), once for all rows:
+// A first kernel converts the cached tokens that rows see, 64 at a time, to images of what the second has in LDS: keys in bf16 with their scale, values in fp16
+// (converted by every workgroup for itself they cost a quarter of its time).  Then a wavefront holds 32 rows, a workgroup eight of them, and walks the images:
 //   scores^T = K q^T   MFMA 32x32x16 bf16, cached tokens as rows
 //   out^T    = V^T p^T MFMA 32x32x16 f16, dimensions as rows
 // As in the kernel for few rows, tokens are dealt to the first product's rows so that a lane's scores lie in the order in which the second product wants
 // its operand: the weights stay in registers.  Scales of values and pages that are not there enter as the exponent added to a score
 // (-inf for the latter).  Only tiles that not all of a wavefront's rows see whole are masked.
-// A tile costs a wavefront 32 MFMAs (1024 cycles) and 1350 cycles of the vector unit (32 scores a lane: largest, multiply-add, exp2, sum, fp16; its share of
-// the conversions), and the two wavefronts of a SIMD overlap only a part of them: 2.1 us a tile.  A chunk of 2048 after 2048 tokens (56 / 8 heads): 217 us, 0.84
-// PFLOP/s; counters say 35% of the time in MFMAs, 55% of vector instructions, LDS 25%.  Tried and no faster: half of the wavefronts half a tile behind, with
-// barriers between (225 us), conversions and exp2 dealt out between the MFMAs (211 to 231).  Slower: four wavefronts of 64 rows, whose accumulators
-// leave the registers that vector instructions reach.
+// A tile costs a wavefront 32 MFMAs (1024 cycles) and 1070 cycles of vector instructions (32 scores a lane: largest, multiply-add, exp2, sum, fp16).  Left to
+// themselves the two wavefronts of a SIMD do the same at the same time; so the second four are half a tile behind: while one multiplies (values of the last
+// tile, keys of this one, operands read eight products ahead) the other has its softmax, a barrier between.  The weights are pinned to their half, or the compiler moves
+// the exp2 behind the barrier.  Images go to LDS by buffer loads: with global ones to LDS under way the compiler waits for all LDS reads at once.
+// A chunk of 2048 after 2048 tokens (56 / 8 heads): 8 us for the images and 173 us, 1.0 PFLOP/s (converting in the kernel itself, no halves: 217); a half takes 1860
+// cycles, the chip is idle for a fifth of the time at the end, as 448 workgroups of unequal length meet 256 CUs.  Slower: four wavefronts of 64 rows, whose
+// accumulators leave the registers that vector instructions reach.
+#include <type_traits>
+
 #include "ccq_attention.h"
 
 namespace ccq {
 
 namespace {
 
-constexpr int D = 128, kTile = 64;
+constexpr int D = 128, kTile = 64, kThreads = 2 * kManyRows, kKeys = kTile * D * 2, kImage = 2 * kKeys;
+static_assert(kImage == kImageBytes, "");
+static_assert(kTile * D / 16 == kThreads, "a thread converts 16 keys' and 16 values' bytes");
 
-__global__ __launch_bounds__(2 * kManyRows) __attribute__((amdgpu_waves_per_eu(2, 2))) void ccq_attention_rows_kernel(AttnArgs a) {
+// A tile's keys in bf16, with their scale, and values in fp16, in the order in which they lie in LDS (rows of a token's dimensions, and of a dimension's
+// tokens; 16-byte pieces of a row exchanged by its number, so that the operand reads of neighbouring rows meet all banks), and four exponents of values and
+// their 2^-e.  Nothing of pages that are not there (the exponent -inf), nothing of values that no row sees.
+__global__ __launch_bounds__(kThreads) void ccq_attention_images_kernel(AttnArgs a) {
+  const int head = blockIdx.x % a.kv_heads, n = blockIdx.x / a.kv_heads, b = blockIdx.y;
+  const AttnSequence s = attn_sequence(a, b);
+  const int t0 = image_begin(a, s) + n * kTile;
+  if (s.n <= 0 || t0 >= s.len) return;
+  const int32_t* pages = a.table + b * a.ld_table;
+  const int in_page = (1 << a.page_shift) - 1, piece = threadIdx.x;
+  // piece p of the keys is 16 dimensions of a token, of the values 16 tokens of a dimension
+  const int t = piece / (D / 16), c = piece % (D / 16), d = piece >> 2, quarter = piece & 3;
+  int k_page = pages[min(t0 + t, s.len - 1) >> a.page_shift], v_page = pages[min(t0 + 16 * quarter, s.len - 1) >> a.page_shift];
+  k_page = k_page < a.pages ? k_page : -1, v_page = v_page < a.pages ? v_page : -1;
+  const int64_t k_tile = (int64_t)max(k_page, 0) * a.kv_heads + head, v_tile = (int64_t)max(v_page, 0) * a.kv_heads + head;
+  u32x4_t k = *reinterpret_cast<const u32x4_t*>(a.k + ((k_tile << a.page_shift) + ((t0 + t) & in_page)) * D + c * 16);
+  u32x4_t v = *reinterpret_cast<const u32x4_t*>(a.v + ((v_tile * D + d) << a.page_shift) + ((t0 + 16 * quarter) & in_page));
+  const float k_scale = pow2_of_byte(a.ks[k_tile]);
+  const int v_byte = a.vs[v_tile];
+  if (k_page < 0) k = u32x4_t{0, 0, 0, 0};
+  v = keep_tokens(v, t0 + 16 * quarter, v_page < 0 ? 0x7FFFFFFF : first_seen(a, s.old), s.len);
+  const int64_t image = ((int64_t)b * a.kv_heads + head) * a.image_tiles + n;
+  uint8_t* keys = a.images + image * kImage + t * (2 * D);
+  uint8_t* values = a.images + image * kImage + kKeys + d * (2 * kTile);
+  const int k_swizzle = t & 15, v_swizzle = (d ^ (d >> 3 & 1)) & 7;
+  *reinterpret_cast<bf16x8_t*>(keys + (((2 * c) ^ k_swizzle) * 16)) = values_bf16(k[0], k[1], k_scale);
+  *reinterpret_cast<bf16x8_t*>(keys + (((2 * c + 1) ^ k_swizzle) * 16)) = values_bf16(k[2], k[3], k_scale);
+  *reinterpret_cast<f16x8_t*>(values + (((2 * quarter) ^ v_swizzle) * 16)) = values_f16(v[0], v[1]);
+  *reinterpret_cast<f16x8_t*>(values + (((2 * quarter + 1) ^ v_swizzle) * 16)) = values_f16(v[2], v[3]);
+  if (piece < 4) {
+    a.image_scales[image * 8 + piece] = v_page < 0 ? -__builtin_inff() : (float)(v_byte - 127);
+    a.image_scales[image * 8 + 4 + piece] = v_page < 0 ? 0.f : inverse_of_byte(v_byte);
+  }
+}
+
+// LDS reads may be under way across it.
+__device__ __forceinline__ void barrier() { asm volatile("s_barrier" ::: "memory"); }
+
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void ccq_attention_rows_kernel(AttnArgs a) {
   constexpr int DT = D / 32, STEPS = D / 16;
-  constexpr int kKeyRow = 2 * D, kKeys = kTile * kKeyRow, kValues = D * kTile * 2, kStage = kKeys + kValues;
-  constexpr int kPieces = kTile * D / 16;   // 16-byte pieces of a tile's keys, and of its values
-  static_assert(kPieces == 2 * kManyRows, "a piece to a thread");
-  __shared__ __align__(256) uint8_t lds[2 * kStage];
-  __shared__ float exponents[2][4], inverses[2][4];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, h = lane >> 5;
+  extern __shared__ __align__(256) uint8_t lds[];   // three images
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, h = lane >> 5;
   const int head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, tile = a.row_tiles - 1 - rest % a.row_tiles, split = rest / a.row_tiles, b = blockIdx.y;
   const AttnSequence s = attn_sequence(a, b);
   const int rows = s.n * a.group, row0 = tile * kManyRows;
   if (row0 >= rows) return;
-  const AttnTile w = attn_tile(a, s, row0, kManyRows);   // of the workgroup
-  if (split >= w.splits(a)) return;
-  const int from = w.begin + split * a.chunk, to = from + min(a.chunk, w.any_hi - from);
-  const AttnTile own = attn_tile(a, s, min(row0 + wave * 32, w.last_row), 32);   // of the wavefront
-  const int all_lo = own.all_lo, all_hi = own.all_hi, any_lo = w.any_lo, wave_lo = own.any_lo, wave_hi = min(to, own.any_hi), last_row = w.last_row;
+  const AttnTile all = attn_tile(a, s, row0, kManyRows);   // of the workgroup
+  if (split >= all.splits(a)) return;
+  const int from = all.begin + split * a.chunk, to = from + min(a.chunk, all.any_hi - from);
+  const AttnTile own = attn_tile(a, s, min(row0 + wave * 32, all.last_row), 32);   // of the wavefront
+  const int all_lo = own.all_lo, all_hi = own.all_hi, last_row = all.last_row;
 
   const int row = min(row0 + wave * 32 + l32, last_row), token = row / a.group, q_head = head * a.group + row % a.group;
   const int lo = first_seen(a, s.old + token), hi = min(to, seen_end(a, s, s.old + token));
@@ -47,44 +87,15 @@ __global__ __launch_bounds__(2 * kManyRows) __attribute__((amdgpu_waves_per_eu(2
     for (int i = 0; i < STEPS; ++i) q[i] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t*>(at + 16 * i));
   }
 
-  // staging: piece p of the keys is 16 dimensions of a token, of the values 16 tokens of a dimension
-  const int32_t* pages = a.table + b * a.ld_table;
-  const int in_page = (1 << a.page_shift) - 1;
-  constexpr int kTokenPieces = D / 16;
-  const int piece = threadIdx.x, key_piece_token = piece / kTokenPieces;
-  u32x4_t kr, vr;
-  int k_page, v_page, k_byte, v_byte, k_next, v_next;   // of what kr and vr hold; pages of the tile after it
-  auto find_pages = [&](int t0) {   // looked at a tile later: no wait for memory here
-    k_next = pages[min(t0 + key_piece_token, to - 1) >> a.page_shift];
-    v_next = pages[min(t0 + 16 * (piece & 3), to - 1) >> a.page_shift];
-  };
-  const uint32_t page_bytes = (uint32_t)D << a.page_shift;   // of a head
-  const uint32_t k_inner = piece % kTokenPieces * 16, v_inner = (uint32_t)(piece >> 2) << a.page_shift;
-  auto load = [&](int t0) {   // of pages found before; past the end page 0, never stored
-    k_page = k_next < a.pages ? k_next : -1, v_page = v_next < a.pages ? v_next : -1;
-    const uint32_t k_tile = (uint32_t)max(k_page, 0) * a.kv_heads + head, v_tile = (uint32_t)max(v_page, 0) * a.kv_heads + head;
-    kr = *reinterpret_cast<const u32x4_t*>(a.k + ((uint64_t)k_tile * page_bytes + (((t0 + key_piece_token) & in_page) * D + k_inner)));
-    vr = *reinterpret_cast<const u32x4_t*>(a.v + ((uint64_t)v_tile * page_bytes + (((t0 + 16 * (piece & 3)) & in_page) + v_inner)));
-    k_byte = a.ks[k_tile];
-    v_byte = a.vs[v_tile];
-  };
-  auto store = [&](int t0, int stage) {   // what kr and vr hold, the tile at t0
-    const int t = key_piece_token, c = piece % kTokenPieces * 2, d = piece >> 2, v = (piece & 3) * 2;
-    uint8_t* keys = lds + stage * kStage + t * kKeyRow;
-    uint8_t* values = lds + stage * kStage + kKeys + d * (2 * kTile);
-    u32x4_t k = kr, x = vr;
-    if (__any(k_page < 0)) k = k_page < 0 ? u32x4_t{0, 0, 0, 0} : k;
-    const float scale = pow2_of_byte(k_byte);
-    const int k_swizzle = t & 15, v_swizzle = (d ^ (d >> 3 & 1)) & 7;
-    *reinterpret_cast<bf16x8_t*>(keys + ((c ^ k_swizzle) * 16)) = values_bf16(k[0], k[1], scale);
-    *reinterpret_cast<bf16x8_t*>(keys + (((c + 1) ^ k_swizzle) * 16)) = values_bf16(k[2], k[3], scale);
-    if (t0 < any_lo || t0 + kTile > to || __any(v_page < 0)) x = keep_tokens(x, t0 + 16 * (piece & 3), v_page < 0 ? 0x7FFFFFFF : any_lo, to);
-    *reinterpret_cast<f16x8_t*>(values + ((v ^ v_swizzle) * 16)) = values_f16(x[0], x[1]);
-    *reinterpret_cast<f16x8_t*>(values + (((v + 1) ^ v_swizzle) * 16)) = values_f16(x[2], x[3]);
-    if (threadIdx.x < 4) {
-      exponents[stage][piece] = v_page < 0 ? -__builtin_inff() : (float)(v_byte - 127);
-      inverses[stage][piece] = v_page < 0 ? 0.f : inverse_of_byte(v_byte);
-    }
+  const int first_tile = (from - image_begin(a, s)) / kTile, tiles = from < to ? (to - from + kTile - 1) / kTile : 0;
+  const int64_t image0 = ((int64_t)b * a.kv_heads + head) * a.image_tiles + first_tile;
+  const uint8_t* images = a.images + image0 * kImage;
+  const auto* scales = reinterpret_cast<const __attribute__((address_space(4))) float*>(reinterpret_cast<uintptr_t>(a.image_scales + image0 * 8));   // (constant memory: scalar loads)
+  auto copy = [&](int n, int slot) {
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(images) + (int64_t)n * kImage, 0, kImage, 4 << 15);   // (data format 32 bits)
+#pragma unroll
+    for (int i = 0; i < kImage / 1024 / 8; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(lds + slot * kImage + i * 8192 + wave * 1024), 16, lane * 16, i * 8192 + wave * 1024, 0, 0);
   };
 
   f32x16_t o[DT];
@@ -98,85 +109,130 @@ __global__ __launch_bounds__(2 * kManyRows) __attribute__((amdgpu_waves_per_eu(2
   const int key_token = (l32 & 0x13) | (l32 & 8) >> 1 | (l32 & 4) << 1;
   const int key_swizzle = key_token & 15, value_swizzle = (l32 ^ (l32 >> 3 & 1)) & 7;
 
-  if (from < to) {
-    find_pages(from);
-    load(from);
-    find_pages(from + kTile);
-    store(from, 0);
-    load(from + kTile);
-    find_pages(from + 2 * kTile);
-    __syncthreads();
-  }
-  int stage = 0;
-  for (int t0 = from; t0 < to; t0 += kTile, stage ^= 1) {
-    if (t0 + kTile < to) {
-      store(t0 + kTile, stage ^ 1);
-      load(t0 + 2 * kTile);   // (past the end: page 0, never stored)
-      find_pages(t0 + 3 * kTile);
-    }
-    const uint8_t* keys = lds + stage * kStage;
-    const uint8_t* values = keys + kKeys;
-    if (t0 + kTile > wave_lo && t0 < wave_hi) {   // else none of the wavefront's rows sees the tile
-      f32x16_t sc[2];
+  f32x16_t sc[2];
+  f16x8_t w[4];
+  // operand p of a step: the values of the tile before (the first kValueOperands), then the keys of the tile
+  constexpr int kValueOperands = 4 * DT, kOperands = kValueOperands + 2 * STEPS, kAhead = 8;
+  u32x4_t operand[kAhead];
+  auto read_operand = [&](int p, int before, int slot) {
+    const uint8_t* at = p < kValueOperands ? lds + before * kImage + kKeys + (p % DT * 32 + l32) * (2 * kTile) + (((2 * (p / DT) + h) ^ value_swizzle) * 16)
+                                           : lds + slot * kImage + ((p & 1) * 32 + key_token) * (2 * D) + (((p - kValueOperands) / 2 * 2 + h) ^ key_swizzle) * 16;
+    operand[p % kAhead] = *reinterpret_cast<const u32x4_t*>(at);
+  };
+  auto read_ahead = [&](int first, int before, int slot) {
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
+    for (int p = 0; p < kAhead; ++p) read_operand(first + p, before, slot);
+  };
+  auto multiply = [&](auto FIRST, auto LAST, int before, int slot) {
+    constexpr int first = decltype(FIRST)::value, last = decltype(LAST)::value;
+    if constexpr (last == kOperands) {
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
         for (int e = 0; e < 16; ++e) sc[tt][e] = 0.f;
+    }
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i) {
-          const bf16x8_t key = *reinterpret_cast<const bf16x8_t*>(keys + (tt * 32 + key_token) * kKeyRow + (((2 * i + h) ^ key_swizzle) * 16));
-          sc[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key, q[i], sc[tt], 0, 0, 0);
-        }
-      }
-      if (t0 < all_lo || t0 + kTile > all_hi || t0 + kTile > to) {
+    for (int p = first; p < last; ++p) {
+      const u32x4_t x = operand[p % kAhead];
+      if (p < kValueOperands) o[p % DT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, x), w[p / DT], o[p % DT], 0, 0, 0);
+      else sc[p & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, x), q[(p - kValueOperands) / 2], sc[p & 1], 0, 0, 0);
+      if (p + kAhead < last) read_operand(p + kAhead, before, slot);
+    }
 #pragma unroll
-        for (int tt = 0; tt < 2; ++tt)
+    for (int p = first; p < last; ++p) {
+      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+      if (p + kAhead < last) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+  };
+  auto softmax = [&](int n) {
+    const int t0 = from + n * kTile;
+    float ev[4], inv[4];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int t = t0 + 32 * tt + 16 * (e >> 3) + 8 * h + (e & 7);
-            if (t < lo || t >= hi) sc[tt][e] = -__builtin_inff();
-          }
-      }
-      float ev[4], top = kLowest;
+    for (int i = 0; i < 4; ++i) ev[i] = scales[n * 8 + i], inv[i] = scales[n * 8 + 4 + i];
+    __builtin_amdgcn_sched_barrier(0);
+    if (t0 < all_lo || t0 + kTile > all_hi || t0 + kTile > to) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        ev[i] = exponents[stage][i];
-        float most = sc[i >> 1][8 * (i & 1)];
+      for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-        for (int e = 1; e < 8; ++e) most = fmaxf(most, sc[i >> 1][8 * (i & 1) + e]);
-        top = fmaxf(top, fmaf(most, a.c, ev[i]));
-      }
-      top = fmaxf(top, xor32(top));
-      if (__any(top > m + kRise)) {
-        const float next = top > m + kRise ? top : m;
-        const float f = __builtin_amdgcn_exp2f(m - next);
-        m = next;
-        l *= f;
-#pragma unroll
-        for (int i = 0; i < DT; ++i) o[i] *= f;
-      }
-      f16x8_t w[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float bias = ev[i] - m;
-        float sum = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float p = __builtin_amdgcn_exp2f(fmaf(sc[i >> 1][8 * (i & 1) + e], a.c, bias));
-          sum += p;
-          w[i][e] = (_Float16)p;
-        }
-        l = fmaf(sum, inverses[stage][i], l);
-      }
-#pragma unroll
-      for (int i = 0; i < DT; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const f16x8_t value = *reinterpret_cast<const f16x8_t*>(values + (i * 32 + l32) * (2 * kTile) + (((2 * j + h) ^ value_swizzle) * 16));
-          o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(value, w[j], o[i], 0, 0, 0);
+        for (int e = 0; e < 16; ++e) {
+          const int t = t0 + 32 * tt + 16 * (e >> 3) + 8 * h + (e & 7);
+          if (t < lo || t >= hi) sc[tt][e] = -__builtin_inff();
         }
     }
-    __syncthreads();
+    float most[4], top = kLowest;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      most[i] = sc[i >> 1][8 * (i & 1)];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) most[i] = fmaxf(most[i], sc[i >> 1][8 * (i & 1) + e]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaf(most[i], a.c, ev[i]));
+    top = fmaxf(top, xor32(top));
+    if (__any(top > m + kRise)) {
+      const float next = top > m + kRise ? top : m;
+      const float f = __builtin_amdgcn_exp2f(m - next);
+      m = next;
+      l *= f;
+#pragma unroll
+      for (int i = 0; i < DT; ++i) o[i] *= f;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float bias = ev[i] - m;
+      float sum;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(sc[i >> 1][8 * (i & 1) + e], a.c, bias));
+        sum = e == 0 ? p : sum + p;
+        w[i][e] = (_Float16)p;
+      }
+      l = fmaf(sum, inv[i], l);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(w[i]));   // the weights are made here, not where they are used
+    asm volatile("" : "+v"(l));
+  };
+  // Time in halves of tiles: the first four wavefronts have the scores of tile n, and the values of n - 1, in 2 n, the others in 2 n + 1.  Where tile n + 1 goes, tile
+  // n - 2 lay, last read in 2 n - 1: all copy it in 2 n and wait for it at the end of 2 n + 1.
+  const std::integral_constant<int, 0> zero;
+  const std::integral_constant<int, kValueOperands> values_end;
+  const std::integral_constant<int, kOperands> end;
+  const int behind = wave >> 2;
+  if (tiles > 0) {
+    copy(0, 0);
+    if (1 < tiles) copy(1, 1);
+    wait_loads<0>();
+    barrier();
+    if (behind) barrier();
+    read_ahead(kValueOperands, 0, 0);
+    multiply(values_end, end, 0, 0);
+    barrier();
+    int slot = 1;   // of tile n
+    for (int n = 1; n < tiles; ++n) {
+      const int before = slot == 0 ? 2 : slot - 1, next = slot == 2 ? 0 : slot + 1;
+      if (behind && n + 1 < tiles) copy(n + 1, next);
+      __builtin_amdgcn_sched_barrier(0);
+      softmax(n - 1);
+      read_ahead(0, before, slot);
+      __builtin_amdgcn_sched_barrier(0);
+      if (!behind) wait_loads<0>();
+      barrier();
+      if (!behind && n + 1 < tiles) copy(n + 1, next);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(zero, end, before, slot);
+      __builtin_amdgcn_sched_barrier(0);
+      if (behind) wait_loads<0>();
+      barrier();
+      slot = next;
+    }
+    softmax(tiles - 1);
+    barrier();
+    const int before = slot == 0 ? 2 : slot - 1;
+    read_ahead(0, before, slot);
+    multiply(zero, values_end, before, slot);
+    if (!behind) barrier();
   }
 
   // register e of a lane: dimension 8 (e / 4) + 4 h + e % 4 of its tile
@@ -208,8 +264,9 @@ __global__ __launch_bounds__(2 * kManyRows) __attribute__((amdgpu_waves_per_eu(2
 }  // namespace
 
 int launch_attention_rows(const AttnArgs& a, void* stream) {
-  const dim3 grid((unsigned)(a.kv_heads * a.row_tiles * a.splits), (unsigned)a.batch), block(2 * kManyRows);
-  hipLaunchKernelGGL(ccq_attention_rows_kernel, grid, block, 0, static_cast<hipStream_t>(stream), a);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipLaunchKernelGGL(ccq_attention_images_kernel, dim3((unsigned)(a.kv_heads * a.image_tiles), (unsigned)a.batch), dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL(ccq_attention_rows_kernel, dim3((unsigned)(a.kv_heads * a.row_tiles * a.splits), (unsigned)a.batch), dim3(kThreads), 3 * kImage, s, a);
   return hipGetLastError() == hipSuccess ? CCQ_OK : CCQ_ERR_HIP;
 }
 

@@ -32,11 +32,6 @@ __device__ __forceinline__ f32x4_t multiply8(i32x8_t w, i32x8_t x, int x_scale) 
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, zero, 0, 0, 0, 0x7F7F7F7F, 0, x_scale);
 }
 
-// At most n of the wavefront's loads (copies to LDS among them) are still under way.
-template <int N>
-__device__ __forceinline__ void wait_loads() {
-  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4 << 14) | 0x0F70);
-}
 // All wavefronts' LDS reads and writes before it are done, their copies from memory not: those are waited for by wait_loads.
 __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)

@@ -72,6 +72,12 @@ __device__ __forceinline__ uint32_t xor32(uint32_t v) {
 __device__ __forceinline__ float xor16(float v) { return __builtin_bit_cast(float, xor16(__builtin_bit_cast(uint32_t, v))); }
 __device__ __forceinline__ float xor32(float v) { return __builtin_bit_cast(float, xor32(__builtin_bit_cast(uint32_t, v))); }
 
+// At most n of the wavefront's loads (copies to LDS among them) are still under way.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4 << 14) | 0x0F70);
+}
+
 int launch_norm(const ccq_norm* n, bool norm, void* stream);
 int launch_rope_table(const ccq_rope_scaling* s, int rows, int dims, float* table, void* stream);
 int launch_cache_append(const ccq_cache* c, const ccq_batch* b, const ccq_rope* rope, const ccq_heads* k, const ccq_heads* v, const ccq_heads* q,
