@@ -265,6 +265,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 
 int launch_attention_rows(const AttnArgs& a, void* stream) {
   hipStream_t s = static_cast<hipStream_t>(stream);
+  if (hipFuncSetAttribute(reinterpret_cast<const void*>(ccq_attention_rows_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 3 * kImage) != hipSuccess) return CCQ_ERR_HIP;
   hipLaunchKernelGGL(ccq_attention_images_kernel, dim3((unsigned)(a.kv_heads * a.image_tiles), (unsigned)a.batch), dim3(kThreads), 0, s, a);
   hipLaunchKernelGGL(ccq_attention_rows_kernel, dim3((unsigned)(a.kv_heads * a.row_tiles * a.splits), (unsigned)a.batch), dim3(kThreads), 3 * kImage, s, a);
   return hipGetLastError() == hipSuccess ? CCQ_OK : CCQ_ERR_HIP;
