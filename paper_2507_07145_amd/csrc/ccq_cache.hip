@@ -3,11 +3,13 @@
 // One launch; a workgroup has one job:
 //   keys    of one page and head: rotate, find the largest magnitude, take the page's scale, write [token][dim];
 //   values  of one page and head: the same without the rotation, written [dim][token] through LDS;
-//   queries of one token row: rotate.
+//   queries of one token row, 16 or 32 heads: rotate.
 // A page's scale depends on nothing but the page's own tokens, so no two workgroups share one.  The values of a page are held
 // in registers between the search for the largest and the writing (eight neighbouring dimensions of a token to a thread).
 // Bound by memory for prompts, by the latency of its dependent loads (lengths, table and positions, values, old scale) for
 // single tokens.
+#include <algorithm>
+
 #include "ccq_layer.h"
 
 namespace ccq {
@@ -26,7 +28,7 @@ struct AppendArgs {
   int32_t rope_rows, dims, interleaved;
   int32_t pages, kv_heads, q_heads, table_width, tokens, max_new, max_len;
   int32_t page_slots;         // pages that the new tokens of a sequence may touch
-  int32_t kv_groups, total;   // workgroups of keys (as many of values); of the launch
+  int32_t kv_groups, query_groups, total;   // workgroups of keys (as many of values); a token row's queries; of the launch
 };
 
 struct Sequence {
@@ -63,6 +65,23 @@ struct Turn {
 };
 __device__ __forceinline__ void load_turn(const AppendArgs& a, const float* row, int d0, Turn& t) {
   const int half = a.dims >> 1;
+  if ((half & 7) == 0 && d0 < a.dims) {   // eight pairs, or four, that lie side by side (one number at a time: 20 us instead of 17 for 2048 rows of 56 + 8 heads of 128)
+    const float* from = row + (a.interleaved ? d0 >> 1 : d0 < half ? d0 : d0 - half);
+    const float sign = d0 < half ? -1.f : 1.f;
+    f32x4_t c[2], s[2];
+    __builtin_memcpy(&c[0], from, 16);
+    __builtin_memcpy(&s[0], from + half, 16);
+    if (!a.interleaved) {
+      __builtin_memcpy(&c[1], from + 4, 16);
+      __builtin_memcpy(&s[1], from + half + 4, 16);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      t.c[i] = a.interleaved ? c[0][i >> 1] : c[i >> 2][i & 3];
+      t.s[i] = a.interleaved ? ((i & 1) ? s[0][i >> 1] : -s[0][i >> 1]) : s[i >> 2][i & 3] * sign;
+    }
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int d = d0 + i;
@@ -78,7 +97,13 @@ __device__ __forceinline__ void load_turn(const AppendArgs& a, const float* row,
   }
 }
 // x: dimensions d0 .. d0 + 7 of the head at `head` (bf16).  Products and sum are each rounded: c a - s b and c b + s a.
-__device__ __forceinline__ void rotate8(const AppendArgs& a, const uint16_t* head, int d0, const Turn& t, float (&x)[8]) {
+// `partner`: what load_partner gave.
+__device__ __forceinline__ u32x4_t load_partner(const AppendArgs& a, const uint16_t* head, int d0) {
+  const int half = a.dims >> 1;
+  if (a.interleaved || (half & 7) || d0 >= a.dims) return u32x4_t{0, 0, 0, 0};
+  return *reinterpret_cast<const u32x4_t*>(head + (d0 < half ? d0 + half : d0 - half));
+}
+__device__ __forceinline__ void rotate8(const AppendArgs& a, const uint16_t* head, int d0, const Turn& t, u32x4_t partner, float (&x)[8]) {
 #pragma clang fp contract(off)
   if (d0 >= a.dims) return;
   float other[8];
@@ -87,7 +112,7 @@ __device__ __forceinline__ void rotate8(const AppendArgs& a, const uint16_t* hea
 #pragma unroll
     for (int i = 0; i < 8; ++i) other[i] = x[i ^ 1];
   } else if ((half & 7) == 0) {
-    unpack8(*reinterpret_cast<const u32x4_t*>(head + (d0 < half ? d0 + half : d0 - half)), other);
+    unpack8(partner, other);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -137,13 +162,7 @@ __device__ __forceinline__ void append_page(const AppendArgs& a, int b, int slot
   const int page_no = max(s.old, 0) / P + slot;
   const int lo = max(max(s.old, 0), page_no * P), hi = min(min(s.old + s.n, a.max_len), (page_no + 1) * P);   // positions of the page's new tokens
   if (lo >= hi || page_no >= a.table_width) return;
-  const int page = a.table[b * a.ld_table + page_no];
-  if (page < 0 || page >= a.pages) return;
-  const int older = lo - page_no * P;   // slots that hold older tokens
-  const int64_t tile = (int64_t)page * a.kv_heads + h;
-  uint8_t* scale_at = (KEYS ? a.ks : a.vs) + tile;
-  const int old_byte = older > 0 ? *scale_at : 0;
-  uint8_t* codes = (KEYS ? a.kc : a.vc) + tile * (P * D);
+  const int page = a.table[b * a.ld_table + page_no];   // (first looked at when the tokens are loaded: one wait for memory, not two)
   const int d0 = (threadIdx.x % kPieces) * 8, t0 = threadIdx.x / kPieces;
   const int row0 = s.first + (lo - s.old);   // token row of position lo
 
@@ -157,17 +176,24 @@ __device__ __forceinline__ void append_page(const AppendArgs& a, int b, int slot
     if (t >= hi - lo) continue;
     const int row = row0 + t;
     const u32x4_t vv = *reinterpret_cast<const u32x4_t*>(a.v + row * a.v_token + h * a.v_head + d0);
+    const uint16_t* head = a.k + row * a.k_token + h * a.k_head;
+    const float* angle = nullptr;
+    u32x4_t kk, partner;
+    Turn turn;
+    if (KEYS) {
+      kk = *reinterpret_cast<const u32x4_t*>(head + d0);
+      angle = angles(a, row, lo + t);
+      if (angle) {
+        partner = load_partner(a, head, d0);
+        load_turn(a, angle, d0, turn);
+      }
+    }
     bool bad = any_bad(vv);   // of the token: its threads stand side by side in a wavefront
     const uint64_t votes = __ballot(bad);
     bad = (votes >> ((threadIdx.x & 63) / kPieces * kPieces) & ((1ull << kPieces) - 1)) != 0;
     if (KEYS) {
-      const uint16_t* head = a.k + row * a.k_token + h * a.k_head;
-      unpack8(*reinterpret_cast<const u32x4_t*>(head + d0), x[j]);
-      if (const float* angle = angles(a, row, lo + t)) {
-        Turn turn;
-        load_turn(a, angle, d0, turn);
-        rotate8(a, head, d0, turn, x[j]);
-      }
+      unpack8(kk, x[j]);
+      if (angle) rotate8(a, head, d0, turn, partner, x[j]);
       if (bad) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[j][i] = __builtin_nanf("");
@@ -185,6 +211,12 @@ __device__ __forceinline__ void append_page(const AppendArgs& a, int b, int slot
       if (finite_bits(m)) top = max(top, m);
     }
   }
+  if (page < 0 || page >= a.pages) return;
+  const int older = lo - page_no * P;   // slots that hold older tokens
+  const int64_t tile = (int64_t)page * a.kv_heads + h;
+  uint8_t* scale_at = (KEYS ? a.ks : a.vs) + tile;
+  const int old_byte = older > 0 ? *scale_at : 0;
+  uint8_t* codes = (KEYS ? a.kc : a.vc) + tile * (P * D);
   int byte = scale_byte(max_of_block(top), 127 - kCacheExp, 127 + kCacheExp);
   if (older > 0 && old_byte > byte) byte = min(old_byte, 254);
   const float inv = inverse_of_byte(min(byte, 253));
@@ -258,30 +290,29 @@ __device__ __forceinline__ void append_page(const AppendArgs& a, int b, int slot
 }
 
 template <int D>
-__device__ __forceinline__ void rotate_queries(const AppendArgs& a, int b, int i) {
+constexpr int kQueryHeads = 256 / (D / 8);   // of a workgroup
+template <int D>
+__device__ __forceinline__ void rotate_queries(const AppendArgs& a, int b, int i, int heads) {
   const Sequence s = sequence_of(a, b);
   if (i >= s.n) return;
-  const int row = s.first + i, d0 = (threadIdx.x % (D / 8)) * 8;
-  Turn turn;
+  const int row = s.first + i, d0 = (threadIdx.x % (D / 8)) * 8, own = threadIdx.x / (D / 8);
+  auto head_at = [&](int h) { return a.q + row * a.q_token + min(h, a.q_heads - 1) * a.q_head; };
+  u32x4_t q = *reinterpret_cast<const u32x4_t*>(head_at(heads * kQueryHeads<D> + own) + d0);
   const float* angle = angles(a, row, s.old + i);
+  Turn turn;
   if (angle) load_turn(a, angle, d0, turn);
-  // (every thread's partner dimensions are read before anything of their head is written: q_out may be q)
-  const int heads_at_once = 256 / (D / 8);
-  for (int h0 = 0; h0 < a.q_heads; h0 += heads_at_once) {
-    const int h = h0 + threadIdx.x / (D / 8);
+  for (int h0 = heads * kQueryHeads<D>; h0 < a.q_heads; h0 += a.query_groups * kQueryHeads<D>) {
+    const int h = h0 + own;
     float x[8];
-    const uint16_t* head = a.q + row * a.q_token + h * a.q_head;
-    if (h < a.q_heads) {
-      unpack8(*reinterpret_cast<const u32x4_t*>(head + d0), x);
-      if (angle) rotate8(a, head, d0, turn, x);
-    }
-    __syncthreads();
-    if (h < a.q_heads) {
-      u32x4_t v;
+    unpack8(q, x);
+    if (angle) rotate8(a, head_at(h), d0, turn, load_partner(a, head_at(h), d0), x);
+    q = *reinterpret_cast<const u32x4_t*>(head_at(h + a.query_groups * kQueryHeads<D>) + d0);   // the next heads'
+    __syncthreads();   // every thread's partner dimensions are read before anything of their head is written: q_out may be q
+    if (h >= a.q_heads) continue;
+    u32x4_t v;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = pack_bf16(x[2 * e], x[2 * e + 1]);
-      *reinterpret_cast<u32x4_t*>(a.q_out + row * a.o_token + h * a.o_head + d0) = v;
-    }
+    for (int e = 0; e < 4; ++e) v[e] = pack_bf16(x[2 * e], x[2 * e + 1]);
+    *reinterpret_cast<u32x4_t*>(a.q_out + row * a.o_token + h * a.o_head + d0) = v;
   }
 }
 
@@ -297,7 +328,8 @@ __global__ __launch_bounds__(256) void ccq_append_kernel(AppendArgs a) {
     else append_page<D, P, false>(a, r / a.page_slots, r % a.page_slots, h, lds);
   } else {
     g -= 2 * a.kv_groups;
-    rotate_queries<D>(a, g / a.max_new, g % a.max_new);
+    const int heads = g % a.query_groups, r = g / a.query_groups;
+    rotate_queries<D>(a, r / a.max_new, r % a.max_new, heads);
   }
 }
 
@@ -379,7 +411,11 @@ int launch_cache_append(const ccq_cache* c, const ccq_batch* b, const ccq_rope* 
   const int P = c->page_tokens;
   a.page_slots = (int)(((int64_t)b->max_new + P - 2) / P + 1);
   const int64_t groups = k ? (int64_t)b->batch * a.page_slots * c->kv_heads : 0;
-  const int64_t total = 2 * groups + (q ? (int64_t)b->batch * b->max_new : 0);
+  // few token rows: a workgroup to every 16 heads (64 rows of 64 heads: 6.3 us, with a workgroup to a row 7.7); many: one to a row (2048 rows of 56: 16.6 us against 22.6)
+  const int64_t rows = (int64_t)b->batch * b->max_new, heads_at_once = c->head_dim == 64 ? kQueryHeads<64> : kQueryHeads<128>;
+  const int64_t head_groups = (q_heads + heads_at_once - 1) / heads_at_once;
+  a.query_groups = rows * head_groups <= 1024 ? (int)std::max<int64_t>(head_groups, 1) : 1;
+  const int64_t total = 2 * groups + (q ? (int64_t)b->batch * b->max_new * a.query_groups : 0);
   if (total > 0x7FFFFFFF) return CCQ_ERR_BAD_PARAM;
   if (total == 0) return CCQ_OK;
   a.kv_groups = (int)groups, a.total = (int)total;

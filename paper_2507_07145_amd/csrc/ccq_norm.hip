@@ -203,7 +203,7 @@ void launch(const NormArgs& a, bool norm, hipStream_t s) {
   constexpr int kRows = T < 256 ? 256 / T : 1;
   const dim3 grid((unsigned)((a.M + kRows - 1) / kRows)), block(T < 256 ? 256 : T);
   if (norm) hipLaunchKernelGGL((ccq_norm_kernel<T, C, true>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((ccq_norm_kernel<T, C, false>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((ccq_norm_kernel<T, (T * C > 2048 ? 0 : C), false>), grid, block, 0, s, a);   // (long rows: their pieces do not need each other, and with four held at once the compiler spills)
 }
 
 }  // namespace
