@@ -22,7 +22,7 @@ namespace ccq {
 
 namespace {
 
-constexpr int D = 128, kTile = 64, kThreads = 2 * kManyRows, kKeys = kTile * D * 2, kImage = 2 * kKeys;
+constexpr int D = 128, kTile = 64, kThreads = 2 * kManyRows, kKeys = kTile * D * 2, kImage = 2 * kKeys, kLds = 3 * (kImage + 256);
 static_assert(kImage == kImageBytes, "");
 static_assert(kTile * D / 16 == kThreads, "a thread converts 16 keys' and 16 values' bytes");
 
@@ -66,7 +66,7 @@ __device__ __forceinline__ void barrier() { asm volatile("s_barrier" ::: "memory
 
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void ccq_attention_rows_kernel(AttnArgs a) {
   constexpr int DT = D / 32, STEPS = D / 16;
-  extern __shared__ __align__(256) uint8_t lds[];   // three images
+  extern __shared__ __align__(256) uint8_t lds[];   // three images, and 256 bytes for the exponents of each
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, h = lane >> 5;
   const int head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, tile = a.row_tiles - 1 - rest % a.row_tiles, split = rest / a.row_tiles, b = blockIdx.y;
   const AttnSequence s = attn_sequence(a, b);
@@ -90,12 +90,15 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int first_tile = (from - image_begin(a, s)) / kTile, tiles = from < to ? (to - from + kTile - 1) / kTile : 0;
   const int64_t image0 = ((int64_t)b * a.kv_heads + head) * a.image_tiles + first_tile;
   const uint8_t* images = a.images + image0 * kImage;
-  const auto* scales = reinterpret_cast<const __attribute__((address_space(4))) float*>(reinterpret_cast<uintptr_t>(a.image_scales + image0 * 8));   // (constant memory: scalar loads)
   auto copy = [&](int n, int slot) {
     const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(images) + (int64_t)n * kImage, 0, kImage, 4 << 15);   // (data format 32 bits)
 #pragma unroll
     for (int i = 0; i < kImage / 1024 / 8; ++i)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(lds + slot * kImage + i * 8192 + wave * 1024), 16, lane * 16, i * 8192 + wave * 1024, 0, 0);
+    if (wave == 0) {
+      const auto scales = __builtin_amdgcn_make_buffer_rsrc(a.image_scales + (image0 + n) * 8, 0, 32, 4 << 15);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(scales, (__attribute__((address_space(3))) void*)(lds + 3 * kImage + slot * 256), 4, lane * 4, 0, 0, 0);
+    }
   };
 
   f32x16_t o[DT];
@@ -144,11 +147,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       if (p + kAhead < last) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     }
   };
-  auto softmax = [&](int n) {
+  auto softmax = [&](int n, int slot) {
     const int t0 = from + n * kTile;
-    float ev[4], inv[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) ev[i] = scales[n * 8 + i], inv[i] = scales[n * 8 + 4 + i];
+    const f32x4_t ev = *reinterpret_cast<const f32x4_t*>(lds + 3 * kImage + slot * 256), inv = *reinterpret_cast<const f32x4_t*>(lds + 3 * kImage + slot * 256 + 16);
     __builtin_amdgcn_sched_barrier(0);
     if (t0 < all_lo || t0 + kTile > all_hi || t0 + kTile > to) {
 #pragma unroll
@@ -162,9 +163,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     float most[4], top = kLowest;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      most[i] = sc[i >> 1][8 * (i & 1)];
+      most[i] = -__builtin_inff();   // (from here on pairs: three-operand instructions)
 #pragma unroll
-      for (int e = 1; e < 8; ++e) most[i] = fmaxf(most[i], sc[i >> 1][8 * (i & 1) + e]);
+      for (int e = 0; e < 8; e += 2) most[i] = fmaxf(fmaxf(most[i], sc[i >> 1][8 * (i & 1) + e]), sc[i >> 1][8 * (i & 1) + e + 1]);
     }
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -214,7 +215,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       const int before = slot == 0 ? 2 : slot - 1, next = slot == 2 ? 0 : slot + 1;
       if (behind && n + 1 < tiles) copy(n + 1, next);
       __builtin_amdgcn_sched_barrier(0);
-      softmax(n - 1);
+      softmax(n - 1, before);
       read_ahead(0, before, slot);
       __builtin_amdgcn_sched_barrier(0);
       if (!behind) wait_loads<0>();
@@ -227,9 +228,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       barrier();
       slot = next;
     }
-    softmax(tiles - 1);
-    barrier();
     const int before = slot == 0 ? 2 : slot - 1;
+    softmax(tiles - 1, before);
+    barrier();
     read_ahead(0, before, slot);
     multiply(zero, values_end, before, slot);
     if (!behind) barrier();
@@ -265,9 +266,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 
 int launch_attention_rows(const AttnArgs& a, void* stream) {
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (hipFuncSetAttribute(reinterpret_cast<const void*>(ccq_attention_rows_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 3 * kImage) != hipSuccess) return CCQ_ERR_HIP;
+  if (hipFuncSetAttribute(reinterpret_cast<const void*>(ccq_attention_rows_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kLds) != hipSuccess) return CCQ_ERR_HIP;
   hipLaunchKernelGGL(ccq_attention_images_kernel, dim3((unsigned)(a.kv_heads * a.image_tiles), (unsigned)a.batch), dim3(kThreads), 0, s, a);
-  hipLaunchKernelGGL(ccq_attention_rows_kernel, dim3((unsigned)(a.kv_heads * a.row_tiles * a.splits), (unsigned)a.batch), dim3(kThreads), 3 * kImage, s, a);
+  hipLaunchKernelGGL(ccq_attention_rows_kernel, dim3((unsigned)(a.kv_heads * a.row_tiles * a.splits), (unsigned)a.batch), dim3(kThreads), kLds, s, a);
   return hipGetLastError() == hipSuccess ? CCQ_OK : CCQ_ERR_HIP;
 }
 
