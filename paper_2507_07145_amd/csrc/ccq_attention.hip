@@ -333,10 +333,14 @@ Plan plan_of(const ccq_cache* c, const ccq_batch* b, const ccq_attn* at) {
   int64_t range = b->max_len;
   if (at->window > 0) range = std::min<int64_t>(range, (int64_t)at->window + std::min<int64_t>(b->max_new, p.tile_rows / (at->q_heads / c->kv_heads) + 1) + 63);
   const int64_t unit = kWaves * kTile, units = std::max<int64_t>(1, (range + unit - 1) / unit), groups = pairs * p.row_tiles;
-  const int64_t at_once = p.many ? 256 : 3 * 256;   // workgroups that the chip holds
-  int64_t per = (units * groups + at_once - 1) / at_once;
-  const int64_t least = (units + kMostSplits - 1) / kMostSplits;
-  per = groups >= 4 * at_once || (p.many && groups >= at_once) ? units : std::max(least, std::min<int64_t>(std::min<int64_t>(per, 8), units));
+  // Split so far that every place for a workgroup has one (one a CU for many rows, two for few): further, the parts and the second launch cost more than
+  // shorter pieces bring (64 sequences of up to 8192, 8 heads: 131 us whole, 135 in two, 144 in four; 131072 tokens of 8 heads: 55 us in 32 or 64 pieces, 60 in
+  // 86; 16 sequences of up to 2048: 20 us whole, 16.5 in four; for many rows
+  // 240 workgroups: 50 us whole, 74 in two).  Up to 768 tokens the second launch alone costs more (one sequence of 512: 7.5 us against 9.1).
+  const int64_t places = p.many ? 256 : 2 * 256;
+  int64_t splits = groups >= places || units <= 3 ? 1 : std::min((places + (p.many ? 0 : groups - 1)) / groups, units);
+  splits = std::min<int64_t>(splits, kMostSplits);
+  const int64_t per = (units + splits - 1) / splits;
   p.splits = (int)((units + per - 1) / per);
   if (p.many) p.image_tiles = (int)image_tiles(b, at);
   p.chunk = p.splits == 1 ? 0x7FFFFFFF : (int)(per * unit);
