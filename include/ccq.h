@@ -411,7 +411,8 @@ int ccq_cache_append(const ccq_cache *c, const ccq_batch *b, const ccq_rope *rop
  * the row at position p sees: j <= p when causal, j > p - window when window > 0.  A row that sees none is zero.  Scores, softmax and sums in
  * fp32; the softmax weights enter the second product as fp16, the cached values as they are.  `v` of the tokens that are seen holds no NaN
  * (ccq_cache_append writes none); slots that are not written, and pages outside the window, may hold anything.
- *   workspace DEVICE, at least ccq_attention_workspace_bytes(...) bytes (may be NULL if that is 0; -1: invalid arguments). */
+ *   workspace DEVICE, at least ccq_attention_workspace_bytes(...) bytes (may be NULL if that is 0; -1: invalid arguments): partial results where few rows meet
+ *   many tokens; for chunks of prompts, heads of 128, four bytes per cached number that max_len and window admit, 4 GiB at most. */
 typedef struct {
   int32_t q_heads;         /* a multiple of kv_heads                                                     */
   int32_t causal;

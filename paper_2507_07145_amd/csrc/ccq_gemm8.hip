@@ -1,7 +1,9 @@
 // 8-bit product for few rows: weights go from memory to registers once, activations come from the caches.
 //
 // A workgroup owns 16 outputs (of all rows of a tile of 16 MT rows); its wavefronts take the blocks of K in turn and their
-// accumulators are added through LDS at the end, in a fixed order.  Bound by memory: the weights' bytes.
+// accumulators are added through LDS at the end, in a fixed order.  Bound by memory: the weights' bytes.  One row, 8192 x 8192: 13.0 us, 5.2 TB/s.
+// (For 17 to 64 rows its activations cost more than the weights: every 16 columns read them all.  37 rows, 5001 x 7184: 22 to 27 us in all shapes tried, the
+// streaming kernel with its join 15.5.)
 #include <algorithm>
 #include <cmath>
 

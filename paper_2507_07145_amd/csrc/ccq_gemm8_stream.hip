@@ -4,7 +4,8 @@
 // the even and the odd blocks of K of the share.  Two blocks are a step: the activations of a step (16 MT rows, 256 bytes each) are copied to
 // LDS, asked for as far ahead as the weights (mixed with copies that pass by the registers the compiler's waits would be for all loads); every
 // wavefront asks for its 4 KB of weights two or three steps ahead, straight into registers: no
-// other wavefront of the workgroup needs them.  Bound by memory: the weights' bytes.
+// other wavefront of the workgroup needs them.  Bound by memory: the weights' bytes.  64 rows, 28672 x 8192: 57 us, 4.1 TB/s; 37 rows, 5001 x 7184, six
+// shares: 15.5 us, 3.7 of them for the join (40 blocks of columns alone would leave most of the chip idle).
 #include "ccq_gemm8.h"
 
 namespace ccq {
