@@ -38,7 +38,7 @@ template <int MI>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void ccq_gemm8_block_kernel(Gemm8Block p) {
   constexpr int kRows = 64 * MI, kXBytes = kRows * kScaleBlock;
   constexpr int kXCopies = kRows / 8 / 4, kWCopies = kCols / 8 / 4;   // 1 KB copies (eight rows) of a wavefront that copies: four at a time do
-  extern __shared__ __align__(256) uint8_t lds[];   // two steps of activations, two of weights, row scales
+  extern __shared__ __align__(256) uint8_t lds[];   // two steps of activations, two of weights, row scales, the weights' scales
   const Gemm8Args& a = p.a;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, h = lane >> 5;
   const int wm = wave & 1, wn = wave >> 1;
@@ -74,11 +74,14 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     const uint8_t* base = r.base + (int64_t)min(eighth, r.end) * (8 * r.ld) + k;
     uint32_t from = eighth >= r.end ? r.at[2] : (eighth & 1) ? r.at[1] : r.at[0];
     asm volatile("" : "+v"(from));   // (the zero extension stays next to the load)
-    const uint8_t* src = base + from;
     if constexpr (decltype(RAGGED)::value) {   // zeros past K
+      const uint8_t* src = base + from;
       if (k + (((lane & 7) ^ sub ^ (eighth & 1)) * 16) >= a.K) src = reinterpret_cast<const uint8_t*>(&kZeros);
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+    } else {   // (with global loads to LDS under way the compiler waits for all LDS reads at once)
+      const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, -1, 4 << 15);   // (data format 32 bits)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)to, 16, from, 0, 0, 0);
     }
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
   };
   auto x_slot = [&](int s) { return lds + s * kXBytes; };
   auto w_slot = [&](int s) { return lds + 2 * kXBytes + s * kWBytes; };
@@ -107,9 +110,12 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
       }
       *reinterpret_cast<uint32_t*>(scales + row * kScalePitch + c) = v;
     }
+    for (int i = threadIdx.x; i < 2 * kScaleSteps; i += 64 * kWaves)   // of the weights: 128 columns each
+      reinterpret_cast<float*>(scales + kRows * kScalePitch)[i] =
+          a.ws[(int64_t)(min(n0 + i / kScaleSteps * kScaleBlock, a.N - 1) / kScaleBlock) * a.ld_ws + min(step + i % kScaleSteps, a.blocks - 1)];
   };
   const uint8_t* my_scales = scales + (wm * 32 * MI + l32) * kScalePitch;
-  const auto* ws = reinterpret_cast<const __attribute__((address_space(4))) float*>(reinterpret_cast<uintptr_t>(a.ws + (int64_t)(min(n0 + wn * 64, a.N - 1) / kScaleBlock) * a.ld_ws));   // (constant memory: a scalar load)
+  const float* my_ws = reinterpret_cast<const float*>(scales + kRows * kScalePitch) + (wn >> 1) * kScaleSteps;
 
   // operand reads: lane (row l32, half h) takes chunks 4 kk + 2 h and 4 kk + 2 h + 1 for MFMA kk of the block
   uint32_t operand_at = l32 * kScaleBlock + (((2 * h) ^ ((l32 ^ (l32 >> 3 & 1)) & 7)) * 16);   // of kk = 0; the others differ in bits 4 and 6
@@ -140,7 +146,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     for (int kk = 0; kk < 2; ++kk) w[j][kk] = operand(rows, kk);
   };
   // Two MFMAs of a tile, and the result of the two before them goes into its accumulators: the matrix unit has work while the vector unit adds.
-  float s = ws[first], s_next = s, s_before = s;
+  float s = 0.f, s_before = 0.f, s_read = 0.f;   // of this step, the one before, the next (s_read: the same in all lanes, the others in scalar registers)
   f32x16_t before = zeros16();
   auto multiply = [&](int i, int j) {
     f32x16_t r = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w[j][0], x[i & 1][0], zeros16(), 0, 0, 0, 0x7F7F7F7F, 0, xs_now[i]);
@@ -151,17 +157,20 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     for (int e = 0; e < 16; ++e) acc[pi][pj][e] = fmaf(before[e], f, acc[pi][pj][e]);
     before = r;
   };
+  auto uniform = [](float v) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v))); };
   // Step k: its first operands were asked for in step k - 1.  Before its last tile of rows all its operands are in registers: a barrier there
   // frees its place, and shows that step k + 1 is in LDS.
+  // (after the last step of those that are staged: another's, and read again when the next are)
+  auto next_scale = [&](int k, int i) { xs_now[i] = my_scales[i * 32 * kScalePitch + (k + 1 - first) % kScaleSteps]; };
   auto one_step = [&](int k, auto AHEAD, auto RAGGED) {
     const int slot = (k - first) & 1;
     // (which of the three an eighth takes, and where operands lie, is formed in each step, not kept)
     asm volatile("" : "+v"(xr.at[0]), "+v"(xr.at[1]), "+v"(xr.at[2]), "+v"(wr.at[0]), "+v"(wr.at[1]), "+v"(wr.at[2]), "+v"(operand_at));
-    s_next = ws[min(k + 1, last - 1)];
     __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int i = 0; i < MI; ++i) xs_now[i] = my_scales[i * 32 * kScalePitch + (k - first) % kScaleSteps];
     load_w(slot, 1);
+#pragma unroll
+    for (int i = 1; i < MI; ++i) next_scale(k - 1, i);
+    s = uniform(s_read);
 #pragma unroll
     for (int i = 0; i < kLastTile; ++i) {
       load_x(slot, i + 1);
@@ -193,9 +202,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     load_w(slot ^ 1, 0);
     multiply(kLastTile, 1);
     if (kLastTile % 2 == 0) load_x(slot ^ 1, 0);
-    __builtin_amdgcn_sched_barrier(0);
+    next_scale(k, 0);
+    s_read = my_ws[(k + 1 - first) % kScaleSteps];
     s_before = s;
-    s = s_next;
+    __builtin_amdgcn_sched_barrier(0);
   };
 
   if (first + (wave >> 2) < last) {
@@ -212,6 +222,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
       load_x(0, 0);
       load_w(0, 0);
     }
+    next_scale(k - 1, 0);
+    s_read = my_ws[(k - first) % kScaleSteps];
+    if (k == first) s_before = uniform(s_read);
     for (; k < until && k + 3 < last; ++k) one_step(k, yes, no);
     for (; k < until && k + 2 < last; ++k) one_step(k, yes, yes);
     for (; k < until; ++k) one_step(k, no, no);   // (in the last one the operands asked for are of no step: what lies in the place, unused)
@@ -265,7 +278,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
 
 template <int MI>
 int launch(const Gemm8Block& p, hipStream_t s) {
-  constexpr int kLds = 2 * 64 * MI * kScaleBlock + 2 * kWBytes + 64 * MI * kScalePitch;
+  constexpr int kLds = 2 * 64 * MI * kScaleBlock + 2 * kWBytes + 64 * MI * kScalePitch + 2 * kScaleSteps * 4;
   const void* kernel = reinterpret_cast<const void*>(ccq_gemm8_block_kernel<MI>);
   if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds) != hipSuccess) return CCQ_ERR_HIP;
   const int per = (p.m_tiles * p.n_tiles + 7) / 8;
