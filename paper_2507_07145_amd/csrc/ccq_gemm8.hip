@@ -113,7 +113,7 @@ int run(const Gemm8Args& a, const Plan8& p, void* stream) {
 constexpr double kCus = 256.0;
 double rounds_of(double groups) { return std::ceil(groups / kCus); }
 double busy(double groups) { return std::min(1.0, groups / (kCus * rounds_of(groups))); }
-double add_time(double shares, double M, double N) { return shares > 1 ? 2.0 + shares * M * N * 4.0 / 5e6 : 0.0; }
+double add_time(double shares, double M, double N, bool block) { return shares > 1 ? (block ? 4.0 + shares * M * N * 4.0 / 3e6 : 2.0 + shares * M * N * 4.0 / 5e6) : 0.0; }
 double few_time(int mt, int waves, int M, int N, int blocks) {
   const double tiles = (N + 15) / 16, its = (blocks + waves - 1) / waves;
   if (mt == 4) return 4.0 + its * std::ceil(M / 64.0) * (1.2 + 2.3 * std::min(4.0, tiles / 512.0));
@@ -121,13 +121,13 @@ double few_time(int mt, int waves, int M, int N, int blocks) {
 }
 double stream_time(int mt, int shares, int M, int N, int blocks) {
   const double groups = (double)((N + 127) / 128) * shares * ((M + 16 * mt - 1) / (16 * mt)), steps = std::ceil(std::ceil((double)blocks / shares) / 2.0);
-  return 4.0 + rounds_of(groups) * (1.0 + steps * (0.75 + 0.1 * mt + 0.6 * busy(groups))) + add_time(shares, M, N);
+  return 4.0 + rounds_of(groups) * (1.0 + steps * (0.75 + 0.1 * mt + 0.6 * busy(groups))) + add_time(shares, M, N, false);
 }
 // `alone`: one block of rows, whose weights come from memory and not from a neighbour's reading
 double block_rounds_time(int mi, double groups, double steps, bool alone) {
   const double full = busy(groups);
-  const double per = mi == 4 ? 1.75 + 0.55 * full : mi == 2 ? (alone ? 1.1 + 0.6 * full : 0.9 + 0.3 * full) : alone ? 1.0 + 0.45 * full : 0.75 + 0.3 * full;
-  return rounds_of(groups) * ((alone ? 5.0 : 2.0) + steps * per);
+  const double per = mi == 4 ? 1.45 + 0.5 * full : mi == 2 ? (alone ? 0.9 + 0.6 * full : 0.8 + 0.35 * full) : alone ? 1.0 + 0.45 * full : 0.75 + 0.3 * full;
+  return rounds_of(groups) * ((alone ? 5.0 : mi == 4 ? 4.0 : mi == 2 ? 2.5 : 0.5) + steps * per);
 }
 double block_groups(int mi, int M, int n, int shares) { return (double)((M + 64 * mi - 1) / (64 * mi)) * ((n + 255) / 256) * shares; }
 
@@ -168,7 +168,7 @@ Plan8 find_plan(int M, int N, int K) {
         if (shares > 1 && (shares * 4 > blocks || (double)shares * M * N * 4 > 256e6)) break;
         Plan8 p;
         p.kind = kBlock, p.mt = mi, p.shares = shares;
-        p.time = std::max(bytes, 4.0 + block_rounds_time(mi, block_groups(mi, M, N, shares), std::ceil((double)blocks / shares), M <= 64 * mi)) + add_time(shares, M, N);
+        p.time = std::max(bytes, 4.0 + block_rounds_time(mi, block_groups(mi, M, N, shares), std::ceil((double)blocks / shares), M <= 64 * mi)) + add_time(shares, M, N, true);
         offer(p);
       }
       // whole rounds of the chip in these blocks, the columns that are left in smaller ones
@@ -180,7 +180,7 @@ Plan8 find_plan(int M, int N, int K) {
             Plan8 p;
             p.kind = kBlock, p.mt = mi, p.n_rest = full * 256, p.mt_rest = rest, p.shares_rest = shares;
             p.time = 6.0 + block_rounds_time(mi, block_groups(mi, M, p.n_rest, 1), blocks, M <= 64 * mi) +
-                     block_rounds_time(rest, block_groups(rest, M, N - p.n_rest, shares), std::ceil((double)blocks / shares), false) + add_time(shares, M, N - p.n_rest);
+                     block_rounds_time(rest, block_groups(rest, M, N - p.n_rest, shares), std::ceil((double)blocks / shares), false) + add_time(shares, M, N - p.n_rest, true);
             offer(p);
           }
         }

@@ -37,7 +37,6 @@ __device__ __forceinline__ f32x16_t zeros16() {
 template <int MI>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void ccq_gemm8_block_kernel(Gemm8Block p) {
   constexpr int kRows = 64 * MI, kXBytes = kRows * kScaleBlock;
-  constexpr int kXCopies = kRows / 8 / 4, kWCopies = kCols / 8 / 4;   // 1 KB copies (eight rows) of a wavefront that copies: four at a time do
   extern __shared__ __align__(256) uint8_t lds[];   // two steps of activations, two of weights, row scales, the weights' scales
   const Gemm8Args& a = p.a;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, h = lane >> 5;
@@ -85,14 +84,12 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   };
   auto x_slot = [&](int s) { return lds + s * kXBytes; };
   auto w_slot = [&](int s) { return lds + 2 * kXBytes + s * kWBytes; };
-  const int quarter = wave & 3;
-  auto copy_x = [&](int step, int slot, auto RAGGED) {
-#pragma unroll
-    for (int i = 0; i < kXCopies; ++i) copy(xr, quarter * kXCopies + i, step, x_slot(slot) + (quarter * kXCopies + i) * 1024, RAGGED);
-  };
-  auto copy_w = [&](int step, int slot, auto RAGGED) {
-#pragma unroll
-    for (int i = 0; i < kWCopies; ++i) copy(wr, quarter * kWCopies + i, step, w_slot(slot) + (quarter * kWCopies + i) * 1024, RAGGED);
+  // Copy c of a wavefront's kCopies of a step: weights, then activations.
+  constexpr int kCopiers = MI < 4 ? 4 : 8, kMyW = kCols / 8 / kCopiers, kMyX = kRows / 8 / kCopiers, kCopies = kMyW + kMyX;
+  const int copier = wave & (kCopiers - 1);
+  auto copy_one = [&](int c, int step, int slot, auto RAGGED) {
+    if (c < kMyW) copy(wr, copier * kMyW + c, step, w_slot(slot) + (copier * kMyW + c) * 1024, RAGGED);
+    else copy(xr, copier * kMyX + c - kMyW, step, x_slot(slot) + (copier * kMyX + c - kMyW) * 1024, RAGGED);
   };
 
   // scales: of the rows a byte each, 64 steps at a time in LDS (from memory they are a cache line each in every step); of the weights one
@@ -185,21 +182,28 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     wait_loads<0>();
     lds_barrier();
     __builtin_amdgcn_sched_barrier(0);
-    // The copies of a step keep the path to LDS busy for about half of it, and a wavefront that issues them waits for it: one of the two wavefronts
-    // of a SIMD does, in turn, while the other multiplies.
-    if constexpr (decltype(AHEAD)::value) {
+    // A wavefront that issues copies waits for the path to LDS, which they keep busy for half a step.  In the largest blocks all eight copy, some before each of
+    // the last two products, and the others' products go on meanwhile (2048 x 18432 x 7168: 318 us, with one wavefront of a SIMD that copies in turn 340); in
+    // smaller ones the barriers lie too close for that, and in turn is faster (256 x 8192 x 8192 in blocks of 128 rows: 74 us against 84).
+    if constexpr (decltype(AHEAD)::value && MI < 4) {
       if (wave >> 2 == slot) {
-        copy_w(k + 2, slot, RAGGED);
-        copy_x(k + 2, slot, RAGGED);
-      }
 #pragma unroll
-      for (int i = 0; i < kLastTile; ++i) asm volatile("" : "+v"(acc[i][0]), "+v"(acc[i][1]));
+        for (int c = 0; c < kCopies; ++c) copy_one(c, k + 2, slot, RAGGED);
+      }
     }
     __builtin_amdgcn_sched_barrier(0);
+    auto copy_some = [&](int from, int to) {
+      if constexpr (decltype(AHEAD)::value && MI == 4) {
+#pragma unroll
+        for (int c = from; c < to; ++c) copy_one(c, k + 2, slot, RAGGED);
+      }
+    };
     if (kLastTile % 2 == 1) load_x(slot ^ 1, 0);
+    copy_some(0, (kCopies + 1) / 2);
     multiply(kLastTile, 0);
     __builtin_amdgcn_sched_barrier(0);
     load_w(slot ^ 1, 0);
+    copy_some((kCopies + 1) / 2, kCopies);
     multiply(kLastTile, 1);
     if (kLastTile % 2 == 0) load_x(slot ^ 1, 0);
     next_scale(k, 0);
@@ -208,9 +212,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     __builtin_amdgcn_sched_barrier(0);
   };
 
-  if (first + (wave >> 2) < last) {
-    copy_w(first + (wave >> 2), wave >> 2, yes);
-    copy_x(first + (wave >> 2), wave >> 2, yes);
+  for (int step = first; step < min(first + 2, last); ++step) {
+    if (MI < 4 && wave >> 2 != step - first) continue;
+#pragma unroll
+    for (int c = 0; c < kCopies; ++c) copy_one(c, step, step - first, yes);
   }
   int k = first;
   while (k < last) {
