@@ -9,11 +9,12 @@
 // (-inf for the latter).  Only tiles that not all of a wavefront's rows see whole are masked.
 // A tile costs a wavefront 32 MFMAs (1024 cycles) and 1070 cycles of vector instructions (32 scores a lane: largest, multiply-add, exp2, sum, fp16).  Left to
 // themselves the two wavefronts of a SIMD do the same at the same time; so the second four are half a tile behind: while one multiplies (values of the last
-// tile, keys of this one, operands read eight products ahead) the other has its softmax, a barrier between.  The weights are pinned to their half, or the compiler moves
-// the exp2 behind the barrier.  Images go to LDS by buffer loads: with global ones to LDS under way the compiler waits for all LDS reads at once.
-// A chunk of 2048 after 2048 tokens (56 / 8 heads): 8 us for the images and 173 us, 1.0 PFLOP/s (converting in the kernel itself, no halves: 217); a half takes 1860
-// cycles, the chip is idle for a fifth of the time at the end, as 448 workgroups of unequal length meet 256 CUs.  Slower: four wavefronts of 64 rows, whose
-// accumulators leave the registers that vector instructions reach.
+// tile, keys of this one, operands read eight products ahead) the other has its softmax.  One barrier a tile holds them there (two, one a half: 4 % slower).  The
+// weights are pinned to their half, or the compiler moves the exp2 behind the barrier.  Images go to LDS by buffer loads: with global ones to LDS under way the compiler
+// waits for all LDS reads at once.
+// A chunk of 2048 after 2048 tokens (56 / 8 heads): 8 us for the images and 165 us, 1.1 PFLOP/s (converting in the kernel itself, no halves: 217).  Bound by
+// issue and power (zeros for data: 15 % less time), and the chip is idle for a fifth of the time at the end, as 448 workgroups of unequal length meet 256 CUs.
+// Slower: four wavefronts of 64 rows, whose accumulators leave the registers that vector instructions reach.
 #include <type_traits>
 
 #include "ccq_attention.h"
@@ -195,8 +196,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(w[i]));   // the weights are made here, not where they are used
     asm volatile("" : "+v"(l));
   };
-  // Time in halves of tiles: the first four wavefronts have the scores of tile n, and the values of n - 1, in 2 n, the others in 2 n + 1.  Where tile n + 1 goes, tile
-  // n - 2 lay, last read in 2 n - 1: all copy it in 2 n and wait for it at the end of 2 n + 1.
+  // Between two barriers the first four wavefronts multiply and then have the softmax of tile n, the others have the softmax of tile n - 1 and then multiply.  Where
+  // tile n + 1 goes, tile n - 2 lay, last read before the barrier before.
   const std::integral_constant<int, 0> zero;
   const std::integral_constant<int, kValueOperands> values_end;
   const std::integral_constant<int, kOperands> end;
@@ -206,10 +207,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     if (1 < tiles) copy(1, 1);
     wait_loads<0>();
     barrier();
-    if (behind) barrier();
     read_ahead(kValueOperands, 0, 0);
     multiply(values_end, end, 0, 0);
-    barrier();
+    if (behind) barrier();
     int slot = 1;   // of tile n
     for (int n = 1; n < tiles; ++n) {
       const int before = slot == 0 ? 2 : slot - 1, next = slot == 2 ? 0 : slot + 1;
@@ -218,22 +218,27 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       softmax(n - 1, before);
       read_ahead(0, before, slot);
       __builtin_amdgcn_sched_barrier(0);
-      if (!behind) wait_loads<0>();
-      barrier();
-      if (!behind && n + 1 < tiles) copy(n + 1, next);
+      if (!behind) {
+        wait_loads<0>();
+        barrier();
+        if (n + 1 < tiles) copy(n + 1, next);
+      }
       __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(1);
       multiply(zero, end, before, slot);
+      __builtin_amdgcn_s_setprio(0);
       __builtin_amdgcn_sched_barrier(0);
-      if (behind) wait_loads<0>();
-      barrier();
+      if (behind) {
+        wait_loads<0>();
+        barrier();
+      }
       slot = next;
     }
     const int before = slot == 0 ? 2 : slot - 1;
     softmax(tiles - 1, before);
-    barrier();
+    if (!behind) barrier();
     read_ahead(0, before, slot);
     multiply(zero, values_end, before, slot);
-    if (!behind) barrier();
   }
 
   // register e of a lane: dimension 8 (e / 4) + 4 h + e % 4 of its tile
