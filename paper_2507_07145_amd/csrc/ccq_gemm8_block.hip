@@ -7,7 +7,8 @@
 // is filled again, so that a copy has a step's time to arrive.
 // Products are scaled MFMAs 32x32x64, two for a block of K, into a fresh result that one multiply-add per register adds to the
 // accumulators with the weights' scale.  The vector unit does not reach accumulation registers: 512 registers a wavefront would not help.
-// 2048 rows, 16384 x 7168: 262 us, 1.84 PFLOP/s.  Bound by the way into and out of LDS (64 KB in, 192 KB out a step): 190 us without the copies, 231 with copies that
+// 2048 rows, 8192 x 8192 (a block to each CU): 120 us, 2.3 PFLOP/s; 18432 x 7168: 276 us, 1.96.  Bound by the way into and out of LDS (64 KB in, 192 KB out a step) and by
+// power; on 2048 x 16384 x 7168 an earlier form with 262 us took 190 without the copies, 231 with copies that
 // all read one address, no less without waiting for them.
 #include <type_traits>
 

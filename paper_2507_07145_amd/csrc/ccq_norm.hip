@@ -25,23 +25,24 @@ struct NormArgs {
   int32_t M, N;
   float eps, inv_n;
   uint8_t residual_fp32, weight_fp32;
-  // rows and columns lie so that eight values are one or two 16-byte pieces
-  uint8_t x_al, residual_al, sum_al, weight_al, y_al;
 };
 
-// Eight values of a row from column c on; those at N and past it are `past`.
-__device__ __forceinline__ void load8(const void* row, int c, int N, bool fp32, bool aligned, float past, float (&v)[8]) {
-  if (aligned && c + 8 <= N) {
+// Eight values of a row from column c on; those at N and past it are `past`.  One or two 16-byte pieces, which may start at any value: the card's memory
+// accesses need no alignment (4096 rows of 8191, one value at a time: 120 us instead of 60).
+__device__ __forceinline__ void load8(const void* row, int c, int N, bool fp32, float past, float (&v)[8]) {
+  if (c + 8 <= N) {
     if (fp32) {
-      const f32x4_t a = *reinterpret_cast<const f32x4_t*>(static_cast<const float*>(row) + c);
-      const f32x4_t b = *reinterpret_cast<const f32x4_t*>(static_cast<const float*>(row) + c + 4);
+      f32x4_t a, b;
+      __builtin_memcpy(&a, static_cast<const float*>(row) + c, 16);
+      __builtin_memcpy(&b, static_cast<const float*>(row) + c + 4, 16);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         v[i] = a[i];
         v[4 + i] = b[i];
       }
     } else {
-      const u32x4_t a = *reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(row) + c);
+      u32x4_t a;
+      __builtin_memcpy(&a, static_cast<const uint16_t*>(row) + c, 16);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         v[2 * i] = bf16_lo(a[i]);
@@ -57,16 +58,17 @@ __device__ __forceinline__ void load8(const void* row, int c, int N, bool fp32, 
   }
 }
 
-__device__ __forceinline__ void store8(void* row, int c, int N, bool fp32, bool aligned, const float (&v)[8]) {
-  if (aligned && c + 8 <= N) {
+__device__ __forceinline__ void store8(void* row, int c, int N, bool fp32, const float (&v)[8]) {
+  if (c + 8 <= N) {
     if (fp32) {
-      *reinterpret_cast<f32x4_t*>(static_cast<float*>(row) + c) = f32x4_t{v[0], v[1], v[2], v[3]};
-      *reinterpret_cast<f32x4_t*>(static_cast<float*>(row) + c + 4) = f32x4_t{v[4], v[5], v[6], v[7]};
+      const f32x4_t a = {v[0], v[1], v[2], v[3]}, b = {v[4], v[5], v[6], v[7]};
+      __builtin_memcpy(static_cast<float*>(row) + c, &a, 16);
+      __builtin_memcpy(static_cast<float*>(row) + c + 4, &b, 16);
     } else {
       u32x4_t a;
 #pragma unroll
       for (int i = 0; i < 4; ++i) a[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
-      *reinterpret_cast<u32x4_t*>(static_cast<uint16_t*>(row) + c) = a;
+      __builtin_memcpy(static_cast<uint16_t*>(row) + c, &a, 16);
     }
     return;
   }
@@ -119,10 +121,10 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void ccq_norm_kernel(NormArgs a)
   char* y_row = const_cast<char*>(row_of(a.y, a.ldy, m, 2));
 
   auto load_h = [&](int c, float (&h)[8]) {
-    load8(x, c, a.N, false, a.x_al, 0.f, h);
+    load8(x, c, a.N, false, 0.f, h);
     if (NORM && a.residual) {
       float r[8];
-      load8(res, c, a.N, a.residual_fp32, a.residual_al, 0.f, r);
+      load8(res, c, a.N, a.residual_fp32, 0.f, r);
 #pragma unroll
       for (int i = 0; i < 8; ++i) h[i] += r[i];
     }
@@ -130,17 +132,17 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void ccq_norm_kernel(NormArgs a)
   auto finish = [&](int c, const float (&h)[8], float inv) {
     float y[8];
     if (NORM) {
-      if (a.sum && c < a.N) store8(sum, c, a.N, a.residual_fp32, a.sum_al, h);
+      if (a.sum && c < a.N) store8(sum, c, a.N, a.residual_fp32, h);
       float w[8];
       if (a.weight) {
-        load8(a.weight, c, a.N, a.weight_fp32, a.weight_al, 0.f, w);
+        load8(a.weight, c, a.N, a.weight_fp32, 0.f, w);
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[i] = c + i < a.N ? 1.f : 0.f;
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) y[i] = c + i < a.N ? h[i] * inv * w[i] : 0.f;
-      if (a.y && c < a.N) store8(y_row, c, a.N, false, a.y_al, y);
+      if (a.y && c < a.N) store8(y_row, c, a.N, false, y);
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) y[i] = h[i];
@@ -197,8 +199,6 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void ccq_norm_kernel(NormArgs a)
   }
 }
 
-bool rows_aligned(const void* p, int64_t ld, int bytes) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld * bytes % 16 == 0; }
-
 template <int T, int C>
 void launch(const NormArgs& a, bool norm, hipStream_t s) {
   constexpr int kRows = T < 256 ? 256 / T : 1;
@@ -223,11 +223,6 @@ int launch_norm(const ccq_norm* n, bool norm, void* stream) {
   a.M = n->M, a.N = n->N;
   a.eps = n->eps, a.inv_n = (float)(1.0 / n->N);
   a.residual_fp32 = n->residual_type == CCQ_FP32, a.weight_fp32 = n->weight_type == CCQ_FP32;
-  a.x_al = rows_aligned(n->x, n->ldx, 2);
-  a.residual_al = rows_aligned(n->residual, n->ld_residual, a.residual_fp32 ? 4 : 2);
-  a.sum_al = rows_aligned(n->sum, n->ld_sum, a.residual_fp32 ? 4 : 2);
-  a.weight_al = rows_aligned(n->weight, 0, 1);
-  a.y_al = rows_aligned(n->y, n->ldy, 2);
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int N = n->N;
   // few rows leave the chip empty: as many threads to a row as it has pieces of eight columns
