@@ -46,3 +46,57 @@ def test_bounds(kernel):
 def test_more_rows_than_a_tile_in_splits(kernel):
     """Few sequences and long: the cached tokens are cut, rows of several tiles."""
     t._run([(45, 5000)], 64, 128, 1, 2, seed=3)
+
+
+def test_offsets_past_32_bits(kernel):
+    t.test_offsets_past_32_bits()
+
+
+def test_strides_and_another_stream(kernel):
+    t.test_strides_and_the_general_path()
+
+
+def test_a_captured_call(kernel):
+    """Replays give the eager bits, with lengths and queries that change between them."""
+    pairs, P, D, Hkv, Hq = [(40, 700), (3, 90)], 64, 128, 2, 8
+    seq = r.Sequences(pairs, P, 11)
+    cache = r.to_device(r.random_cache(seq, Hkv, D, 12))
+    batch = seq.batch()
+    q = torch.randn(seq.T, Hq, D, generator=r.gen(13)).bfloat16().to(r.DEV)
+    first, second = q.clone(), q.flip(0).contiguous()
+    lens = batch.lens.clone()
+    eager = [layer.attention(cache, batch, first).clone(), layer.attention(cache, batch, second).clone()]
+    batch.lens.copy_(lens - 33)
+    eager.append(layer.attention(cache, batch, second).clone())
+    batch.lens.copy_(lens)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = layer.attention(cache, batch, q)
+    for i in (0, 1, 2, 1, 0):
+        q.copy_(first if i == 0 else second)
+        batch.lens.copy_(lens - 33 if i == 2 else lens)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out.view(torch.int16), eager[i].view(torch.int16))
+        torch.randn(1 << 16, device=r.DEV).sum().item()
+
+
+def _workspace(n, length, Hkv, Hq, D=128, window=0, B=1):
+    import ctypes
+    cache = layer.ccq_cache(64, 64, Hkv, D, None, None, None, None)
+    batch = layer.ccq_batch(B, B * n, n, length, None, None, None, 1 << 20, 1 << 20)
+    return layer._load().ccq_attention_workspace_bytes(ctypes.byref(cache), ctypes.byref(batch), ctypes.byref(layer.ccq_attn(Hq, 1, window, 1.0)))
+
+
+def test_the_rule_reaches_every_kernel():
+    image = 4 * 64 * 128   # bytes of 64 tokens of a head
+    assert _workspace(2048, 4096, 8, 56) >= 64 * 8 * image      # many rows
+    assert _workspace(2048, 4096, 8, 56, D=64) == 0             # heads of 64: the kernel for few, enough of them
+    assert _workspace(1, 200, 8, 32) == 0                       # one launch
+    assert 0 < _workspace(1, 131072, 8, 64) < 64 << 20          # pieces of a long sequence
+    assert _workspace(2048, 1 << 20, 8, 32, B=16) < 4 << 30     # images of all these tokens would be 16 times that
+
+
+def test_a_chunk_as_the_rule_serves_it():
+    t._run([(700, 1100)], 64, 128, 4, 32, seed=21)
+    t._run([(500, 900), (130, 640)], 32, 128, 8, 32, window=300, seed=22)
