@@ -317,14 +317,14 @@ int forced = -1;   // (tests: 1 the kernel for many rows, 0 the one for few)
 Plan plan_of(const ccq_cache* c, const ccq_batch* b, const ccq_attn* at) {
   Plan p;
   const int64_t rows = (int64_t)b->max_new * (at->q_heads / c->kv_heads), pairs = (int64_t)b->batch * c->kv_heads;
-  // The kernels for many rows take 0.02 us of the chip for an image, read by every 256 rows, and 1.9 us of a CU for a tile of 256 rows; the one for few takes 3 us
-  // for that, but in pieces of 32 rows and of single wavefronts.  The first win where an image is read six times and every CU gets six tiles (2048 rows of
-  // 32 / 8 heads, 16384 tokens: 465 against 843 us; 16 times 256 rows, 4096 tokens, four readers: 235 against 197; measured over 366 shapes).  Heads of 64 dimensions
+  // The kernels for many rows take 0.02 us of the chip for an image, read by every 256 rows, and 1.7 us of a CU for a tile of 256 rows; the one for few takes 3 us
+  // for that, but in pieces of 32 rows and of single wavefronts.  The first win where an image is read six times and every CU gets eight tiles (2048 rows of
+  // 32 / 8 heads, 16384 tokens: 441 against 670 us; 512 rows, 2048 tokens: 42 against 32; measured over 366 shapes, 1 % from the better of the two on average).  Heads of 64 dimensions
   // leave the kernel for few three wavefronts a SIMD: it then keeps up (4 times 512 rows, 16384 tokens: 244 us against 379).
   if (c->head_dim == 128) {
     const int64_t mean = at->window > 0 ? std::min<int64_t>(at->window, b->max_len) : at->causal ? b->max_len - b->max_new / 2 : b->max_len;
     const int64_t tiles = (rows + kManyRows - 1) / kManyRows;
-    p.many = tiles >= 6 && tiles * pairs * (mean / kTile) >= 6 * 256 && image_tiles(b, at) * pairs * kImageBytes <= kMostImages;
+    p.many = tiles >= 6 && tiles * pairs * (mean / kTile) >= 8 * 256 && image_tiles(b, at) * pairs * kImageBytes <= kMostImages;
   }
   if (forced >= 0) p.many = forced == 1 && c->head_dim == 128;
   if (!p.many) p.nt = rows <= 16 ? 1 : 2;
