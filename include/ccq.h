@@ -335,6 +335,10 @@ typedef struct {
 int64_t ccq_gemm8_workspace_bytes(const ccq_weight8 *w, int32_t M);
 int ccq_gemm8(const ccq_weight8 *w, const ccq_rows8 *x, int32_t M, void *y, int64_t ldy, void *workspace, int64_t workspace_bytes,
               void *hip_stream);
+/* The same with bf16 rows x DEVICE [M][ldx], ldx >= K: their 8-bit rows are those of ccq_quantize8, made on the way where rows are few. */
+int64_t ccq_gemm8_bf16_workspace_bytes(const ccq_weight8 *w, int32_t M);
+int ccq_gemm8_bf16(const ccq_weight8 *w, const void *x, int64_t ldx, int32_t M, void *y, int64_t ldy, void *workspace, int64_t workspace_bytes,
+                   void *hip_stream);
 
 /* A paged cache.  A page holds page_tokens tokens of one sequence, for every key head:
  *   k DEVICE e4m3 [pages][kv_heads][page_tokens][head_dim],  v DEVICE e4m3 [pages][kv_heads][head_dim][page_tokens]

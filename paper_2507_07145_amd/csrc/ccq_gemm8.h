@@ -21,11 +21,42 @@ struct Gemm8Args {
   float* partial;       // fp32 [shares][M][ld_partial]
   int64_t ldw, ld_ws, ldx, ld_xs, ldy, ld_partial;   // ld_partial: N rounded up to a multiple of 4
   int32_t M, N, K, blocks;   // blocks: of K, the last one possibly shorter
+  const uint16_t* x16;       // bf16 rows in place of x and xs, quantized by the kernels for few rows (null: none)
+  int64_t ldx16;
 };
 
 __device__ __forceinline__ i32x8_t operand8(u32x4_t a, u32x4_t b) {
   return i32x8_t{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
 }
+// 16 bf16 values of a row, on their way to codes; a row may start at any of them.
+struct Wide16 {
+  u32x4_t v[2];
+};
+__device__ __forceinline__ Wide16 load_wide16(const uint16_t* p, bool there) {
+  Wide16 x = {};
+  if (there) __builtin_memcpy(&x, p, 32);
+  return x;
+}
+// The largest magnitude among them, as an fp32 number's bits.
+__device__ __forceinline__ uint32_t magnitude16(const Wide16& x) {
+  typedef __attribute__((ext_vector_type(2))) unsigned short pair;
+  pair most = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) most = __builtin_elementwise_max(most, __builtin_bit_cast(pair, x.v[i >> 2][i & 3] & 0x7FFF7FFFu));
+  return (uint32_t)(most.x > most.y ? most.x : most.y) << 16;
+}
+// Their codes by the largest magnitude of their block: what ccq_quantize8 writes.
+__device__ __forceinline__ u32x4_t codes16(const Wide16& x, uint32_t top) {
+  const float inv = inverse_of_byte(scale_byte(top, kRowsByteLo, kRowsByteHi));
+  u32x4_t q;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t a = x.v[i >> 1][2 * (i & 1)], b = x.v[i >> 1][2 * (i & 1) + 1];
+    q[i] = top >= kInfBits ? 0x7F7F7F7Fu : pack_e4m3(bf16_lo(a) * inv, bf16_hi(a) * inv, bf16_lo(b) * inv, bf16_hi(b) * inv);
+  }
+  return q;
+}
+__device__ __forceinline__ int scale_of(uint32_t top) { return top >= kInfBits ? 255 : scale_byte(top, kRowsByteLo, kRowsByteHi); }
 // A block of K: weights times activations, scaled by the activations' scale byte (the low byte of `x_scale`).
 __device__ __forceinline__ f32x4_t multiply8(i32x8_t w, i32x8_t x, int x_scale) {
   const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};

@@ -13,7 +13,8 @@ namespace ccq {
 
 namespace {
 
-template <int MT, int W>
+// WIDE: bf16 rows, quantized on the way to the product: the lanes of a row hold a block between them.
+template <int MT, int W, bool WIDE>
 __global__ __launch_bounds__(64 * W) void ccq_gemm8_few_kernel(Gemm8Args a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
   const int n0 = blockIdx.x * 16, m0 = blockIdx.y * (16 * MT);
@@ -22,11 +23,16 @@ __global__ __launch_bounds__(64 * W) void ccq_gemm8_few_kernel(Gemm8Args a) {
   const float* ws = a.ws + (int64_t)(n0 / kScaleBlock) * a.ld_ws;
   const uint8_t* x[MT];
   const uint8_t* xs[MT];
+  const uint16_t* x16[MT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
     const int64_t m = min(m0 + 16 * i + r16, a.M - 1);
-    x[i] = a.x + m * a.ldx;
-    xs[i] = a.xs + m * a.ld_xs;
+    if constexpr (WIDE) {
+      x16[i] = a.x16 + m * a.ldx16;
+    } else {
+      x[i] = a.x + m * a.ldx;
+      xs[i] = a.xs + m * a.ld_xs;
+    }
   }
   f32x4_t acc[MT];
 #pragma unroll
@@ -43,7 +49,20 @@ __global__ __launch_bounds__(64 * W) void ccq_gemm8_few_kernel(Gemm8Args a) {
     const float s = ws[kb];
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-      const f32x4_t p = multiply8(wv, operand8(piece(x[i], k), piece(x[i], k + 64)), xs[i][kb]);
+      i32x8_t xv;
+      int scale;
+      if constexpr (WIDE) {
+        const Wide16 lo = load_wide16(x16[i] + k, k < a.K), hi = load_wide16(x16[i] + k + 64, k + 64 < a.K);
+        uint32_t top = max(magnitude16(lo), magnitude16(hi));
+        top = max(top, xor16(top));
+        top = max(top, xor32(top));
+        xv = operand8(codes16(lo, top), codes16(hi, top));
+        scale = scale_of(top);
+      } else {
+        xv = operand8(piece(x[i], k), piece(x[i], k + 64));
+        scale = xs[i][kb];
+      }
+      const f32x4_t p = multiply8(wv, xv, scale);
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[i][e] = fmaf(p[e], s, acc[i][e]);
     }
@@ -65,9 +84,9 @@ __global__ __launch_bounds__(64 * W) void ccq_gemm8_few_kernel(Gemm8Args a) {
 namespace {
 
 Gemm8Args args_of(const ccq_weight8* w, const ccq_rows8* x, int M, void* y, int64_t ldy, void* workspace) {
-  Gemm8Args a;
+  Gemm8Args a = {};
   a.w = static_cast<const uint8_t*>(w->codes), a.ws = w->scales, a.ldw = w->ldw, a.ld_ws = w->ld_scales;
-  a.x = static_cast<const uint8_t*>(x->codes), a.xs = x->scales, a.ldx = x->ld, a.ld_xs = x->ld_scales;
+  if (x) a.x = static_cast<const uint8_t*>(x->codes), a.xs = x->scales, a.ldx = x->ld, a.ld_xs = x->ld_scales;
   a.y = static_cast<uint16_t*>(y), a.ldy = ldy, a.partial = static_cast<float*>(workspace);
   a.M = M, a.N = w->N, a.K = w->K, a.blocks = (w->K + kScaleBlock - 1) / kScaleBlock;
   a.ld_partial = ((int64_t)a.N + 3) / 4 * 4;
@@ -76,7 +95,9 @@ Gemm8Args args_of(const ccq_weight8* w, const ccq_rows8* x, int M, void* y, int6
 
 template <int MT, int W>
 int launch_few(const Gemm8Args& a, hipStream_t s) {
-  hipLaunchKernelGGL((ccq_gemm8_few_kernel<MT, W>), dim3((unsigned)((a.N + 15) / 16), (unsigned)((a.M + 16 * MT - 1) / (16 * MT))), dim3(64 * W), 0, s, a);
+  const dim3 grid((unsigned)((a.N + 15) / 16), (unsigned)((a.M + 16 * MT - 1) / (16 * MT)));
+  if (a.x16) hipLaunchKernelGGL((ccq_gemm8_few_kernel<MT, W, true>), grid, dim3(64 * W), 0, s, a);
+  else hipLaunchKernelGGL((ccq_gemm8_few_kernel<MT, W, false>), grid, dim3(64 * W), 0, s, a);
   return hipGetLastError() == hipSuccess ? CCQ_OK : CCQ_ERR_HIP;
 }
 
@@ -85,7 +106,8 @@ int launch_few(const Gemm8Args& a, hipStream_t s) {
 enum Kind8 { kFew = 0, kStream = 1, kBlock = 2 };
 struct Plan8 {
   int kind = kFew, mt = 1, shares = 1, waves = 4, n_rest = 0, mt_rest = 0, shares_rest = 1;
-  double time = 1e30;   // estimate, microseconds
+  bool quantizes = false;   // bf16 rows become 8-bit rows in the kernel, not by a launch before it
+  double time = 1e30;       // estimate, microseconds
 };
 
 int64_t columns_of_partial(int64_t n) { return (n + 3) / 4 * 4; }
@@ -131,10 +153,23 @@ double block_rounds_time(int mi, double groups, double steps, bool alone) {
 }
 double block_groups(int mi, int M, int n, int shares) { return (double)((M + 64 * mi - 1) / (64 * mi)) * ((n + 255) / 256) * shares; }
 
-Plan8 find_plan(int M, int N, int K) {
+// Whether a kernel for few rows quantizes bf16 rows itself: that saves a launch of 3 us, and every workgroup does it for all rows.  Measured against the
+// launch: few rows, 2048 x 7168, 1 / 4 / 16 rows: 7.6 / 8.4 / 12.8 us against 8.8 / 9.7 / 11.1; 5001 x 7184: alike; 28672 x 8192: 48 - 55 against 43 - 47.  Streaming
+// kernel, 8192 x 8192, 32 / 37 rows: 20.3 / 23.5 against 22.5 / 23.1; 2048 x 7168, 37 rows: 16.3 against 17.5.  1024 x 1024, 1 to 64 rows: 4.2 - 8.2 against 9.
+bool quantizes(const Plan8& p, int M, int N, int K) {
+  const double size = (double)N * K;
+  if (p.kind == kFew) return size <= (M <= 8 ? 40e6 : 4e6);
+  return p.kind == kStream && (p.mt <= 2 || (p.mt <= 4 && size <= 16e6));
+}
+
+// wide: bf16 rows
+Plan8 find_plan(int M, int N, int K, bool wide) {
   const int blocks = (K + kScaleBlock - 1) / kScaleBlock;
+  const double quantizing = wide ? 3.0 + (double)M * K * 3.0 / 4.9e6 : 0.0;
   Plan8 best;
-  auto offer = [&](const Plan8& p) {
+  auto offer = [&](Plan8 p) {
+    p.quantizes = wide && quantizes(p, M, N, K);
+    if (wide && !p.quantizes) p.time += quantizing;
     if (p.time < best.time) best = p;
   };
   auto few = [&](int mt, int waves) {
@@ -191,15 +226,15 @@ Plan8 find_plan(int M, int N, int K) {
 }
 
 // The plans of the sizes that a thread asked for last: finding one takes up to 5 us of host time.
-Plan8 plan_of(int M, int N, int K) {
+Plan8 plan_of(int M, int N, int K, bool wide) {
   struct Known {
     int M = 0, N = 0, K = 0;
     Plan8 plan;
   };
-  static thread_local Known known[64];
-  Known& k = known[((unsigned)M * 31 + (unsigned)N * 7 + (unsigned)K / 16) % 64];
+  static thread_local Known known[2][64];
+  Known& k = known[wide][((unsigned)M * 31 + (unsigned)N * 7 + (unsigned)K / 16) % 64];
   if (k.M != M || k.N != N || k.K != K) {
-    k.plan = find_plan(M, N, K);
+    k.plan = find_plan(M, N, K, wide);
     k.M = M, k.N = N, k.K = K;
   }
   return k.plan;
@@ -209,21 +244,51 @@ Plan8 plan_of(int M, int N, int K) {
 
 int64_t gemm8_workspace(const ccq_weight8* w, int M) {
   if (M <= 0) return 0;
-  const Plan8 p = plan_of(M, w->N, w->K);
-  return workspace_of(p, M, w->N);
+  return workspace_of(plan_of(M, w->N, w->K, false), M, w->N);
+}
+
+namespace {
+
+// Calls whose weights' or activations' rows are too far apart for 32-bit offsets within the block kernel's 256 rows.
+constexpr int64_t kFarRows = 1 << 23;
+const Plan8 kFar = {kFew, 4, 1, 4, 0, 0, 1, true, 0.0};
+
+Plan8 wide_plan(const ccq_weight8* w, int M) { return w->ldw > kFarRows || w->K > kFarRows ? kFar : plan_of(M, w->N, w->K, true); }
+// Workspace of a call with bf16 rows that are quantized first: partial results, codes, scales.
+int64_t codes_at(const Plan8& p, int64_t M, int64_t N) { return (workspace_of(p, M, N) + 255) / 256 * 256; }
+
+}  // namespace
+
+int64_t gemm8_bf16_workspace(const ccq_weight8* w, int M) {
+  if (M <= 0) return 0;
+  const Plan8 p = wide_plan(w, M);
+  return !p.quantizes ? codes_at(p, M, w->N) + (int64_t)M * w->K + (int64_t)M * ((w->K + kScaleBlock - 1) / kScaleBlock) : workspace_of(p, M, w->N);
+}
+
+int launch_gemm8_bf16(const ccq_weight8* w, const void* x, int64_t ldx, int M, void* y, int64_t ldy, void* workspace, void* stream) {
+  const Plan8 p = wide_plan(w, M);
+  if (p.quantizes) {
+    Gemm8Args a = args_of(w, nullptr, M, y, ldy, workspace);
+    a.x16 = static_cast<const uint16_t*>(x), a.ldx16 = ldx;
+    return run(a, p, stream);
+  }
+  ccq_norm n = {};
+  n.M = M, n.N = w->K, n.x = x, n.ldx = ldx;
+  n.y8.codes = static_cast<uint8_t*>(workspace) + codes_at(p, M, w->N), n.y8.ld = w->K;
+  n.y8.scales = static_cast<uint8_t*>(n.y8.codes) + (int64_t)M * w->K, n.y8.ld_scales = (w->K + kScaleBlock - 1) / kScaleBlock;
+  const int rc = launch_norm(&n, false, stream);
+  return rc != CCQ_OK ? rc : run(args_of(w, &n.y8, M, y, ldy, workspace), p, stream);
 }
 
 int launch_gemm8(const ccq_weight8* w, const ccq_rows8* x, int M, void* y, int64_t ldy, void* workspace, void* stream) {
   const Gemm8Args a = args_of(w, x, M, y, ldy, workspace);
-  Plan8 p = plan_of(M, a.N, a.K);
-  if (a.ldw > (1 << 23) || a.ldx > (1 << 23)) p = Plan8{kFew, 4, 1, 4, 0, 0, 1, 0.0};   // too far apart for 32-bit offsets within the block kernel's 256 rows
-  return run(a, p, stream);
+  return run(a, a.ldw > kFarRows || a.ldx > kFarRows ? kFar : plan_of(M, a.N, a.K, false), stream);
 }
 
 // For tests, no part of the interface: how a call of these sizes is served (the numbers of the plan, and the estimate), and a call as a named plan, whose
 // arguments are not checked.
 extern "C" void ccq_gemm8_plan(int32_t M, int32_t N, int32_t K, int32_t* out, double* time) {
-  const Plan8 p = plan_of(M, N, K);
+  const Plan8 p = plan_of(M, N, K, false);
   const int v[7] = {p.kind, p.mt, p.shares, p.waves, p.n_rest, p.mt_rest, p.shares_rest};
   for (int i = 0; i < 7; ++i) out[i] = v[i];
   *time = p.time;
@@ -231,7 +296,9 @@ extern "C" void ccq_gemm8_plan(int32_t M, int32_t N, int32_t K, int32_t* out, do
 extern "C" int ccq_gemm8_as(const ccq_weight8* w, const ccq_rows8* x, int32_t M, void* y, int64_t ldy, void* workspace, const int32_t* plan, void* stream) {
   Plan8 p;
   p.kind = plan[0], p.mt = plan[1], p.shares = plan[2], p.waves = plan[3], p.n_rest = plan[4], p.mt_rest = plan[5], p.shares_rest = plan[6];
-  return run(args_of(w, x, M, y, ldy, workspace), p, stream);
+  Gemm8Args a = args_of(w, x, M, y, ldy, workspace);
+  if (!x->scales) a.x16 = static_cast<const uint16_t*>(x->codes), a.ldx16 = x->ld;   // bf16 rows
+  return run(a, p, stream);
 }
 
 }  // namespace ccq

@@ -6,6 +6,8 @@
 // wavefront asks for its 4 KB of weights two or three steps ahead, straight into registers: no
 // other wavefront of the workgroup needs them.  Bound by memory: the weights' bytes.  64 rows, 28672 x 8192: 57 us, 4.1 TB/s; 37 rows, 5001 x 7184, six
 // shares: 15.5 us, 3.7 of them for the join (40 blocks of columns alone would leave most of the chip idle).
+#include <type_traits>
+
 #include "ccq_gemm8.h"
 
 namespace ccq {
@@ -21,7 +23,15 @@ struct Gemm8Stream {
   int32_t n_tiles, shares, blocks_per_share;   // blocks_per_share even
 };
 
-template <int MT>
+// The largest over eight neighbouring lanes.
+__device__ __forceinline__ uint32_t max8(uint32_t v) {
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, false));    // quad_perm 1 0 3 2
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, false));    // quad_perm 2 3 0 1
+  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xF, 0xF, false));   // the other way round in each half row
+}
+
+// WIDE: bf16 rows, quantized on their way to LDS.
+template <int MT, bool WIDE>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 4))) void ccq_gemm8_stream_kernel(Gemm8Stream p) {
   constexpr int kRows = 16 * MT, kDepth = depth(MT), kPieces = pieces(MT), kStage = kRows * kStepK;
   extern __shared__ __align__(256) uint8_t lds[];             // two steps of activations, row scales; at the end the sums of the odd blocks
@@ -35,20 +45,22 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   // row scales of the share
   uint8_t* scales = lds + 2 * kStage;
   const int pitch = (p.blocks_per_share + 7) & ~3;
-  for (int i = threadIdx.x; i < rows * blocks; i += 64 * kWaves) {
+  for (int i = threadIdx.x; !WIDE && i < rows * blocks; i += 64 * kWaves) {
     const int r = i / blocks, c = i % blocks;
     scales[r * pitch + c] = a.xs[(int64_t)(m0 + r) * a.ld_xs + first + c];
   }
 
   // Piece q of the step's activations: row q / 16, chunk q % 16, at the chunk's place ^ row % 16 (the reads of 16 rows meet all banks).
-  const uint8_t* x = a.x + (int64_t)m0 * a.ldx;
-  u32x4_t xr[kDepth][kPieces];
+  const uint8_t* x = WIDE ? nullptr : a.x + (int64_t)m0 * a.ldx;
+  const uint16_t* x16 = WIDE ? a.x16 + (int64_t)m0 * a.ldx16 : nullptr;
+  std::conditional_t<WIDE, Wide16, u32x4_t> xr[kDepth][kPieces];
   auto load_x = [&](int step, int at) {
     const int k0 = (first + 2 * step) * kScaleBlock;
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-      const int q = threadIdx.x + 512 * i, row = q >> 4, k = k0 + (q & 15) * 16;
-      xr[at][i] = *reinterpret_cast<const u32x4_t*>(x + (int64_t)min(row, rows - 1) * a.ldx + min(k, a.K - 16));
+      const int q = threadIdx.x + 512 * i, row = min(q >> 4, rows - 1), k = min(k0 + (q & 15) * 16, a.K - 16);
+      if constexpr (WIDE) xr[at][i] = load_wide16(x16 + (int64_t)row * a.ldx16 + k, true);
+      else xr[at][i] = *reinterpret_cast<const u32x4_t*>(x + (int64_t)row * a.ldx + k);
     }
   };
   auto store_x = [&](int step, int at) {
@@ -57,7 +69,14 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     for (int i = 0; i < kPieces; ++i) {
       const int q = threadIdx.x + 512 * i, row = q >> 4;
       const bool there = k0 + (q & 15) * 16 < a.K;
-      u32x4_t v = xr[at][i];
+      u32x4_t v;
+      if constexpr (WIDE) {
+        const uint32_t top = max8(there ? magnitude16(xr[at][i]) : 0);   // of the block: eight threads side by side
+        v = codes16(xr[at][i], top);
+        if ((q & 7) == 0 && row < kRows) scales[row * pitch + 2 * step + (q >> 3 & 1)] = (uint8_t)scale_of(top);
+      } else {
+        v = xr[at][i];
+      }
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] = there ? v[e] : 0;   // zeros past K
       if (row < kRows) *reinterpret_cast<u32x4_t*>(lds + (step & 1) * kStage + row * kStepK + (((q & 15) ^ (row & 15)) * 16)) = v;
@@ -183,9 +202,13 @@ template <int MT>
 int launch(const Gemm8Stream& p, hipStream_t s) {
   constexpr int kRows = 16 * MT;
   const int pitch = (p.blocks_per_share + 7) & ~3, loop = 2 * kRows * kStepK + kRows * pitch, sums = 4 * kRows * 36 * 4, bytes = loop > sums ? loop : sums;
-  const void* kernel = reinterpret_cast<const void*>(ccq_gemm8_stream_kernel<MT>);
+  constexpr bool kWide = MT <= 4;   // (of 96 bf16 rows the registers do not hold three steps)
+  if (p.a.x16 && !kWide) return CCQ_ERR_UNSUPPORTED;
+  const void* kernel = p.a.x16 ? reinterpret_cast<const void*>(ccq_gemm8_stream_kernel<MT, kWide>) : reinterpret_cast<const void*>(ccq_gemm8_stream_kernel<MT, false>);
   if (bytes > 64 * 1024 && hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return CCQ_ERR_HIP;
-  hipLaunchKernelGGL((ccq_gemm8_stream_kernel<MT>), dim3((unsigned)(p.n_tiles * p.shares), (unsigned)((p.a.M + kRows - 1) / kRows)), dim3(64 * kWaves), (unsigned)bytes, s, p);
+  const dim3 grid((unsigned)(p.n_tiles * p.shares), (unsigned)((p.a.M + kRows - 1) / kRows));
+  if (p.a.x16) hipLaunchKernelGGL((ccq_gemm8_stream_kernel<MT, kWide>), grid, dim3(64 * kWaves), (unsigned)bytes, s, p);
+  else hipLaunchKernelGGL((ccq_gemm8_stream_kernel<MT, false>), grid, dim3(64 * kWaves), (unsigned)bytes, s, p);
   return hipGetLastError() == hipSuccess ? CCQ_OK : CCQ_ERR_HIP;
 }
 

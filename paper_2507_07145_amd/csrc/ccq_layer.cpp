@@ -111,20 +111,43 @@ extern "C" int64_t ccq_gemm8_workspace_bytes(const ccq_weight8* w, int32_t M) {
   return gemm8_workspace(w, M);
 }
 
-extern "C" int ccq_gemm8(const ccq_weight8* w, const ccq_rows8* x, int32_t M, void* y, int64_t ldy, void* workspace, int64_t workspace_bytes,
-                         void* hip_stream) {
-  int rc = check_weight8(w);
+static int check_gemm8(const ccq_weight8* w, int32_t M, const void* y, int64_t ldy, const void* workspace) {
+  const int rc = check_weight8(w);
   if (rc != CCQ_OK) return rc;
-  if (!x) return CCQ_ERR_NULL;
   if (M < 0 || ldy < w->N) return CCQ_ERR_BAD_PARAM;
   if (ldy % 8 != 0) return CCQ_ERR_ALIGN;
   if (M == 0) return CCQ_OK;
   if (!w->codes || !w->scales || !y) return CCQ_ERR_NULL;
+  return off16(w->codes) || off16(w->scales) || off16(y) || off16(workspace) ? CCQ_ERR_ALIGN : CCQ_OK;
+}
+
+extern "C" int ccq_gemm8(const ccq_weight8* w, const ccq_rows8* x, int32_t M, void* y, int64_t ldy, void* workspace, int64_t workspace_bytes,
+                         void* hip_stream) {
+  if (w && !x && check_weight8(w) == CCQ_OK) return CCQ_ERR_NULL;
+  int rc = check_gemm8(w, M, y, ldy, workspace);
+  if (rc != CCQ_OK || M == 0) return rc;
   if ((rc = check_rows8(*x, w->K)) != CCQ_OK) return rc;
-  if (off16(w->codes) || off16(w->scales) || off16(y) || off16(workspace)) return CCQ_ERR_ALIGN;
   const int64_t need = gemm8_workspace(w, M);
   if (need > 0 && (!workspace || workspace_bytes < need)) return CCQ_ERR_WORKSPACE;
   return launch_gemm8(w, x, M, y, ldy, workspace, hip_stream);
+}
+
+extern "C" int64_t ccq_gemm8_bf16_workspace_bytes(const ccq_weight8* w, int32_t M) {
+  if (check_weight8(w) != CCQ_OK || M < 0) return -1;
+  return gemm8_bf16_workspace(w, M);
+}
+
+extern "C" int ccq_gemm8_bf16(const ccq_weight8* w, const void* x, int64_t ldx, int32_t M, void* y, int64_t ldy, void* workspace, int64_t workspace_bytes,
+                              void* hip_stream) {
+  const int rc = check_gemm8(w, M, y, ldy, workspace);
+  if (rc != CCQ_OK) return rc;
+  if (ldx < w->K) return CCQ_ERR_BAD_PARAM;
+  if (M == 0) return CCQ_OK;
+  if (!x) return CCQ_ERR_NULL;
+  if (off(x, 2)) return CCQ_ERR_ALIGN;
+  const int64_t need = gemm8_bf16_workspace(w, M);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return CCQ_ERR_WORKSPACE;
+  return launch_gemm8_bf16(w, x, ldx, M, y, ldy, workspace, hip_stream);
 }
 
 extern "C" int ccq_rope_table(const ccq_rope_scaling* s, int32_t rows, int32_t dims, float* table, void* hip_stream) {

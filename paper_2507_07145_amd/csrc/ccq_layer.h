@@ -85,6 +85,8 @@ int launch_cache_append(const ccq_cache* c, const ccq_batch* b, const ccq_rope* 
 int64_t attention_workspace(const ccq_cache* c, const ccq_batch* b, const ccq_attn* a);
 int launch_attention(const ccq_cache* c, const ccq_batch* b, const ccq_attn* a, const ccq_heads* q, const ccq_heads* out, void* workspace, void* stream);
 int64_t gemm8_workspace(const ccq_weight8* w, int M);
+int64_t gemm8_bf16_workspace(const ccq_weight8* w, int M);
+int launch_gemm8_bf16(const ccq_weight8* w, const void* x, int64_t ldx, int M, void* y, int64_t ldy, void* workspace, void* stream);
 int launch_gemm8(const ccq_weight8* w, const ccq_rows8* x, int M, void* y, int64_t ldy, void* workspace, void* stream);
 
 }  // namespace ccq

@@ -11,6 +11,8 @@ struct Entry {
   decltype(&ccq_quantize8) quantize = nullptr;
   decltype(&ccq_gemm8) gemm = nullptr;
   decltype(&ccq_gemm8_workspace_bytes) gemm_workspace = nullptr;
+  decltype(&ccq_gemm8_bf16) gemm_bf16 = nullptr;
+  decltype(&ccq_gemm8_bf16_workspace_bytes) gemm_bf16_workspace = nullptr;
   decltype(&ccq_cache_append) append = nullptr;
   decltype(&ccq_attention) attention = nullptr;
   decltype(&ccq_attention_workspace_bytes) attention_workspace = nullptr;
@@ -139,24 +141,21 @@ PyObject* call_gemm8(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (a[3] != Py_None && (!plain_bf16(y) || y->device() != x->device() || y->size(0) != M || y->size(1) != w.p->N)) return general();
   Workspace ws;
   if (a[4] != Py_None && !ws.of(a[4])) return general();
-  const int64_t need = a[4] == Py_None ? entry.gemm_workspace(w.p, (int32_t)M) : 0;
+  const int64_t need = a[4] != Py_None ? 0 : wide ? entry.gemm_bf16_workspace(w.p, (int32_t)M) : entry.gemm_workspace(w.p, (int32_t)M);
   if (need < 0) return general();
   at::Tensor made;
-  Made8 made8;
-  int rc = CCQ_OK;
+  int rc;
   {
     Unlocked u;
     if (!y) y = &(made = new_output(M, w.p->N, x->device()));
     ws.make(need, x->device());
-    ccq_rows8 rows;
+    const int64_t ldy = a[3] == Py_None || M > 1 ? y->stride(0) : (w.p->N + 7) / 8 * 8;
     if (wide) {
-      made8.make(M, w.p->K, x->device());
-      rows = made8.rows();
-      rc = entry.quantize(x->data_ptr(), ld(x), (int32_t)M, w.p->K, &rows, current_stream());
+      rc = entry.gemm_bf16(w.p, x->data_ptr(), ld(x), (int32_t)M, y->data_ptr(), ldy, ws.ptr, ws.bytes, current_stream());
     } else {
-      rows = {x->data_ptr(), ld(x), static_cast<uint8_t*>(scales->data_ptr()), std::max(scales->stride(0), scales->size(1))};
+      const ccq_rows8 rows = {x->data_ptr(), ld(x), static_cast<uint8_t*>(scales->data_ptr()), std::max(scales->stride(0), scales->size(1))};
+      rc = entry.gemm(w.p, &rows, (int32_t)M, y->data_ptr(), ldy, ws.ptr, ws.bytes, current_stream());
     }
-    if (rc == CCQ_OK) rc = entry.gemm(w.p, &rows, (int32_t)M, y->data_ptr(), a[3] == Py_None ? y->stride(0) : M > 1 ? y->stride(0) : (w.p->N + 7) / 8 * 8, ws.ptr, ws.bytes, current_stream());
   }
   if (rc != CCQ_OK) return PyLong_FromLong(rc);
   if (a[3] == Py_None) return THPVariable_Wrap(std::move(made));
@@ -249,10 +248,10 @@ PyObject* call_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 // bind(addresses of ccq_rms_norm, ccq_quantize8, ccq_gemm8, ccq_gemm8_workspace_bytes, ccq_cache_append, ccq_attention,
-// ccq_attention_workspace_bytes)
+// ccq_attention_workspace_bytes, ccq_gemm8_bf16, ccq_gemm8_bf16_workspace_bytes)
 PyObject* call_bind(PyObject*, PyObject* args) {
-  unsigned long long p[7];
-  if (!PyArg_ParseTuple(args, "KKKKKKK", &p[0], &p[1], &p[2], &p[3], &p[4], &p[5], &p[6])) return nullptr;
+  unsigned long long p[9];
+  if (!PyArg_ParseTuple(args, "KKKKKKKKK", &p[0], &p[1], &p[2], &p[3], &p[4], &p[5], &p[6], &p[7], &p[8])) return nullptr;
   entry.norm = reinterpret_cast<decltype(entry.norm)>(p[0]);
   entry.quantize = reinterpret_cast<decltype(entry.quantize)>(p[1]);
   entry.gemm = reinterpret_cast<decltype(entry.gemm)>(p[2]);
@@ -260,6 +259,8 @@ PyObject* call_bind(PyObject*, PyObject* args) {
   entry.append = reinterpret_cast<decltype(entry.append)>(p[4]);
   entry.attention = reinterpret_cast<decltype(entry.attention)>(p[5]);
   entry.attention_workspace = reinterpret_cast<decltype(entry.attention_workspace)>(p[6]);
+  entry.gemm_bf16 = reinterpret_cast<decltype(entry.gemm_bf16)>(p[7]);
+  entry.gemm_bf16_workspace = reinterpret_cast<decltype(entry.gemm_bf16_workspace)>(p[8]);
   Py_RETURN_NONE;
 }
 

@@ -72,12 +72,14 @@ def _load() -> ctypes.CDLL:
         L, p = binding.load(), ctypes.POINTER
         for name, args in (("ccq_rms_norm", [p(ccq_norm), _vp]), ("ccq_quantize8", [_vp, _i64, _i32, _i32, p(ccq_rows8), _vp]),
                            ("ccq_gemm8", [p(ccq_weight8), p(ccq_rows8), _i32, _vp, _i64, _vp, _i64, _vp]),
+                           ("ccq_gemm8_bf16", [p(ccq_weight8), _vp, _i64, _i32, _vp, _i64, _vp, _i64, _vp]),
                            ("ccq_rope_table", [p(ccq_rope_scaling), _i32, _i32, _vp, _vp]),
                            ("ccq_cache_append", [p(ccq_cache), p(ccq_batch), p(ccq_rope), p(ccq_heads), p(ccq_heads), p(ccq_heads), p(ccq_heads), _i32, _vp]),
                            ("ccq_attention", [p(ccq_cache), p(ccq_batch), p(ccq_attn), p(ccq_heads), p(ccq_heads), _vp, _i64, _vp])):
             f = getattr(L, name)
             f.restype, f.argtypes = ctypes.c_int, args
-        L.ccq_gemm8_workspace_bytes.restype, L.ccq_gemm8_workspace_bytes.argtypes = _i64, [p(ccq_weight8), _i32]
+        for f in (L.ccq_gemm8_workspace_bytes, L.ccq_gemm8_bf16_workspace_bytes):
+            f.restype, f.argtypes = _i64, [p(ccq_weight8), _i32]
         L.ccq_attention_workspace_bytes.restype, L.ccq_attention_workspace_bytes.argtypes = _i64, [p(ccq_cache), p(ccq_batch), p(ccq_attn)]
         _lib = L
     return _lib
@@ -96,7 +98,8 @@ def _calls():
         except ImportError as e:
             raise RuntimeError("_ccq_layer.so is missing or does not load: build it with `python -m paper_2507_07145_amd.build`") from e
         m.bind(*(ctypes.cast(getattr(L, name), _vp).value for name in
-                 ("ccq_rms_norm", "ccq_quantize8", "ccq_gemm8", "ccq_gemm8_workspace_bytes", "ccq_cache_append", "ccq_attention", "ccq_attention_workspace_bytes")))
+                 ("ccq_rms_norm", "ccq_quantize8", "ccq_gemm8", "ccq_gemm8_workspace_bytes", "ccq_cache_append", "ccq_attention", "ccq_attention_workspace_bytes",
+                  "ccq_gemm8_bf16", "ccq_gemm8_bf16_workspace_bytes")))
         _native = m
     return _native
 
@@ -296,36 +299,36 @@ def quantize8(x: torch.Tensor, stream=None) -> Rows8:
 
 
 def gemm8(w: Weight8, x, out: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
-    """y = x W^T through ccq_gemm8; x: Rows8, or bf16 rows that are quantized first (ccq_quantize8)."""
+    """y = x W^T through ccq_gemm8; x: Rows8, or bf16 rows, whose 8-bit rows are formed on the way (ccq_gemm8_bf16)."""
     is8 = type(x) is Rows8
     if stream is None:
         r = _answer((_native or _calls()).gemm8(w.desc, x.codes if is8 else x, x.scales if is8 else None, out, workspace), "ccq_gemm8")
         if r is not None:
             return r
-    if not is8:
-        x = quantize8(x, stream=stream)
-        if stream is not None:   # the temporary returns to the allocator at once; its memory must outlive the kernels
-            x.codes.record_stream(stream)
-            x.scales.record_stream(stream)
-    _on_this_gpu(x.codes, w.codes, out)
+    _need(is8 or (x.dtype == torch.bfloat16 and _rows(x)), "x: Rows8 or bf16 rows are needed")
+    held = x.codes if is8 else x
+    _on_this_gpu(held, w.codes, out)
     M, N = x.shape[0], w.N
     _need(x.shape[1] == w.K, "x and the weights have another K")
-    y = binding._new_output(M, N, x.codes.device) if out is None else out
+    y = binding._new_output(M, N, held.device) if out is None else out
     _need(y.dtype == torch.bfloat16 and y.shape == (M, N) and _rows(y), "out: bf16 rows [M][N] are needed")
     if workspace is None:
-        workspace = binding._workspace(gemm8_workspace_bytes(w, M), y.device)
-        if workspace is not None and stream is not None:
+        workspace = binding._workspace(gemm8_workspace_bytes(w, M, not is8), y.device)
+        if workspace is not None and stream is not None:   # it returns to the allocator at once; its memory must outlive the kernels
             workspace.record_stream(stream)
-    d = x.desc()
-    _check(_load().ccq_gemm8(ctypes.byref(w.desc), ctypes.byref(d), M, _t_ptr(y), y.stride(0) if M > 1 else (N + 7) // 8 * 8, _t_ptr(workspace),
-                             0 if workspace is None else workspace.nbytes, _stream_ptr(stream)), "ccq_gemm8")
+    tail = (M, _t_ptr(y), y.stride(0) if M > 1 else (N + 7) // 8 * 8, _t_ptr(workspace), 0 if workspace is None else workspace.nbytes, _stream_ptr(stream))
+    if is8:
+        _check(_load().ccq_gemm8(ctypes.byref(w.desc), ctypes.byref(x.desc()), *tail), "ccq_gemm8")
+    else:
+        _check(_load().ccq_gemm8_bf16(ctypes.byref(w.desc), _t_ptr(x), _ld(x), *tail), "ccq_gemm8_bf16")
     return y
 
 
-def gemm8_workspace_bytes(w: Weight8, M: int) -> int:
-    need = int(_load().ccq_gemm8_workspace_bytes(ctypes.byref(w.desc), M))
+def gemm8_workspace_bytes(w: Weight8, M: int, bf16_rows: bool = False) -> int:
+    f = _load().ccq_gemm8_bf16_workspace_bytes if bf16_rows else _load().ccq_gemm8_workspace_bytes
+    need = int(f(ctypes.byref(w.desc), M))
     if need < 0:
-        raise CcqError(-2, "ccq_gemm8_workspace_bytes")
+        raise CcqError(-2, f.__name__)
     return need
 
 

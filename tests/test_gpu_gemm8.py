@@ -106,3 +106,24 @@ def test_another_stream():
     got = layer.gemm8(weight, x, stream=s)
     s.synchronize()
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("M", [1, 7, 16, 40, 64, 90, 150, 400, 1100])
+@pytest.mark.parametrize("N,K", [(300, 1040), (5001, 2000), (2048, 7168)])
+def test_bf16_rows(M, N, K):
+    """The bits of quantize8 and the product, through the native path, the general one with a stream, and a workspace of the caller's."""
+    w, ws, _, _ = _inputs(1, N, K, 21)
+    weight = layer.Weight8(w.to(r.DEV), ws.to(r.DEV))
+    x = torch.randn(M, K + 3, generator=r.gen(22)).bfloat16().to(r.DEV)[:, 1:K + 1]
+    got = layer.gemm8(weight, x)
+    want, size = x.double() @ r.values(w).to(r.DEV).mul(ws.repeat_interleave(128, 0)[:N].repeat_interleave(128, 1)[:, :K].double().to(r.DEV)).t(), None
+    # a value's rounding is 2^-4 of it at most, independent from value to value: the norm of the error is far below that of the result
+    assert ((got.double() - want).norm() / want.norm()).item() < 2.0 ** -4
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    other = layer.gemm8(weight, x, stream=s)
+    s.synchronize()
+    need = layer.gemm8_workspace_bytes(weight, M, True)
+    given = torch.full((need + 64,), 0xFF, dtype=torch.uint8, device=r.DEV)
+    own = layer.gemm8(weight, x, workspace=given[:need] if need else None)
+    assert torch.equal(other, got) and torch.equal(own, got) and bool((given[need:] == 0xFF).all())

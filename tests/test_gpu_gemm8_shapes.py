@@ -24,6 +24,15 @@ def _as(weight, rows, M, N, plan):
     return y[:, :N]
 
 
+def _as_bf16(weight, x, N, plan):
+    """The same with bf16 rows."""
+    class Rows:
+        @staticmethod
+        def desc():
+            return layer.ccq_rows8(x.data_ptr(), x.stride(0), None, 0)
+    return _as(weight, Rows, x.shape[0], N, plan)
+
+
 def plan(M, N, K):
     out, time = (ctypes.c_int32 * 7)(), ctypes.c_double()
     layer._load().ccq_gemm8_plan(M, N, K, out, ctypes.byref(time))
@@ -43,6 +52,22 @@ def test_shape(M, N, K, p):
     want, lost = t._product(w, ws, x, xs, K)
     got = _as(layer.Weight8(w.to(r.DEV)[:, :K], ws.to(r.DEV)), layer.Rows8(x.to(r.DEV)[:, :K], xs.to(r.DEV)), M, N, p)
     t._check(got, want, lost, K)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 16, 16), (5, 130, 384), (37, 601, 1936), (64, 333, 768), (100, 129, 144), (129, 300, 1552)])
+@pytest.mark.parametrize("p", [q for q in PLANS if q[0] == FEW or (q[0] == STREAM and q[1] <= 4)], ids=str)
+def test_bf16_rows_give_the_bits_of_their_8_bit_rows(M, N, K, p):
+    w, ws, _, _ = t._inputs(M, N, K, M + N + K, 3)
+    wide = torch.randn(M, K + 5, generator=r.gen(M)).mul(torch.randn(M, 1, generator=r.gen(N)).mul(8).exp2()).bfloat16()
+    wide[:, 3:3 + min(K, 100)] *= 2.0 ** -30
+    if M > 2:
+        wide[1, K // 2] = float("nan")
+        wide[2, 3] = float("-inf")
+        wide[M - 1] = 0
+    x = wide.to(r.DEV)[:, 3:3 + K]   # (rows that start at odd addresses)
+    weight = layer.Weight8(w.to(r.DEV)[:, :K], ws.to(r.DEV))
+    want = _as(weight, layer.quantize8(x), M, N, p)
+    assert torch.equal(_as_bf16(weight, x, N, p).contiguous().view(torch.int16), want.contiguous().view(torch.int16))
 
 
 @pytest.mark.parametrize("p", [[BLOCK, 1, 1, 4, 0, 0, 1], [BLOCK, 2, 1, 4, 0, 0, 1], [BLOCK, 4, 1, 4, 0, 0, 1], [STREAM, 4, 1, 4, 0, 0, 1], [FEW, 1, 1, 16, 0, 0, 1]], ids=str)

@@ -60,6 +60,22 @@ def test_gemm8():
             assert l._load().ccq_gemm8(ctypes.byref(wd), ctypes.byref(xd), M, P, 512, P, n - 1, None) == WORKSPACE
 
 
+def test_gemm8_of_bf16_rows():
+    def call(w={}, x=P, ldx=256, M=2, y=P, ldy=128, ws=None, n=0):
+        wd = l.ccq_weight8(**{**dict(K=256, N=128, codes=P, ldw=256, scales=P, ld_scales=2), **w})
+        return l._load().ccq_gemm8_bf16(ctypes.byref(wd), x, ldx, M, y, ldy, ws, n, None)
+    assert l._load().ccq_gemm8_bf16(None, P, 256, 1, P, 128, None, 0, None) == NULL
+    assert call(M=0) == 0 and call(M=-1) == BAD and call(ldx=255) == BAD and call(x=None) == NULL and call(x=P + 1) == ALIGN and call(w=dict(K=0)) == BAD
+    assert call(ldy=120) == BAD and call(ldy=129) == ALIGN and call(y=None) == NULL and call(w=dict(codes=None)) == NULL and call(y=P + 8) == ALIGN and call(ws=P + 8) == ALIGN
+    wd = l.ccq_weight8(28672, 512, P, 28672, P, 224)
+    need = l._load().ccq_gemm8_bf16_workspace_bytes
+    assert need(None, 1) == -1 and need(ctypes.byref(wd), -1) == -1 and need(ctypes.byref(wd), 0) == 0
+    n = need(ctypes.byref(wd), 2048)
+    assert n >= 2048 * (28672 + 224)   # the 8-bit rows of a call that is served in blocks
+    for ws, size in ((None, 0), (P, n - 1)):
+        assert l._load().ccq_gemm8_bf16(ctypes.byref(wd), P, 28672, 2048, P, 512, ws, size, None) == WORKSPACE
+
+
 def cache(**kw):
     return l.ccq_cache(**{**dict(pages=4, page_tokens=16, kv_heads=2, head_dim=64, k=P, v=P, k_scales=P, v_scales=P), **kw})
 
