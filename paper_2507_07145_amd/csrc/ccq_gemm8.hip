@@ -148,8 +148,8 @@ double stream_time(int mt, int shares, int M, int N, int blocks) {
 // `alone`: one block of rows, whose weights come from memory and not from a neighbour's reading
 double block_rounds_time(int mi, double groups, double steps, bool alone) {
   const double full = busy(groups);
-  const double per = mi == 4 ? 1.45 + 0.5 * full : mi == 2 ? (alone ? 0.9 + 0.6 * full : 0.8 + 0.35 * full) : alone ? 1.0 + 0.45 * full : 0.75 + 0.3 * full;
-  return rounds_of(groups) * ((alone ? 5.0 : mi == 4 ? 4.0 : mi == 2 ? 2.5 : 0.5) + steps * per);
+  const double per = mi == 4 ? 1.45 + 0.5 * full : mi == 2 ? (alone ? 0.9 + 0.6 * full : 0.8 + 0.35 * full) : alone ? 0.7 + 0.4 * full : 0.55 + 0.22 * full;
+  return rounds_of(groups) * ((alone ? 5.0 : mi == 4 ? 4.0 : 2.5) + steps * per);
 }
 double block_groups(int mi, int M, int n, int shares) { return (double)((M + 64 * mi - 1) / (64 * mi)) * ((n + 255) / 256) * shares; }
 

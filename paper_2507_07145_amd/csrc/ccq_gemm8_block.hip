@@ -3,13 +3,13 @@
 // A workgroup of eight wavefronts, two per SIMD, owns a block of 64 MI x 256 outputs (two wavefronts along the rows, four along the columns,
 // 32 MI x 64 each) and a share of K.  A block of K (128) is a step.  Activations and weights go from memory to LDS without passing
 // registers (16 bytes a lane), in the order of memory; a row's eight 16-byte chunks are permuted by its number, so that the operand reads
-// of neighbouring rows meet all banks.  Two steps lie in LDS: before its last tile of rows a step's operands are all in registers, and its place
-// is filled again, so that a copy has a step's time to arrive.
+// of neighbouring rows meet all banks.  Two steps lie in LDS, or three: before its last tile of rows a step's operands are all in registers, and its place
+// is filled again, so that a copy has a step's time to arrive, or two.
 // Products are scaled MFMAs 32x32x64, two for a block of K, into a fresh result that one multiply-add per register adds to the
 // accumulators with the weights' scale.  The vector unit does not reach accumulation registers: 512 registers a wavefront would not help.
 // 2048 rows, 8192 x 8192 (a block to each CU): 120 us, 2.3 PFLOP/s; 18432 x 7168: 276 us, 1.96.  Bound by the way into and out of LDS (64 KB in, 192 KB out a step) and by
-// power; on 2048 x 16384 x 7168 an earlier form with 262 us took 190 without the copies, 231 with copies that
-// all read one address, no less without waiting for them.
+// power; on 2048 x 16384 x 7168 an earlier form with 262 us took 190 without the copies, 231 with copies that all read one address, no less without
+// waiting for them.
 #include <type_traits>
 
 #include "ccq_gemm8.h"
@@ -35,10 +35,15 @@ __device__ __forceinline__ f32x16_t zeros16() {
   for (int i = 0; i < 16; ++i) z[i] = 0.f;
   return z;
 }
+// Steps that lie in LDS.  A copy that waits for memory takes longer than a step of the smallest blocks: of 64 rows, 256 x 8192 x 8192, with three 49 us, with two 67.  In blocks of 128
+// rows three gain 8 % where weights come from memory (73 us, 67) and lose 7 % where neighbours have read them (2048 x 2048 x 7168: 55 us, 59).
+constexpr int slots(int mi) { return mi == 1 ? 3 : 2; }
+
 template <int MI>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void ccq_gemm8_block_kernel(Gemm8Block p) {
   constexpr int kRows = 64 * MI, kXBytes = kRows * kScaleBlock;
-  extern __shared__ __align__(256) uint8_t lds[];   // two steps of activations, two of weights, row scales, the weights' scales
+  constexpr int kSlots = slots(MI);
+  extern __shared__ __align__(256) uint8_t lds[];   // kSlots steps of activations, as many of weights, row scales, the weights' scales
   const Gemm8Args& a = p.a;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, h = lane >> 5;
   const int wm = wave & 1, wn = wave >> 1;
@@ -84,7 +89,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     }
   };
   auto x_slot = [&](int s) { return lds + s * kXBytes; };
-  auto w_slot = [&](int s) { return lds + 2 * kXBytes + s * kWBytes; };
+  auto w_slot = [&](int s) { return lds + kSlots * kXBytes + s * kWBytes; };
   // Copy c of a wavefront's kCopies of a step: weights, then activations.
   constexpr int kCopiers = MI < 4 ? 4 : 8, kMyW = kCols / 8 / kCopiers, kMyX = kRows / 8 / kCopiers, kCopies = kMyW + kMyX;
   const int copier = wave & (kCopiers - 1);
@@ -95,7 +100,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
 
   // scales: of the rows a byte each, 64 steps at a time in LDS (from memory they are a cache line each in every step); of the weights one
   // number (64 columns lie in one block)
-  uint8_t* scales = lds + 2 * kXBytes + 2 * kWBytes;
+  uint8_t* scales = lds + kSlots * (kXBytes + kWBytes);
   auto stage_scales = [&](int step) {
     for (int i = threadIdx.x; i < kRows * (kScaleSteps / 4); i += 64 * kWaves) {
       const int row = i / (kScaleSteps / 4), c = i % (kScaleSteps / 4) * 4;
@@ -132,6 +137,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   constexpr std::false_type no{};
   constexpr int kLastTile = MI - 1;
   int xs_now[MI];
+  int third = 0;   // of step k, of three
   i32x8_t w[2][2], x[2][2];
   auto load_x = [&](int slot, int i) {
     const uint8_t* rows = x_slot(slot) + (wm * 32 * MI + i * 32) * kScaleBlock;
@@ -161,7 +167,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   // (after the last step of those that are staged: another's, and read again when the next are)
   auto next_scale = [&](int k, int i) { xs_now[i] = my_scales[i * 32 * kScalePitch + (k + 1 - first) % kScaleSteps]; };
   auto one_step = [&](int k, auto AHEAD, auto RAGGED) {
-    const int slot = (k - first) & 1;
+    const int slot = kSlots == 2 ? (k - first) & 1 : third, next = kSlots == 2 ? slot ^ 1 : third == 2 ? 0 : third + 1;
+    const bool turn = MI == 4 || ((k - first) & 1) == wave >> 2;   // to copy
     // (which of the three an eighth takes, and where operands lie, is formed in each step, not kept)
     asm volatile("" : "+v"(xr.at[0]), "+v"(xr.at[1]), "+v"(xr.at[2]), "+v"(wr.at[0]), "+v"(wr.at[1]), "+v"(wr.at[2]), "+v"(operand_at));
     __builtin_amdgcn_sched_barrier(0);
@@ -180,41 +187,42 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     // (products are not moved past the branch)
 #pragma unroll
     for (int i = 0; i < kLastTile; ++i) asm volatile("" : "+v"(acc[i][0]), "+v"(acc[i][1]));
-    wait_loads<0>();
+    if (kSlots == 2 || turn) wait_loads<0>();   // step k + 1 (of three steps the others' copies under way are of step k + 2)
     lds_barrier();
     __builtin_amdgcn_sched_barrier(0);
     // A wavefront that issues copies waits for the path to LDS, which they keep busy for half a step.  In the largest blocks all eight copy, some before each of
     // the last two products, and the others' products go on meanwhile (2048 x 18432 x 7168: 318 us, with one wavefront of a SIMD that copies in turn 340); in
     // smaller ones the barriers lie too close for that, and in turn is faster (256 x 8192 x 8192 in blocks of 128 rows: 74 us against 84).
     if constexpr (decltype(AHEAD)::value && MI < 4) {
-      if (wave >> 2 == slot) {
+      if (turn) {
 #pragma unroll
-        for (int c = 0; c < kCopies; ++c) copy_one(c, k + 2, slot, RAGGED);
+        for (int c = 0; c < kCopies; ++c) copy_one(c, k + kSlots, slot, RAGGED);
       }
     }
     __builtin_amdgcn_sched_barrier(0);
     auto copy_some = [&](int from, int to) {
       if constexpr (decltype(AHEAD)::value && MI == 4) {
 #pragma unroll
-        for (int c = from; c < to; ++c) copy_one(c, k + 2, slot, RAGGED);
+        for (int c = from; c < to; ++c) copy_one(c, k + kSlots, slot, RAGGED);
       }
     };
-    if (kLastTile % 2 == 1) load_x(slot ^ 1, 0);
+    if (kLastTile % 2 == 1) load_x(next, 0);
     copy_some(0, (kCopies + 1) / 2);
     multiply(kLastTile, 0);
     __builtin_amdgcn_sched_barrier(0);
-    load_w(slot ^ 1, 0);
+    load_w(next, 0);
     copy_some((kCopies + 1) / 2, kCopies);
     multiply(kLastTile, 1);
-    if (kLastTile % 2 == 0) load_x(slot ^ 1, 0);
+    if (kLastTile % 2 == 0) load_x(next, 0);
     next_scale(k, 0);
     s_read = my_ws[(k + 1 - first) % kScaleSteps];
     s_before = s;
+    third = next;
     __builtin_amdgcn_sched_barrier(0);
   };
 
-  for (int step = first; step < min(first + 2, last); ++step) {
-    if (MI < 4 && wave >> 2 != step - first) continue;
+  for (int step = first; step < min(first + kSlots, last); ++step) {
+    if (MI < 4 && wave >> 2 != ((step - first) & 1)) continue;
 #pragma unroll
     for (int c = 0; c < kCopies; ++c) copy_one(c, step, step - first, yes);
   }
@@ -231,8 +239,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     next_scale(k - 1, 0);
     s_read = my_ws[(k - first) % kScaleSteps];
     if (k == first) s_before = uniform(s_read);
-    for (; k < until && k + 3 < last; ++k) one_step(k, yes, no);
-    for (; k < until && k + 2 < last; ++k) one_step(k, yes, yes);
+    for (; k < until && k + kSlots + 1 < last; ++k) one_step(k, yes, no);
+    for (; k < until && k + kSlots < last; ++k) one_step(k, yes, yes);
     for (; k < until; ++k) one_step(k, no, no);   // (in the last one the operands asked for are of no step: what lies in the place, unused)
     lds_barrier();   // the scales of these steps have been read
   }
@@ -284,7 +292,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
 
 template <int MI>
 int launch(const Gemm8Block& p, hipStream_t s) {
-  constexpr int kLds = 2 * 64 * MI * kScaleBlock + 2 * kWBytes + 64 * MI * kScalePitch + 2 * kScaleSteps * 4;
+  constexpr int kLds = slots(MI) * (64 * MI * kScaleBlock + kWBytes) + 64 * MI * kScalePitch + 2 * kScaleSteps * 4;
   const void* kernel = reinterpret_cast<const void*>(ccq_gemm8_block_kernel<MI>);
   if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds) != hipSuccess) return CCQ_ERR_HIP;
   const int per = (p.m_tiles * p.n_tiles + 7) / 8;
