@@ -30,7 +30,7 @@ struct AttnArgs {
   float* image_scales;    // the same, eight numbers each
   int32_t pages, page_shift, kv_heads, q_heads, group, table_width, batch, tokens, max_new, max_len;
   int32_t causal, window;
-  int32_t chunk, splits;
+  int32_t splits;   // at most so many pieces
   int32_t row_tiles, tile_rows, image_tiles;
   float c;          // scale * log2(e)
 };
@@ -55,11 +55,13 @@ __device__ __forceinline__ AttnSequence attn_sequence(const AttnArgs& a, int b) 
 // Cached tokens [first, second) that the row at position p sees.
 __device__ __forceinline__ int seen_end(const AttnArgs& a, const AttnSequence& s, int p) { return a.causal ? min(max(p + 1, 0), s.len) : s.len; }
 
-// Rows [first_row, last_row] of a tile and what they see: any of them, all of them; the tile's splits begin at `begin`, every a.chunk tokens.
+// Rows [first_row, last_row] of a tile and what they see: any of them, all of them; the tokens from `begin` on in `splits` pieces of `chunk`.  The pieces go by
+// the sequence's own length, not by the bound that the grid was made for: a program whose max_len is what its page table holds has them too.
+constexpr int kUnit = 256;   // tokens of the smallest piece
 struct AttnTile {
   int first_row, last_row;
   int any_lo, any_hi, all_lo, all_hi, begin;
-  __device__ __forceinline__ int splits(const AttnArgs& a) const { return max(1, min(a.splits, (any_hi - begin - 1) / a.chunk + 1)); }
+  int chunk, splits;
 };
 __device__ __forceinline__ AttnTile attn_tile(const AttnArgs& a, const AttnSequence& s, int first_row, int rows) {
   AttnTile t;
@@ -71,6 +73,9 @@ __device__ __forceinline__ AttnTile attn_tile(const AttnArgs& a, const AttnSeque
   t.all_lo = first_seen(a, p_last);
   t.all_hi = seen_end(a, s, p_first);
   t.begin = min(t.any_lo, max(s.len, 0)) & ~63;
+  const int units = (max(t.any_hi - t.begin, 1) - 1) / kUnit + 1, per = (units - 1) / a.splits + 1;
+  t.chunk = per > 0x7FFFFFFF / kUnit ? 0x7FFFFFFF : per * kUnit;
+  t.splits = (units - 1) / per + 1;
   return t;
 }
 

@@ -33,8 +33,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
   const int rows = s.n * a.group, row0 = tile * (16 * NT);
   if (row0 >= rows) return;
   const AttnTile t = attn_tile(a, s, row0, 16 * NT);
-  if (split >= t.splits(a)) return;
-  const int begin = t.begin + split * a.chunk, from = begin, to = begin + min(a.chunk, t.any_hi - begin);
+  if (split >= t.splits) return;
+  const int begin = t.begin + split * t.chunk, from = begin, to = begin + min(t.chunk, t.any_hi - begin);
 
   // queries: the same dimensions as a lane's pieces of the keys
   bf16x8_t q[NT][STEPS];
@@ -225,7 +225,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
 constexpr int kFewSplits = 8;
 __device__ __forceinline__ int splits_of(const AttnArgs& a, const AttnSequence& s, int r) {   // r: new token * q_heads + q head
   const int row = r / a.q_heads * a.group + r % a.q_heads % a.group;
-  return attn_tile(a, s, row / a.tile_rows * a.tile_rows, a.tile_rows).splits(a);
+  return attn_tile(a, s, row / a.tile_rows * a.tile_rows, a.tile_rows).splits;
 }
 template <int D>
 __global__ __launch_bounds__(256) void ccq_attention_join_few_kernel(AttnArgs a) {
@@ -306,7 +306,7 @@ __global__ __launch_bounds__(256) void ccq_attention_join_kernel(AttnArgs a) {
 struct Plan {
   bool many = false;   // the kernel for many rows
   int nt = 0;          // the one for few: 16-row tiles of a workgroup
-  int tile_rows = 0, row_tiles = 0, chunk = 0, splits = 0;
+  int tile_rows = 0, row_tiles = 0, splits = 0;
   int image_tiles = 0;   // of a sequence
 };
 constexpr int64_t kMostImages = int64_t(4) << 30;   // bytes of workspace; past it the kernel for few rows
@@ -333,7 +333,8 @@ Plan plan_of(const ccq_cache* c, const ccq_batch* b, const ccq_attn* at) {
   // tokens that a tile of rows can see
   int64_t range = b->max_len;
   if (at->window > 0) range = std::min<int64_t>(range, (int64_t)at->window + std::min<int64_t>(b->max_new, p.tile_rows / (at->q_heads / c->kv_heads) + 1) + 63);
-  const int64_t unit = kWaves * kTile, units = std::max<int64_t>(1, (range + unit - 1) / unit), groups = pairs * p.row_tiles;
+  static_assert(kUnit == kWaves * kTile, "");
+  const int64_t units = std::max<int64_t>(1, (range + kUnit - 1) / kUnit), groups = pairs * p.row_tiles;
   // Split so far that every place for a workgroup has one (one a CU for many rows, two for few): further, the parts and the second launch cost more than
   // shorter pieces bring (64 sequences of up to 8192, 8 heads: 131 us whole, 135 in two, 144 in four; 131072 tokens of 8 heads: 55 us in 32 or 64 pieces, 60 in
   // 86; 16 sequences of up to 2048: 20 us whole, 16.5 in four; for many rows
@@ -344,7 +345,6 @@ Plan plan_of(const ccq_cache* c, const ccq_batch* b, const ccq_attn* at) {
   const int64_t per = (units + splits - 1) / splits;
   p.splits = (int)((units + per - 1) / per);
   if (p.many) p.image_tiles = (int)image_tiles(b, at);
-  p.chunk = p.splits == 1 ? 0x7FFFFFFF : (int)(per * unit);
   return p;
 }
 
@@ -388,7 +388,7 @@ int launch_attention(const ccq_cache* c, const ccq_batch* b, const ccq_attn* at,
   a.pages = c->pages, a.page_shift = __builtin_ctz((unsigned)c->page_tokens), a.kv_heads = c->kv_heads, a.q_heads = at->q_heads;
   a.group = at->q_heads / c->kv_heads, a.table_width = b->table_width, a.batch = b->batch, a.tokens = b->tokens, a.max_new = b->max_new, a.max_len = b->max_len;
   a.causal = at->causal, a.window = at->window, a.c = at->scale * 1.4426950408889634f;
-  a.chunk = p.chunk, a.splits = p.splits, a.row_tiles = p.row_tiles, a.tile_rows = p.tile_rows;
+  a.splits = p.splits, a.row_tiles = p.row_tiles, a.tile_rows = p.tile_rows;
   if (p.splits > 1) {
     a.part_o = static_cast<float*>(workspace);
     a.part_ml = a.part_o + (int64_t)p.splits * b->tokens * at->q_heads * c->head_dim;

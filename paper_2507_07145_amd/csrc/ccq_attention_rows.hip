@@ -74,8 +74,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int rows = s.n * a.group, row0 = tile * kManyRows;
   if (row0 >= rows) return;
   const AttnTile all = attn_tile(a, s, row0, kManyRows);   // of the workgroup
-  if (split >= all.splits(a)) return;
-  const int from = all.begin + split * a.chunk, to = from + min(a.chunk, all.any_hi - from);
+  if (split >= all.splits) return;
+  const int from = all.begin + split * all.chunk, to = from + min(all.chunk, all.any_hi - from);
   const AttnTile own = attn_tile(a, s, min(row0 + wave * 32, all.last_row), 32);   // of the wavefront
   const int all_lo = own.all_lo, all_hi = own.all_hi, last_row = all.last_row;
 

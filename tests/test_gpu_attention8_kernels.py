@@ -100,3 +100,16 @@ def test_the_rule_reaches_every_kernel():
 def test_a_chunk_as_the_rule_serves_it():
     t._run([(700, 1100)], 64, 128, 4, 32, seed=21)
     t._run([(500, 900), (130, 640)], 32, 128, 8, 32, window=300, seed=22)
+
+
+@pytest.mark.parametrize("pairs", [[(1, 900)], [(1, 2500), (1, 30), (1, 0), (1, 1300)], [(40, 700), (3, 2000)]])
+def test_a_bound_far_above_the_lengths(pairs):
+    """max_len is what a table could hold: the pieces go by the lengths."""
+    seq = r.Sequences(pairs, 64, 31)
+    cache = r.random_cache(seq, 2, 128, 32)
+    q = torch.randn(seq.T, 8, 128, generator=r.gen(33)).bfloat16()
+    batch = seq.batch()
+    far = layer.Batch(batch.offsets, batch.lens, batch.table, seq.T, max(n for n, _ in pairs), 1 << 17)
+    got = layer.attention(r.to_device(cache), far, q.to(r.DEV)).cpu().double()
+    want, size = r.attend(seq, cache, q, 128 ** -0.5)
+    assert bool(((got - want).abs() <= r.attend_limit(want, size)).all())
