@@ -10,6 +10,7 @@
 // 2048 rows, 8192 x 8192 (a block to each CU): 120 us, 2.3 PFLOP/s; 18432 x 7168: 276 us, 1.96.  Bound by the way into and out of LDS (64 KB in, 192 KB out a step) and by
 // power; on 2048 x 16384 x 7168 an earlier form with 262 us took 190 without the copies, 231 with copies that all read one address, no less without
 // waiting for them.
+#include <algorithm>
 #include <type_traits>
 
 #include "ccq_gemm8.h"
@@ -28,6 +29,11 @@ struct Gemm8Block {
 };
 
 __device__ const uint4 kZeros = {0, 0, 0, 0};
+
+// Which 16-byte chunk of a block of K a lane copies in an eighth of rows.  Eighths past the one in which the array ends are read as that one, its chunks with them: what
+// lies past K goes by the chunk that is read.
+__host__ __device__ __forceinline__ int block_chunk(int lane, int eighth) { return (lane & 7) ^ (lane >> 3) ^ (eighth & 1); }
+__host__ __device__ __forceinline__ bool block_past_k(int lane, int eighth, int end, int k, int K) { return k + block_chunk(lane, eighth < end ? eighth : end) * 16 >= K; }
 
 __device__ __forceinline__ f32x16_t zeros16() {
   f32x16_t z;
@@ -67,10 +73,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   auto rows_from = [&](const uint8_t* base, int64_t ld, int last_row) {
     Rows r = {base, ld, last_row >> 3, {}};
 #pragma unroll
-    for (int e = 0; e < 3; ++e) {
-      const int parity = e < 2 ? e : r.end & 1, row = e < 2 ? sub : min(sub, last_row & 7);
-      r.at[e] = (uint32_t)row * (uint32_t)ld + (((lane & 7) ^ sub ^ parity) * 16);
-    }
+    for (int e = 0; e < 3; ++e) r.at[e] = (uint32_t)(e < 2 ? sub : min(sub, last_row & 7)) * (uint32_t)ld + block_chunk(lane, e < 2 ? e : r.end) * 16;
     return r;
   };
   Rows xr = rows_from(a.x + (int64_t)m0 * a.ldx, a.ldx, a.M - 1 - m0), wr = rows_from(a.w + (int64_t)n0 * a.ldw, a.ldw, a.N - 1 - n0);
@@ -81,7 +84,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     asm volatile("" : "+v"(from));   // (the zero extension stays next to the load)
     if constexpr (decltype(RAGGED)::value) {   // zeros past K
       const uint8_t* src = base + from;
-      if (k + (((lane & 7) ^ sub ^ (eighth & 1)) * 16) >= a.K) src = reinterpret_cast<const uint8_t*>(&kZeros);
+      if (block_past_k(lane, eighth, r.end, k, a.K)) src = reinterpret_cast<const uint8_t*>(&kZeros);
       __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
     } else {   // (with global loads to LDS under way the compiler waits for all LDS reads at once)
       const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, -1, 4 << 15);   // (data format 32 bits)
@@ -301,6 +304,14 @@ int launch(const Gemm8Block& p, hipStream_t s) {
 }
 
 }  // namespace
+
+// For tests, no part of the interface: what lane `lane` copies for eighth `eighth` of rows 0 .. last_row at column k: the offset of its 16 bytes, or -1 for zeros.
+extern "C" int64_t ccq_gemm8_block_source(int32_t lane, int32_t eighth, int32_t last_row, int64_t ld, int32_t k, int32_t K) {
+  const int end = last_row >> 3, sub = lane >> 3;
+  if (block_past_k(lane, eighth, end, k, K)) return -1;
+  const int64_t row = eighth >= end ? 8 * end + std::min(sub, last_row & 7) : 8 * eighth + sub;
+  return row * ld + k + block_chunk(lane, std::min(eighth, end)) * 16;
+}
 
 int launch_gemm8_block(const Gemm8Args& a, int mi, int shares, void* stream) {
   Gemm8Block p;
