@@ -153,7 +153,8 @@ PyObject* call_gemm8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (wide) {
       rc = entry.gemm_bf16(w.p, x->data_ptr(), ld(x), (int32_t)M, y->data_ptr(), ldy, ws.ptr, ws.bytes, current_stream());
     } else {
-      const ccq_rows8 rows = {x->data_ptr(), ld(x), static_cast<uint8_t*>(scales->data_ptr()), std::max(scales->stride(0), scales->size(1))};
+      const int64_t ld_scales = M > 1 ? scales->stride(0) : std::max(scales->stride(0), scales->size(1));
+      const ccq_rows8 rows = {x->data_ptr(), ld(x), static_cast<uint8_t*>(scales->data_ptr()), ld_scales};
       rc = entry.gemm(w.p, &rows, (int32_t)M, y->data_ptr(), ldy, ws.ptr, ws.bytes, current_stream());
     }
   }

@@ -132,6 +132,11 @@ def _ld(t) -> int:
     return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), (t.shape[1] + 15) // 16 * 16)
 
 
+def _own_rows(t) -> bool:
+    """Rows that do not share memory, as rows made by expand do."""
+    return t.shape[0] <= 1 or t.stride(0) >= t.shape[1]
+
+
 def _type(t) -> int:
     _need(t.dtype in (torch.bfloat16, torch.float32), "bf16 or fp32 is needed")
     return FP32 if t.dtype == torch.float32 else BF16
@@ -152,6 +157,7 @@ class Rows8:
         c, s = self.codes, self.scales
         _need(_is_codes(c) and _rows(c) and _is_scales(s) and _rows(s), "8-bit rows: codes [M][N] and scales [M][ceil(N / 128)] are needed")
         _need(s.shape == (c.shape[0], -(-c.shape[1] // BLOCK)) and s.device == c.device, "8-bit rows: one scale per row and block of 128 columns is needed")
+        _need(_own_rows(s), "8-bit rows: rows of scales must not overlap")
         return ccq_rows8(c.data_ptr(), _ld(c), s.data_ptr(), max(s.stride(0), s.shape[1]))
 
 
@@ -168,6 +174,7 @@ class Weight8:
         N, K = codes.shape
         _need(scales.dtype == torch.float32 and _rows(scales) and scales.shape == (-(-N // BLOCK), -(-K // BLOCK)) and scales.device == codes.device,
               "8-bit weights: fp32 scales [ceil(N / 128)][ceil(K / 128)] are needed")
+        _need(_own_rows(scales), "8-bit weights: rows of scales must not overlap")
         self.codes, self.scales = codes, scales
         self.desc = ccq_weight8(K, N, codes.data_ptr(), _ld(codes), scales.data_ptr(), max(scales.stride(0), scales.shape[1]))
 
@@ -212,6 +219,7 @@ class Batch:
         _need(lens.dim() == 1 and (B <= 1 or lens.stride(0) == 1) and offsets.shape == (B + 1,) and (B == 0 or offsets.stride(0) == 1),
               "batch: offsets [B + 1] and lens [B] are needed")
         _need(_rows(table) and table.shape[0] == B, "batch: a table [B][pages of a sequence] is needed")
+        _need(_own_rows(table), "batch: rows of the table must not overlap")
         self.offsets, self.lens, self.table = offsets, lens, table
         self.desc = ccq_batch(B, tokens, max_new, max_len, offsets.data_ptr(), lens.data_ptr(), table.data_ptr(), max(table.stride(0), table.shape[1]), table.shape[1])
 

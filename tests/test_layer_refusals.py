@@ -1,0 +1,28 @@
+"""Tensors behind the layer operators' descriptors that no kernel may be given.  Host only: nothing is launched."""
+import pytest
+import torch
+
+from paper_2507_07145_amd import layer as l
+
+
+def u8(*s):
+    return torch.zeros(s, dtype=torch.uint8)
+
+
+def i32(*s):
+    return torch.zeros(s, dtype=torch.int32)
+
+
+def test_rows_that_share_memory():
+    """A kernel reads rows [i][width] of the table and of scales; of one row that was expanded to several there is only one."""
+    with pytest.raises(ValueError, match="overlap"):
+        l.Batch(i32(5), i32(4), i32(1, 3).expand(4, 3), 4, 1, 48)
+    with pytest.raises(ValueError, match="overlap"):
+        l.Batch(i32(5), i32(4), i32(6).as_strided((4, 3), (1, 1)), 4, 1, 48)
+    with pytest.raises(ValueError, match="overlap"):
+        l.Batch(i32(5), i32(4), i32(1, 1).expand(4, 1), 4, 1, 16)
+    with pytest.raises(ValueError, match="overlap"):
+        l.Weight8(u8(300, 256), torch.zeros(1, 2).expand(3, 2))
+    for N in (128, 300):
+        with pytest.raises(ValueError, match="overlap"):
+            l.Rows8(u8(4, N), u8(1, -(-N // 128)).expand(4, -(-N // 128))).desc()
