@@ -40,6 +40,11 @@ class Struct {
 };
 
 bool here(const at::Tensor* t) { return t->is_cuda() && t->device().index() == c10::hip::current_device(); }
+// The GPU that a descriptor's memory is on, as its object has it.
+bool here(PyObject* gpu) {
+  int overflow = 0;
+  return PyLong_Check(gpu) && PyLong_AsLongAndOverflow(gpu, &overflow) == c10::hip::current_device();
+}
 bool is_codes(const at::Tensor* t) { return t->scalar_type() == at::kByte || t->scalar_type() == at::kFloat8_e4m3fn; }
 bool is_scales(const at::Tensor* t) { return t->scalar_type() == at::kByte || t->scalar_type() == at::kFloat8_e8m0fnu; }
 bool rows_like(const at::Tensor* t, const at::Tensor* x) {
@@ -124,24 +129,24 @@ PyObject* call_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-// gemm8(weight's descriptor, x (bf16) or codes, None or scales, out or None, workspace or None)
+// gemm8(weight's descriptor, its GPU, x (bf16) or codes, None or scales, out or None, workspace or None)
 PyObject* call_gemm8(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
-  if (n != 5 || !entry.gemm || looked_on()) return general();
+  if (n != 6 || !entry.gemm || looked_on()) return general();
   const Struct<ccq_weight8> w(a[0]);
-  const at::Tensor *x = tensor(a[1]), *scales = tensor(a[2]), *y = tensor(a[3]);
-  if (!w.p || !x || x->dim() != 2 || !here(x) || x->size(1) != w.p->K || x->stride(1) != 1) return general();
+  const at::Tensor *x = tensor(a[2]), *scales = tensor(a[3]), *y = tensor(a[4]);
+  if (!w.p || !here(a[1]) || !x || x->dim() != 2 || !here(x) || x->size(1) != w.p->K || x->stride(1) != 1) return general();
   const int64_t M = x->size(0);
   if (M > INT32_MAX) return general();
-  const bool wide = a[2] == Py_None;
+  const bool wide = a[3] == Py_None;
   if (wide ? x->scalar_type() != at::kBFloat16
            : !is_codes(x) || !scales || scales->dim() != 2 || !is_scales(scales) || scales->device() != x->device() || scales->size(0) != M ||
                  scales->size(1) != (w.p->K + 127) / 128 || (scales->size(1) > 1 && scales->stride(1) != 1))
     return general();
-  if (a[3] != Py_None && (!plain_bf16(y) || y->device() != x->device() || y->size(0) != M || y->size(1) != w.p->N)) return general();
+  if (a[4] != Py_None && (!plain_bf16(y) || y->device() != x->device() || y->size(0) != M || y->size(1) != w.p->N)) return general();
   Workspace ws;
-  if (a[4] != Py_None && !ws.of(a[4])) return general();
-  const int64_t need = a[4] != Py_None ? 0 : wide ? entry.gemm_bf16_workspace(w.p, (int32_t)M) : entry.gemm_workspace(w.p, (int32_t)M);
+  if (a[5] != Py_None && !ws.of(a[5])) return general();
+  const int64_t need = a[5] != Py_None ? 0 : wide ? entry.gemm_bf16_workspace(w.p, (int32_t)M) : entry.gemm_workspace(w.p, (int32_t)M);
   if (need < 0) return general();
   at::Tensor made;
   int rc;
@@ -149,7 +154,7 @@ PyObject* call_gemm8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Unlocked u;
     if (!y) y = &(made = new_output(M, w.p->N, x->device()));
     ws.make(need, x->device());
-    const int64_t ldy = a[3] == Py_None || M > 1 ? y->stride(0) : (w.p->N + 7) / 8 * 8;
+    const int64_t ldy = a[4] == Py_None || M > 1 ? y->stride(0) : (w.p->N + 7) / 8 * 8;
     if (wide) {
       rc = entry.gemm_bf16(w.p, x->data_ptr(), ld(x), (int32_t)M, y->data_ptr(), ldy, ws.ptr, ws.bytes, current_stream());
     } else {
@@ -159,9 +164,9 @@ PyObject* call_gemm8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
   }
   if (rc != CCQ_OK) return PyLong_FromLong(rc);
-  if (a[3] == Py_None) return THPVariable_Wrap(std::move(made));
-  Py_INCREF(a[3]);
-  return a[3];
+  if (a[4] == Py_None) return THPVariable_Wrap(std::move(made));
+  Py_INCREF(a[4]);
+  return a[4];
   END_HANDLE_TH_ERRORS
 }
 
@@ -177,22 +182,22 @@ at::Tensor new_heads(const at::Tensor* like) {
   return at::detail::empty_cuda(like->sizes(), at::kBFloat16, like->device(), std::nullopt);
 }
 
-// append(cache's, batch's descriptor, k or None, v or None, q or None, q_out or None, rope's descriptor or None)
+// append(cache's descriptor and GPU, batch's, k or None, v or None, q or None, q_out or None, rope's descriptor or None, its GPU)
 PyObject* call_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
-  if (n != 7 || !entry.append || looked_on()) return general();
+  if (n != 10 || !entry.append || looked_on()) return general();
   const Struct<ccq_cache> c(a[0]);
-  const Struct<ccq_batch> b(a[1]);
+  const Struct<ccq_batch> b(a[2]);
   std::optional<Struct<ccq_rope>> rope;
-  if (a[6] != Py_None) rope.emplace(a[6]);
-  if (!c.p || !b.p || (rope && !rope->p)) return general();
-  const at::Tensor *k = tensor(a[2]), *v = tensor(a[3]), *q = tensor(a[4]), *out = tensor(a[5]);
+  if (a[8] != Py_None) rope.emplace(a[8]);
+  if (!here(a[1]) || !here(a[3]) || !here(a[9]) || !c.p || !b.p || (rope && !rope->p)) return general();
+  const at::Tensor *k = tensor(a[4]), *v = tensor(a[5]), *q = tensor(a[6]), *out = tensor(a[7]);
   ccq_heads hk, hv, hq, ho;
   const int64_t T = b.p->tokens, D = c.p->head_dim;
-  if (a[2] != Py_None && !heads_of(k, T, c.p->kv_heads, D, &hk)) return general();
-  if (a[3] != Py_None && !heads_of(v, T, c.p->kv_heads, D, &hv)) return general();
-  if (a[4] != Py_None && (!heads_of(q, T, 0, D, &hq) || q->size(1) > INT32_MAX)) return general();
-  if (a[5] != Py_None && (!q || !heads_of(out, T, q->size(1), D, &ho))) return general();
+  if (a[4] != Py_None && !heads_of(k, T, c.p->kv_heads, D, &hk)) return general();
+  if (a[5] != Py_None && !heads_of(v, T, c.p->kv_heads, D, &hv)) return general();
+  if (a[6] != Py_None && (!heads_of(q, T, 0, D, &hq) || q->size(1) > INT32_MAX)) return general();
+  if (a[7] != Py_None && (!q || !heads_of(out, T, q->size(1), D, &ho))) return general();
   at::Tensor made;
   int rc;
   {
@@ -205,30 +210,30 @@ PyObject* call_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
                       current_stream());
   }
   if (rc != CCQ_OK || !q) return PyLong_FromLong(rc);
-  if (a[5] == Py_None) return THPVariable_Wrap(std::move(made));
-  Py_INCREF(a[5]);
-  return a[5];
+  if (a[7] == Py_None) return THPVariable_Wrap(std::move(made));
+  Py_INCREF(a[7]);
+  return a[7];
   END_HANDLE_TH_ERRORS
 }
 
-// attention(cache's, batch's descriptor, q, scale, window, causal, out or None, workspace or None)
+// attention(cache's descriptor and GPU, batch's, q, scale, window, causal, out or None, workspace or None)
 PyObject* call_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
-  if (n != 8 || !entry.attention || looked_on()) return general();
+  if (n != 10 || !entry.attention || looked_on()) return general();
   const Struct<ccq_cache> c(a[0]);
-  const Struct<ccq_batch> b(a[1]);
-  const at::Tensor *q = tensor(a[2]), *out = tensor(a[6]);
+  const Struct<ccq_batch> b(a[2]);
+  const at::Tensor *q = tensor(a[4]), *out = tensor(a[8]);
   ccq_heads hq, ho;
-  if (!c.p || !b.p || !heads_of(q, b.p->tokens, 0, c.p->head_dim, &hq) || q->size(1) > INT32_MAX) return general();
-  if (!PyFloat_Check(a[3]) || !PyLong_Check(a[4])) return general();
+  if (!here(a[1]) || !here(a[3]) || !c.p || !b.p || !heads_of(q, b.p->tokens, 0, c.p->head_dim, &hq) || q->size(1) > INT32_MAX) return general();
+  if (!PyFloat_Check(a[5]) || !PyLong_Check(a[6])) return general();
   int overflow = 0;
-  const long window = PyLong_AsLongAndOverflow(a[4], &overflow);
+  const long window = PyLong_AsLongAndOverflow(a[6], &overflow);
   if (overflow || window < 0 || window > INT32_MAX) return general();
-  if (a[6] != Py_None && !heads_of(out, b.p->tokens, q->size(1), c.p->head_dim, &ho)) return general();
-  ccq_attn at = {(int32_t)q->size(1), a[5] == Py_True ? 1 : 0, (int32_t)window, (float)PyFloat_AS_DOUBLE(a[3])};
+  if (a[8] != Py_None && !heads_of(out, b.p->tokens, q->size(1), c.p->head_dim, &ho)) return general();
+  ccq_attn at = {(int32_t)q->size(1), a[7] == Py_True ? 1 : 0, (int32_t)window, (float)PyFloat_AS_DOUBLE(a[5])};
   Workspace ws;
-  if (a[7] != Py_None && !ws.of(a[7])) return general();
-  const int64_t need = a[7] == Py_None ? entry.attention_workspace(c.p, b.p, &at) : 0;
+  if (a[9] != Py_None && !ws.of(a[9])) return general();
+  const int64_t need = a[9] == Py_None ? entry.attention_workspace(c.p, b.p, &at) : 0;
   if (need < 0) return general();
   at::Tensor made;
   int rc;
@@ -242,9 +247,9 @@ PyObject* call_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     rc = entry.attention(c.p, b.p, &at, &hq, &ho, ws.ptr, ws.bytes, current_stream());
   }
   if (rc != CCQ_OK) return PyLong_FromLong(rc);
-  if (a[6] == Py_None) return THPVariable_Wrap(std::move(made));
-  Py_INCREF(a[6]);
-  return a[6];
+  if (a[8] == Py_None) return THPVariable_Wrap(std::move(made));
+  Py_INCREF(a[8]);
+  return a[8];
   END_HANDLE_TH_ERRORS
 }
 

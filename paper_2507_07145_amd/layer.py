@@ -115,6 +115,12 @@ def _on_this_gpu(*tensors) -> None:
             _need(t.is_cuda and t.device.index == torch.cuda.current_device(), "tensors have to be on the current GPU")
 
 
+def _gpu(t) -> int:
+    """The GPU whose memory a descriptor points to: kernels read what lies behind it unseen."""
+    _need(t.is_cuda, "tensors on a GPU are needed")
+    return t.device.index
+
+
 def _is_codes(t) -> bool:
     return t.dtype in (torch.uint8, torch.float8_e4m3fn)
 
@@ -175,7 +181,7 @@ class Weight8:
         _need(scales.dtype == torch.float32 and _rows(scales) and scales.shape == (-(-N // BLOCK), -(-K // BLOCK)) and scales.device == codes.device,
               "8-bit weights: fp32 scales [ceil(N / 128)][ceil(K / 128)] are needed")
         _need(_own_rows(scales), "8-bit weights: rows of scales must not overlap")
-        self.codes, self.scales = codes, scales
+        self.codes, self.scales, self.gpu = codes, scales, _gpu(codes)
         self.desc = ccq_weight8(K, N, codes.data_ptr(), _ld(codes), scales.data_ptr(), max(scales.stride(0), scales.shape[1]))
 
     @property
@@ -197,7 +203,7 @@ class Cache8:
         for s in (k_scales, v_scales):
             _need(_is_scales(s) and s.is_contiguous() and s.shape == (pages, heads), "cache: scales are contiguous bytes [pages][heads]")
         _need(k.device == v.device == k_scales.device == v_scales.device, "cache: all on one device")
-        self.k, self.v, self.k_scales, self.v_scales = k, v, k_scales, v_scales
+        self.k, self.v, self.k_scales, self.v_scales, self.gpu = k, v, k_scales, v_scales, _gpu(k)
         self.desc = ccq_cache(pages, page_tokens, heads, dim, k.data_ptr(), v.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr())
 
     @classmethod
@@ -220,7 +226,7 @@ class Batch:
               "batch: offsets [B + 1] and lens [B] are needed")
         _need(_rows(table) and table.shape[0] == B, "batch: a table [B][pages of a sequence] is needed")
         _need(_own_rows(table), "batch: rows of the table must not overlap")
-        self.offsets, self.lens, self.table = offsets, lens, table
+        self.offsets, self.lens, self.table, self.gpu = offsets, lens, table, _gpu(lens)
         self.desc = ccq_batch(B, tokens, max_new, max_len, offsets.data_ptr(), lens.data_ptr(), table.data_ptr(), max(table.stride(0), table.shape[1]), table.shape[1])
 
 
@@ -232,7 +238,7 @@ class Rope:
         _need(table.dtype == torch.float32 and table.is_contiguous() and table.dim() == 2 and table.shape[1] == dims, "rope: a contiguous fp32 table [positions][dims] is needed")
         _need(positions is None or (positions.dtype == torch.int32 and positions.is_contiguous() and positions.dim() == 1 and positions.device == table.device),
               "rope: int32 positions, one per token row, are needed")
-        self.table, self.positions = table, positions
+        self.table, self.positions, self.gpu = table, positions, _gpu(table)
         self.desc = ccq_rope(table.data_ptr(), table.shape[0], dims, int(interleaved), None if positions is None else positions.data_ptr())
 
 
@@ -310,7 +316,7 @@ def gemm8(w: Weight8, x, out: torch.Tensor | None = None, workspace: torch.Tenso
     """y = x W^T through ccq_gemm8; x: Rows8, or bf16 rows, whose 8-bit rows are formed on the way (ccq_gemm8_bf16)."""
     is8 = type(x) is Rows8
     if stream is None:
-        r = _answer((_native or _calls()).gemm8(w.desc, x.codes if is8 else x, x.scales if is8 else None, out, workspace), "ccq_gemm8")
+        r = _answer((_native or _calls()).gemm8(w.desc, w.gpu, x.codes if is8 else x, x.scales if is8 else None, out, workspace), "ccq_gemm8")
         if r is not None:
             return r
     _need(is8 or (x.dtype == torch.bfloat16 and _rows(x)), "x: Rows8 or bf16 rows are needed")
@@ -353,7 +359,7 @@ def cache_append(cache: Cache8, batch: Batch, k: torch.Tensor | None, v: torch.T
     if rope is not None and rope.positions is not None:
         _need(rope.positions.numel() >= batch.desc.tokens, "rope: a position per token row is needed")
     if stream is None:
-        r = (_native or _calls()).append(cache.desc, batch.desc, k, v, q, q_out, None if rope is None else rope.desc)
+        r = (_native or _calls()).append(cache.desc, cache.gpu, batch.desc, batch.gpu, k, v, q, q_out, None if rope is None else rope.desc, cache.gpu if rope is None else rope.gpu)
         if type(r) is int:
             _check(r, "ccq_cache_append")
             return None
@@ -381,7 +387,7 @@ def attention(cache: Cache8, batch: Batch, q: torch.Tensor, scale: float | None 
     if scale is None:
         scale = cache.desc.head_dim ** -0.5
     if stream is None:
-        r = _answer((_native or _calls()).attention(cache.desc, batch.desc, q, float(scale), window, causal, out, workspace), "ccq_attention")
+        r = _answer((_native or _calls()).attention(cache.desc, cache.gpu, batch.desc, batch.gpu, q, float(scale), window, causal, out, workspace), "ccq_attention")
         if r is not None:
             return r
     _on_this_gpu(cache.k, batch.lens, q, out)

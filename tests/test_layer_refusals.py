@@ -26,3 +26,17 @@ def test_rows_that_share_memory():
     for N in (128, 300):
         with pytest.raises(ValueError, match="overlap"):
             l.Rows8(u8(4, N), u8(1, -(-N // 128)).expand(4, -(-N // 128))).desc()
+
+
+def test_tensors_on_the_host():
+    """A descriptor holds addresses only, and kernels read there: its tensors have to lie on a GPU when it is made."""
+    with pytest.raises(ValueError, match="GPU"):
+        l.Weight8(u8(128, 256), torch.ones(1, 2))
+    with pytest.raises(ValueError, match="GPU"):
+        l.Cache8(u8(2, 1, 16, 64), u8(2, 1, 64, 16), u8(2, 1), u8(2, 1))
+    with pytest.raises(ValueError, match="GPU"):
+        l.Cache8.empty(2, 16, 1, 64, device="cpu")
+    with pytest.raises(ValueError, match="GPU"):
+        l.Batch(i32(3), i32(2), i32(2, 3), 2, 1, 3)
+    with pytest.raises(ValueError, match="GPU"):
+        l.Rope(torch.zeros(4, 8))
