@@ -410,6 +410,13 @@ def _workspace(nbytes: int, device) -> torch.Tensor | None:
     return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes > 0 else None
 
 
+def _given_workspace(workspace: torch.Tensor, x: torch.Tensor) -> torch.Tensor:
+    """A caller's workspace: kernels write its bytes from the first address on."""
+    if workspace.device != x.device or not workspace.is_contiguous():
+        raise ValueError("workspace: a contiguous tensor on the operands' GPU is needed")
+    return workspace
+
+
 def _new_output(rows: int, N: int, device) -> torch.Tensor:
     """bf16 [rows][N] whose row stride is a multiple of 8 elements, as the entry points require."""
     ld = (N + 7) // 8 * 8
@@ -434,6 +441,8 @@ def gemm(w: Weight, x: torch.Tensor, out: torch.Tensor | None = None, workspace:
         workspace = _workspace(need, x.device)
         if workspace is not None and stream is not None:
             workspace.record_stream(stream)   # the temporary returns to the allocator at once; its memory must outlive the kernels
+    else:
+        _given_workspace(workspace, x)
     ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
     L = load()
     if launch is None:
@@ -489,6 +498,8 @@ def grouped_gemm(w: Weight, x: torch.Tensor, sorted_rows: torch.Tensor, expert_o
         workspace = _workspace(max(grouped_workspace_bytes(w, P), 0), x.device)
         if workspace is not None and stream is not None:
             workspace.record_stream(stream)
+    else:
+        _given_workspace(workspace, x)
     ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
     cs, ss, abs_ = w.strides()
     host = None

@@ -56,9 +56,10 @@ struct Workspace {
   at::Tensor held;
   void* ptr = nullptr;
   int64_t bytes = 0;
-  bool of(PyObject* given) {
+  // (contiguous memory of the operands' GPU: kernels write `bytes` bytes from ptr on)
+  bool of(PyObject* given, const at::Tensor* x) {
     const at::Tensor* t = tensor(given);
-    if (!t) return false;
+    if (!t || t->device() != x->device() || !t->is_contiguous()) return false;
     ptr = t->data_ptr();
     bytes = (int64_t)t->nbytes();
     return true;

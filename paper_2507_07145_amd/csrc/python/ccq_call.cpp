@@ -67,7 +67,7 @@ PyObject* call_gemm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const int64_t M = x->size(0);
   if (M > INT32_MAX) return general();
   Workspace ws;
-  if (a[3] != Py_None && !ws.of(a[3])) return general();
+  if (a[3] != Py_None && !ws.of(a[3], x)) return general();
   const int64_t need = a[3] == Py_None ? entry.gemm_workspace(d.w, (int32_t)M) : 0;
   if (need < 0) return general();
   at::Tensor made;
@@ -163,7 +163,7 @@ PyObject* call_grouped(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const int64_t P = rows->numel();
   if (P > INT32_MAX || x->size(0) > INT32_MAX) return general();
   Workspace ws;
-  if (a[6] != Py_None && !ws.of(a[6])) return general();
+  if (a[6] != Py_None && !ws.of(a[6], x)) return general();
   const int64_t need = a[6] == Py_None ? entry.grouped_workspace(d.w, (int32_t)E, (int32_t)P) : 0;
   at::Tensor made;
   int rc;

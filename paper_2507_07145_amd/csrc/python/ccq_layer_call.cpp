@@ -145,7 +145,7 @@ PyObject* call_gemm8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return general();
   if (a[4] != Py_None && (!plain_bf16(y) || y->device() != x->device() || y->size(0) != M || y->size(1) != w.p->N)) return general();
   Workspace ws;
-  if (a[5] != Py_None && !ws.of(a[5])) return general();
+  if (a[5] != Py_None && !ws.of(a[5], x)) return general();
   const int64_t need = a[5] != Py_None ? 0 : wide ? entry.gemm_bf16_workspace(w.p, (int32_t)M) : entry.gemm_workspace(w.p, (int32_t)M);
   if (need < 0) return general();
   at::Tensor made;
@@ -232,7 +232,7 @@ PyObject* call_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (a[8] != Py_None && !heads_of(out, b.p->tokens, q->size(1), c.p->head_dim, &ho)) return general();
   ccq_attn at = {(int32_t)q->size(1), a[7] == Py_True ? 1 : 0, (int32_t)window, (float)PyFloat_AS_DOUBLE(a[5])};
   Workspace ws;
-  if (a[9] != Py_None && !ws.of(a[9])) return general();
+  if (a[9] != Py_None && !ws.of(a[9], q)) return general();
   const int64_t need = a[9] == Py_None ? entry.attention_workspace(c.p, b.p, &at) : 0;
   if (need < 0) return general();
   at::Tensor made;

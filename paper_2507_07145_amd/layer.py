@@ -330,6 +330,8 @@ def gemm8(w: Weight8, x, out: torch.Tensor | None = None, workspace: torch.Tenso
         workspace = binding._workspace(gemm8_workspace_bytes(w, M, not is8), y.device)
         if workspace is not None and stream is not None:   # it returns to the allocator at once; its memory must outlive the kernels
             workspace.record_stream(stream)
+    else:
+        binding._given_workspace(workspace, held)
     tail = (M, _t_ptr(y), y.stride(0) if M > 1 else (N + 7) // 8 * 8, _t_ptr(workspace), 0 if workspace is None else workspace.nbytes, _stream_ptr(stream))
     if is8:
         _check(_load().ccq_gemm8(ctypes.byref(w.desc), ctypes.byref(x.desc()), *tail), "ccq_gemm8")
@@ -403,6 +405,8 @@ def attention(cache: Cache8, batch: Batch, q: torch.Tensor, scale: float | None 
         workspace = binding._workspace(need, q.device)
         if workspace is not None and stream is not None:
             workspace.record_stream(stream)
+    else:
+        binding._given_workspace(workspace, q)
     _check(_load().ccq_attention(ctypes.byref(cache.desc), ctypes.byref(batch.desc), ctypes.byref(a), ctypes.byref(hq), ctypes.byref(ho), _t_ptr(workspace),
                                  0 if workspace is None else workspace.nbytes, _stream_ptr(stream)), "ccq_attention")
     return out

@@ -15,3 +15,24 @@ def test_scales_whose_rows_share_memory_are_refused():
         with pytest.raises((ValueError, layer.CcqError)):
             layer.gemm8(w, layer.Rows8(codes, one.expand(4, 2)), **kw)
     assert layer.gemm8(w, layer.Rows8(codes, one.repeat(4, 1))).shape == (4, 64)
+
+
+@pytest.mark.parametrize("general", [False, True])
+def test_workspaces_on_the_host_or_in_pieces_are_refused(general):
+    """Where a workspace would be written to: the refusal comes before any launch."""
+    from paper_2507_07145_amd import binding as b
+    from paper_2507_07145_amd import synth
+    kw = dict(stream=torch.cuda.current_stream()) if general else {}
+    bad = [torch.empty(8 << 20, dtype=torch.uint8), torch.empty(2, 8 << 20, dtype=torch.uint8, device=r.DEV)[:, ::2], torch.empty(8 << 20, 2, dtype=torch.uint8, device=r.DEV)[:, 0]]
+    w = layer.Weight8(torch.zeros(512, 7168, dtype=torch.uint8, device=r.DEV), torch.ones(4, 56, device=r.DEV))
+    x = torch.zeros(300, 7168, dtype=torch.bfloat16, device=r.DEV)
+    assert layer.gemm8_workspace_bytes(w, 300, True) > 0
+    seq = r.Sequences([(1, 5000)], 64)
+    cache, batch, q = r.to_device(r.random_cache(seq, 1, 64, 1)), seq.batch(), torch.zeros(1, 4, 64, dtype=torch.bfloat16, device=r.DEV)
+    two = b.quantize(torch.from_numpy(synth.weights_normal(512, 1024, synth.rng(0, 0))).to(r.DEV), b.NARROW)
+    rows, offsets = torch.arange(300, dtype=torch.int32, device=r.DEV), torch.tensor([0, 300], dtype=torch.int32, device=r.DEV)
+    for ws in bad:
+        for call in (lambda: layer.gemm8(w, x, workspace=ws, **kw), lambda: layer.attention(cache, batch, q, workspace=ws, **kw),
+                     lambda: b.gemm(two, x[:, :1024], workspace=ws, **kw), lambda: b.grouped_gemm(two, x[:, :1024], rows, offsets, workspace=ws, **kw)):
+            with pytest.raises(ValueError, match="workspace"):
+                call()

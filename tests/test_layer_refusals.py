@@ -40,3 +40,12 @@ def test_tensors_on_the_host():
         l.Batch(i32(3), i32(2), i32(2, 3), 2, 1, 3)
     with pytest.raises(ValueError, match="GPU"):
         l.Rope(torch.zeros(4, 8))
+
+
+def test_workspaces_that_kernels_cannot_write():
+    x = torch.empty(4, 128, device="meta")   # (another device than the workspaces')
+    for ws, like in ((u8(64), x), (u8(64, 2)[:, 0], u8(1)), (u8(64, 2)[::2], u8(1))):
+        with pytest.raises(ValueError, match="workspace"):
+            l.binding._given_workspace(ws, like)
+    ws = u8(64)
+    assert l.binding._given_workspace(ws, u8(1)) is ws
