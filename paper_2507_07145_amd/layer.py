@@ -167,6 +167,19 @@ class Rows8:
         return ccq_rows8(c.data_ptr(), _ld(c), s.data_ptr(), max(s.stride(0), s.shape[1]))
 
 
+def _on(stream, make, read_here: bool = True):
+    """What `make` allocates for work on `stream` (None: the current one), from that stream's memory: the current stream's may still be in use there by
+    kernels whose tensors were dropped.  A result is kept until the current stream has read it."""
+    if stream is None:
+        return make()
+    here = torch.cuda.current_stream()
+    with torch.cuda.stream(stream):
+        t = make()
+    for x in (t.codes, t.scales) if type(t) is Rows8 else (t,) if read_here and t is not None else ():
+        x.record_stream(here)
+    return t
+
+
 def _new_rows8(M: int, N: int, device) -> Rows8:
     codes = torch.empty((M, (N + 15) // 16 * 16), dtype=torch.uint8, device=device)[:, :N]
     return Rows8(codes, torch.empty((M, -(-N // BLOCK)), dtype=torch.uint8, device=device))
@@ -250,7 +263,7 @@ def rope_table(rows: int, dims: int, base: float = 10000.0, kind: str = "none", 
     """Cosines and sines of positions 0 .. rows - 1, fp32 [rows][dims], through ccq_rope_table; `kind` is the scaling for contexts longer
     than the trained one: "none", "linear", "base" or "parts"."""
     _need(kind in _KINDS, f"kind is one of {', '.join(_KINDS)}")
-    out = torch.empty((rows, dims), dtype=torch.float32, device=device)
+    out = _on(stream, lambda: torch.empty((rows, dims), dtype=torch.float32, device=device))
     s = ccq_rope_scaling(_KINDS[kind], base, factor, original_length, fast, slow, magnitude)
     with torch.cuda.device(out.device):
         _check(_load().ccq_rope_table(ctypes.byref(s), rows, dims, _t_ptr(out), _stream_ptr(stream)), "ccq_rope_table")
@@ -286,11 +299,11 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor | None, eps: float = 1e-6, re
               "residual and residual_out: rows like x's, of one type, are needed")
         n.residual, n.ld_residual, n.residual_type = residual.data_ptr(), _ld(residual), _type(residual)
         n.sum, n.ld_sum = total.data_ptr(), _ld(total)
-    y8 = _new_rows8(M, N, x.device) if rows8 else None
+    y8 = _on(stream, lambda: _new_rows8(M, N, x.device)) if rows8 else None
     if rows8:
         n.y8 = y8.desc()
     elif out is None:
-        out = binding._new_output(M, N, x.device)
+        out = _on(stream, lambda: binding._new_output(M, N, x.device))
     if out is not None:
         _need(out.dtype == torch.bfloat16 and out.shape == x.shape and _rows(out), "out: bf16 rows like x's are needed")
         n.y, n.ldy = out.data_ptr(), _ld(out)
@@ -306,7 +319,7 @@ def quantize8(x: torch.Tensor, stream=None) -> Rows8:
             return Rows8(*r)
     _need(x.dtype == torch.bfloat16 and _rows(x) and x.shape[1] > 0, "x: bf16 rows are needed")
     _on_this_gpu(x)
-    out = _new_rows8(*x.shape, x.device)
+    out = _on(stream, lambda: _new_rows8(*x.shape, x.device))
     d = out.desc()
     _check(_load().ccq_quantize8(_t_ptr(x), _ld(x), x.shape[0], x.shape[1], ctypes.byref(d), _stream_ptr(stream)), "ccq_quantize8")
     return out
@@ -324,12 +337,10 @@ def gemm8(w: Weight8, x, out: torch.Tensor | None = None, workspace: torch.Tenso
     _on_this_gpu(held, w.codes, out)
     M, N = x.shape[0], w.N
     _need(x.shape[1] == w.K, "x and the weights have another K")
-    y = binding._new_output(M, N, held.device) if out is None else out
+    y = _on(stream, lambda: binding._new_output(M, N, held.device)) if out is None else out
     _need(y.dtype == torch.bfloat16 and y.shape == (M, N) and _rows(y), "out: bf16 rows [M][N] are needed")
     if workspace is None:
-        workspace = binding._workspace(gemm8_workspace_bytes(w, M, not is8), y.device)
-        if workspace is not None and stream is not None:   # it returns to the allocator at once; its memory must outlive the kernels
-            workspace.record_stream(stream)
+        workspace = _on(stream, lambda: binding._workspace(gemm8_workspace_bytes(w, M, not is8), y.device), read_here=False)
     else:
         binding._given_workspace(workspace, held)
     tail = (M, _t_ptr(y), y.stride(0) if M > 1 else (N + 7) // 8 * 8, _t_ptr(workspace), 0 if workspace is None else workspace.nbytes, _stream_ptr(stream))
@@ -373,7 +384,7 @@ def cache_append(cache: Cache8, batch: Batch, k: torch.Tensor | None, v: torch.T
     hq = ho = None
     if q is not None:
         hq = _heads(q, T, None, D, "q")
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
+        q_out = _on(stream, lambda: torch.empty(q.shape, dtype=q.dtype, device=q.device)) if q_out is None else q_out
         ho = _heads(q_out, T, q.shape[1], D, "q_out")
     else:
         _need(q_out is None, "q_out needs a q")
@@ -395,16 +406,14 @@ def attention(cache: Cache8, batch: Batch, q: torch.Tensor, scale: float | None 
     _on_this_gpu(cache.k, batch.lens, q, out)
     T, D = batch.desc.tokens, cache.desc.head_dim
     hq = _heads(q, T, None, D, "q")
-    out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+    out = _on(stream, lambda: torch.empty(q.shape, dtype=q.dtype, device=q.device)) if out is None else out
     ho = _heads(out, T, q.shape[1], D, "out")
     a = ccq_attn(q.shape[1], int(bool(causal)), window, scale)
     if workspace is None:
         need = int(_load().ccq_attention_workspace_bytes(ctypes.byref(cache.desc), ctypes.byref(batch.desc), ctypes.byref(a)))
         if need < 0:
             raise CcqError(-2, "ccq_attention")
-        workspace = binding._workspace(need, q.device)
-        if workspace is not None and stream is not None:
-            workspace.record_stream(stream)
+        workspace = _on(stream, lambda: binding._workspace(need, q.device), read_here=False)
     else:
         binding._given_workspace(workspace, q)
     _check(_load().ccq_attention(ctypes.byref(cache.desc), ctypes.byref(batch.desc), ctypes.byref(a), ctypes.byref(hq), ctypes.byref(ho), _t_ptr(workspace),

@@ -36,3 +36,29 @@ def test_workspaces_on_the_host_or_in_pieces_are_refused(general):
                      lambda: b.gemm(two, x[:, :1024], workspace=ws, **kw), lambda: b.grouped_gemm(two, x[:, :1024], rows, offsets, workspace=ws, **kw)):
             with pytest.raises(ValueError, match="workspace"):
                 call()
+
+
+def _memory_of(t):
+    """The stream whose memory pool a tensor lies in."""
+    for s in torch.cuda.memory_snapshot():
+        if s["address"] <= t.data_ptr() < s["address"] + s["total_size"]:
+            return s["stream"]
+    raise AssertionError("no segment holds the tensor")
+
+
+def test_results_on_another_stream_come_from_its_memory():
+    """The current stream's memory may still be read there, by kernels under way whose tensors were dropped; another stream must not write it."""
+    s = torch.cuda.Stream()
+    x = torch.randn(20, 256, generator=r.gen(0)).bfloat16().to(r.DEV)
+    w = layer.Weight8(torch.zeros(64, 256, dtype=torch.uint8, device=r.DEV), torch.ones(1, 2, device=r.DEV))
+    seq = r.Sequences([(3, 90)], 16)
+    cache, batch = r.to_device(r.random_cache(seq, 1, 64, 1)), seq.batch()
+    q = torch.randn(3, 4, 64, generator=r.gen(1)).bfloat16().to(r.DEV)
+    s.wait_stream(torch.cuda.current_stream())
+    rows, q8 = layer.rms_norm(x, None, rows8=True, stream=s), layer.quantize8(x, stream=s)
+    made = [layer.rms_norm(x, None, stream=s), rows.codes, rows.scales, q8.codes, q8.scales, layer.gemm8(w, x, stream=s), layer.gemm8(w, q8, stream=s),
+            layer.attention(cache, batch, q, stream=s), layer.cache_append(cache, batch, None, None, q=q, stream=s), layer.rope_table(10, 8, stream=s)]
+    s.synchronize()
+    assert [_memory_of(t) for t in made] == [s.cuda_stream] * len(made)
+    assert _memory_of(layer.rms_norm(x, None)) == torch.cuda.current_stream().cuda_stream
+    assert torch.equal(made[1], layer.rms_norm(x, None, rows8=True).codes) and torch.equal(made[8], q) and torch.equal(made[9], layer.rope_table(10, 8))
