@@ -91,6 +91,9 @@ __device__ __forceinline__ bf16x8_t values_bf16(uint32_t lo, uint32_t hi, float 
   const pair c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, scale, true);
   return bf16x8_t{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
 }
+// A scale's byte.  Pages that no row sees (missing: the first page's is read in their place; in a tile that starts before the window) may hold any byte, and what is masked has to
+// stay finite beside it: 0 would make a masked score of -inf times 0, 255 a sum of weights of 0 times infinity.
+__device__ __forceinline__ int cache_byte(int byte) { return min(max(byte, 127 - kCacheExp), 127 + kCacheExp); }
 // The bytes of 16 neighbouring slots from token t0 on whose tokens lie in [lo, hi); the others become zero.
 __device__ __forceinline__ u32x4_t keep_tokens(u32x4_t v, int t0, int lo, int hi) {
 #pragma unroll

@@ -105,7 +105,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) sc[nt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q[nt][step], sc[nt][i], 0, 0, 0);
         }
-      const float ck = a.c * pow2_of_byte(k_byte), ev = (float)(v_byte - 127), inv_v = inverse_of_byte(v_byte);
+      const int v_scale = cache_byte(v_byte);
+      const float ck = a.c * pow2_of_byte(cache_byte(k_byte)), ev = (float)(v_scale - 127), inv_v = inverse_of_byte(v_scale);
       const int pv_next = page_of(next_v);
       load_keys(t0 + stride, page_of(next_k));   // (past the end the last page's, never used)
       scale_at = (int64_t)max(pv_next, 0) * a.kv_heads + h;

@@ -44,8 +44,8 @@ __global__ __launch_bounds__(kThreads) void ccq_attention_images_kernel(AttnArgs
   const int64_t k_tile = (int64_t)max(k_page, 0) * a.kv_heads + head, v_tile = (int64_t)max(v_page, 0) * a.kv_heads + head;
   u32x4_t k = *reinterpret_cast<const u32x4_t*>(a.k + ((k_tile << a.page_shift) + ((t0 + t) & in_page)) * D + c * 16);
   u32x4_t v = *reinterpret_cast<const u32x4_t*>(a.v + ((v_tile * D + d) << a.page_shift) + ((t0 + 16 * quarter) & in_page));
-  const float k_scale = pow2_of_byte(a.ks[k_tile]);
-  const int v_byte = a.vs[v_tile];
+  const float k_scale = pow2_of_byte(cache_byte(a.ks[k_tile]));
+  const int v_byte = cache_byte(a.vs[v_tile]);
   if (k_page < 0) k = u32x4_t{0, 0, 0, 0};
   v = keep_tokens(v, t0 + 16 * quarter, v_page < 0 ? 0x7FFFFFFF : first_seen(a, s.old), s.len);
   const int64_t image = ((int64_t)b * a.kv_heads + head) * a.image_tiles + n;
@@ -148,17 +148,18 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       if (p + kAhead < last) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     }
   };
+  bool gone = false;   // whether a page is missing: its scores are masked then, for the sake of queries that hold NaN or infinities
   auto softmax = [&](int n, int slot) {
     const int t0 = from + n * kTile;
     const f32x4_t ev = *reinterpret_cast<const f32x4_t*>(lds + 3 * kImage + slot * 256), inv = *reinterpret_cast<const f32x4_t*>(lds + 3 * kImage + slot * 256 + 16);
     __builtin_amdgcn_sched_barrier(0);
-    if (t0 < all_lo || t0 + kTile > all_hi || t0 + kTile > to) {
+    if (t0 < all_lo || t0 + kTile > all_hi || t0 + kTile > to || gone) {
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int t = t0 + 32 * tt + 16 * (e >> 3) + 8 * h + (e & 7);
-          if (t < lo || t >= hi) sc[tt][e] = -__builtin_inff();
+          if (t < lo || t >= hi || ev[2 * tt + (e >> 3)] == -__builtin_inff()) sc[tt][e] = -__builtin_inff();
         }
     }
     float most[4], top = kLowest;
@@ -205,6 +206,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   if (tiles > 0) {
     copy(0, 0);
     if (1 < tiles) copy(1, 1);
+    // (once, beside the first copies: looked for in each tile's exponents it cost 1.7 % of the whole)
+    for (int i = (from >> a.page_shift) + lane; i <= (to - 1) >> a.page_shift; i += 64) {
+      const int page = a.table[b * a.ld_table + i];
+      gone |= page < 0 || page >= a.pages;
+    }
+    gone = __any(gone);
     wait_loads<0>();
     barrier();
     read_ahead(kValueOperands, 0, 0);
