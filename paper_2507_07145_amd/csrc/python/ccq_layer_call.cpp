@@ -45,6 +45,8 @@ bool here(PyObject* gpu) {
   int overflow = 0;
   return PyLong_Check(gpu) && PyLong_AsLongAndOverflow(gpu, &overflow) == c10::hip::current_device();
 }
+// (what is true without being True, the general path asks for its truth)
+bool is_flag(PyObject* o) { return o == Py_True || o == Py_False; }
 bool is_codes(const at::Tensor* t) { return t->scalar_type() == at::kByte || t->scalar_type() == at::kFloat8_e4m3fn; }
 bool is_scales(const at::Tensor* t) { return t->scalar_type() == at::kByte || t->scalar_type() == at::kFloat8_e8m0fnu; }
 bool rows_like(const at::Tensor* t, const at::Tensor* x) {
@@ -75,7 +77,7 @@ PyObject* call_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   if (n != 7 || !entry.norm || looked_on()) return general();
   const at::Tensor *x = tensor(a[0]), *w = tensor(a[1]), *r = tensor(a[3]), *sum = tensor(a[4]), *y = tensor(a[5]);
-  if (!plain_bf16(x) || !here(x) || !PyFloat_Check(a[2])) return general();
+  if (!plain_bf16(x) || !here(x) || !PyFloat_Check(a[2]) || !is_flag(a[6])) return general();
   const int64_t M = x->size(0), N = x->size(1);
   if (M > INT32_MAX || N > INT32_MAX || N < 1) return general();
   if (a[1] != Py_None && (!w || w->dim() != 1 || w->size(0) != N || w->device() != x->device() || !is_type(w) || (N > 1 && w->stride(0) != 1))) return general();
@@ -225,12 +227,12 @@ PyObject* call_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const at::Tensor *q = tensor(a[4]), *out = tensor(a[8]);
   ccq_heads hq, ho;
   if (!here(a[1]) || !here(a[3]) || !c.p || !b.p || !heads_of(q, b.p->tokens, 0, c.p->head_dim, &hq) || q->size(1) > INT32_MAX) return general();
-  if (!PyFloat_Check(a[5]) || !PyLong_Check(a[6])) return general();
+  if (!PyFloat_Check(a[5]) || !PyLong_Check(a[6]) || !is_flag(a[7])) return general();
   int overflow = 0;
   const long window = PyLong_AsLongAndOverflow(a[6], &overflow);
   if (overflow || window < 0 || window > INT32_MAX) return general();
   if (a[8] != Py_None && !heads_of(out, b.p->tokens, q->size(1), c.p->head_dim, &ho)) return general();
-  ccq_attn at = {(int32_t)q->size(1), a[7] == Py_True ? 1 : 0, (int32_t)window, (float)PyFloat_AS_DOUBLE(a[5])};
+  ccq_attn at = {(int32_t)q->size(1), a[7] == Py_True, (int32_t)window, (float)PyFloat_AS_DOUBLE(a[5])};
   Workspace ws;
   if (a[9] != Py_None && !ws.of(a[9], q)) return general();
   const int64_t need = a[9] == Py_None ? entry.attention_workspace(c.p, b.p, &at) : 0;

@@ -62,3 +62,19 @@ def test_results_on_another_stream_come_from_its_memory():
     assert [_memory_of(t) for t in made] == [s.cuda_stream] * len(made)
     assert _memory_of(layer.rms_norm(x, None)) == torch.cuda.current_stream().cuda_stream
     assert torch.equal(made[1], layer.rms_norm(x, None, rows8=True).codes) and torch.equal(made[8], q) and torch.equal(made[9], layer.rope_table(10, 8))
+
+
+@pytest.mark.parametrize("true,false", [(1, 0), (torch.tensor(True), torch.tensor(False))], ids=["int", "tensor"])
+def test_flags_by_their_truth(true, false):
+    """What is true is true on the native path and the general one, be it True itself or not."""
+    seq = r.Sequences([(5, 90), (1, 40)], 16)
+    cache, batch = r.to_device(r.random_cache(seq, 1, 64, 1)), seq.batch()
+    q = torch.randn(6, 4, 64, generator=r.gen(7)).bfloat16().to(r.DEV)
+    causal, whole = layer.attention(cache, batch, q, causal=True), layer.attention(cache, batch, q, causal=False)
+    assert not torch.equal(causal, whole)
+    x = torch.randn(2, 256, generator=r.gen(2)).bfloat16().to(r.DEV)
+    for kw in ({}, dict(stream=torch.cuda.current_stream())):
+        assert torch.equal(layer.attention(cache, batch, q, causal=true, **kw), causal)
+        assert torch.equal(layer.attention(cache, batch, q, causal=false, **kw), whole)
+        assert torch.equal(layer.rms_norm(x, None, rows8=true, **kw).codes, layer.rms_norm(x, None, rows8=True).codes)
+        assert torch.equal(layer.rms_norm(x, None, rows8=false, **kw), layer.rms_norm(x, None))
