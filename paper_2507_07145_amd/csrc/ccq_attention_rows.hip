@@ -149,6 +149,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     }
   };
   bool gone = false;   // whether a page is missing: its scores are masked then, for the sake of queries that hold NaN or infinities
+  float least = 0.f;   // exponent of values, or less
   auto softmax = [&](int n, int slot) {
     const int t0 = from + n * kTile;
     const f32x4_t ev = *reinterpret_cast<const f32x4_t*>(lds + 3 * kImage + slot * 256), inv = *reinterpret_cast<const f32x4_t*>(lds + 3 * kImage + slot * 256 + 16);
@@ -172,6 +173,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaf(most[i], a.c, ev[i]));
+    least = fminf(fminf(fminf(least, ev[0]), ev[1]), fminf(ev[2], ev[3]));
     top = fmaxf(top, xor32(top));
     if (__any(top > m + kRise)) {
       const float next = top > m + kRise ? top : m;
@@ -246,6 +248,29 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     if (!behind) barrier();
     read_ahead(0, before, slot);
     multiply(zero, values_end, before, slot);
+  }
+  if (__any(least < (float)kTiny)) {   // the sums of weights once more, from the keys of the images as they lie in memory
+    l = 0.f;
+    for (int n = 0; n < tiles; ++n) {
+      const uint8_t* keys = images + (int64_t)n * kImage + key_token * (2 * D);
+      const f32x4_t ev = *reinterpret_cast<const f32x4_t*>(a.image_scales + (image0 + n) * 8);
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        f32x16_t s2;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s2[e] = 0.f;
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+          const u32x4_t key = *reinterpret_cast<const u32x4_t*>(keys + tt * 32 * 2 * D + (((2 * i + h) ^ key_swizzle) * 16));
+          s2 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, key), q[i], s2, 0, 0, 0);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int t = from + n * kTile + 32 * tt + 16 * (e >> 3) + 8 * h + (e & 7);
+          if (t >= lo && t < hi && ev[2 * tt + (e >> 3)] != -__builtin_inff()) l += __builtin_amdgcn_exp2f(fmaf(s2[e], a.c, -m));
+        }
+      }
+    }
   }
 
   // register e of a lane: dimension 8 (e / 4) + 4 h + e % 4 of its tile
