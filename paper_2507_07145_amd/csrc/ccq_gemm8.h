@@ -72,7 +72,14 @@ __device__ __forceinline__ void lds_barrier() {
 // Blocks of 64 mi rows (mi 1, 2, 4) and 256 columns, K in `shares` (more than one: fp32 partial results in a.partial).
 int launch_gemm8_block(const Gemm8Args& a, int mi, int shares, void* stream);
 
-// Tiles of 16 mt rows (mt 1, 2, 3, 4, 6) and 128 columns.
+// Tiles of 16 mt rows (mt 1, 2, 3, 4, 6) and 128 columns.  A workgroup's LDS holds two steps of activations and the row scales of its whole share of K, then its sums.
+constexpr int kMostLds = 160 * 1024;
+constexpr int stream_blocks(int blocks, int shares) { return ((blocks + shares - 1) / shares + 1) & ~1; }   // of a share: even
+constexpr int stream_pitch(int blocks_per_share) { return (blocks_per_share + 7) & ~3; }                    // bytes of a row's scales
+constexpr int64_t stream_lds(int mt, int blocks_per_share) {
+  const int64_t rows = 16 * mt, loop = 2 * rows * 2 * kScaleBlock + rows * stream_pitch(blocks_per_share), sums = 4 * rows * 36 * 4;
+  return loop > sums ? loop : sums;
+}
 int launch_gemm8_stream(const Gemm8Args& a, int mt, int shares, void* stream);
 int launch_gemm8_add(const Gemm8Args& a, int shares, void* stream);   // y = sum of the shares
 

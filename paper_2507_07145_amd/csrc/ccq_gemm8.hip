@@ -189,6 +189,7 @@ Plan8 find_plan(int M, int N, int K, bool wide) {
       if (M > 16 * mt && mt < 4) continue;       // (a tile of all rows, or the larger ones)
       for (const int shares : kShares) {
         if (shares > 1 && shares * 2 > blocks) break;
+        if (stream_lds(mt, stream_blocks(blocks, shares)) > kMostLds) continue;   // (the scales of a long share)
         Plan8 p;
         p.kind = kStream, p.mt = mt, p.shares = shares, p.time = stream_time(mt, shares, M, N, blocks);
         offer(p);

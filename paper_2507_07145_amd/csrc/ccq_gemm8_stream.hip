@@ -44,7 +44,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
 
   // row scales of the share
   uint8_t* scales = lds + 2 * kStage;
-  const int pitch = (p.blocks_per_share + 7) & ~3;
+  const int pitch = stream_pitch(p.blocks_per_share);
   for (int i = threadIdx.x; !WIDE && i < rows * blocks; i += 64 * kWaves) {
     const int r = i / blocks, c = i % blocks;
     scales[r * pitch + c] = a.xs[(int64_t)(m0 + r) * a.ld_xs + first + c];
@@ -201,11 +201,12 @@ __global__ __launch_bounds__(256) void ccq_gemm8_add_kernel(Gemm8Args a, int sha
 template <int MT>
 int launch(const Gemm8Stream& p, hipStream_t s) {
   constexpr int kRows = 16 * MT;
-  const int pitch = (p.blocks_per_share + 7) & ~3, loop = 2 * kRows * kStepK + kRows * pitch, sums = 4 * kRows * 36 * 4, bytes = loop > sums ? loop : sums;
+  const int64_t bytes = stream_lds(MT, p.blocks_per_share);
+  if (bytes > kMostLds) return CCQ_ERR_UNSUPPORTED;
   constexpr bool kWide = MT <= 4;   // (of 96 bf16 rows the registers do not hold three steps)
   if (p.a.x16 && !kWide) return CCQ_ERR_UNSUPPORTED;
   const void* kernel = p.a.x16 ? reinterpret_cast<const void*>(ccq_gemm8_stream_kernel<MT, kWide>) : reinterpret_cast<const void*>(ccq_gemm8_stream_kernel<MT, false>);
-  if (bytes > 64 * 1024 && hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return CCQ_ERR_HIP;
+  if (bytes > 64 * 1024 && hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess) return CCQ_ERR_HIP;
   const dim3 grid((unsigned)(p.n_tiles * p.shares), (unsigned)((p.a.M + kRows - 1) / kRows));
   if (p.a.x16) hipLaunchKernelGGL((ccq_gemm8_stream_kernel<MT, kWide>), grid, dim3(64 * kWaves), (unsigned)bytes, s, p);
   else hipLaunchKernelGGL((ccq_gemm8_stream_kernel<MT, false>), grid, dim3(64 * kWaves), (unsigned)bytes, s, p);
@@ -224,7 +225,7 @@ int launch_gemm8_stream(const Gemm8Args& a, int mt, int shares, void* stream) {
   Gemm8Stream p;
   p.a = a;
   p.n_tiles = (a.N + kCols - 1) / kCols;
-  p.blocks_per_share = ((a.blocks + shares - 1) / shares + 1) & ~1;
+  p.blocks_per_share = stream_blocks(a.blocks, shares);
   p.shares = (a.blocks + p.blocks_per_share - 1) / p.blocks_per_share;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int rc = mt == 1 ? launch<1>(p, s) : mt == 2 ? launch<2>(p, s) : mt == 3 ? launch<3>(p, s) : mt == 4 ? launch<4>(p, s) : launch<6>(p, s);

@@ -78,3 +78,13 @@ def test_flags_by_their_truth(true, false):
         assert torch.equal(layer.attention(cache, batch, q, causal=false, **kw), whole)
         assert torch.equal(layer.rms_norm(x, None, rows8=true, **kw).codes, layer.rms_norm(x, None, rows8=True).codes)
         assert torch.equal(layer.rms_norm(x, None, rows8=false, **kw), layer.rms_norm(x, None))
+
+
+def test_rows_of_four_million_values():
+    """A product whose row scales pass the LDS if the streaming kernel takes it: ones times ones, exact in every order of sums."""
+    K, N = 1 << 22, 2048
+    w = layer.Weight8(torch.full((N, K), 0x38, dtype=torch.uint8, device=r.DEV), torch.ones(N // 128, K // 128, device=r.DEV))   # 0x38 is 1.0
+    for M in (16, 64):
+        rows = layer.Rows8(torch.full((M, K), 0x38, dtype=torch.uint8, device=r.DEV), torch.full((M, K // 128), 127, dtype=torch.uint8, device=r.DEV))
+        assert bool((layer.gemm8(w, rows) == K).all())
+        assert bool((layer.gemm8(w, torch.ones(M, K, dtype=torch.bfloat16, device=r.DEV)) == K).all())
