@@ -109,6 +109,12 @@ def _need(ok: bool, what: str) -> None:
         raise ValueError(what)
 
 
+def _int32(*values: int) -> None:
+    """The entry points take these numbers in 32 bits, and ctypes cuts off what does not fit."""
+    for v in values:
+        _need(-(1 << 31) <= v < 1 << 31, "sizes and counts of up to 31 bits are needed")
+
+
 def _on_this_gpu(*tensors) -> None:
     for t in tensors:
         if t is not None:
@@ -194,6 +200,7 @@ class Weight8:
         _need(scales.dtype == torch.float32 and _rows(scales) and scales.shape == (-(-N // BLOCK), -(-K // BLOCK)) and scales.device == codes.device,
               "8-bit weights: fp32 scales [ceil(N / 128)][ceil(K / 128)] are needed")
         _need(_own_rows(scales), "8-bit weights: rows of scales must not overlap")
+        _int32(N, K)
         self.codes, self.scales, self.gpu = codes, scales, _gpu(codes)
         self.desc = ccq_weight8(K, N, codes.data_ptr(), _ld(codes), scales.data_ptr(), max(scales.stride(0), scales.shape[1]))
 
@@ -216,6 +223,7 @@ class Cache8:
         for s in (k_scales, v_scales):
             _need(_is_scales(s) and s.is_contiguous() and s.shape == (pages, heads), "cache: scales are contiguous bytes [pages][heads]")
         _need(k.device == v.device == k_scales.device == v_scales.device, "cache: all on one device")
+        _int32(pages)
         self.k, self.v, self.k_scales, self.v_scales, self.gpu = k, v, k_scales, v_scales, _gpu(k)
         self.desc = ccq_cache(pages, page_tokens, heads, dim, k.data_ptr(), v.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr())
 
@@ -239,6 +247,7 @@ class Batch:
               "batch: offsets [B + 1] and lens [B] are needed")
         _need(_rows(table) and table.shape[0] == B, "batch: a table [B][pages of a sequence] is needed")
         _need(_own_rows(table), "batch: rows of the table must not overlap")
+        _int32(B, tokens, max_new, max_len, table.shape[1])
         self.offsets, self.lens, self.table, self.gpu = offsets, lens, table, _gpu(lens)
         self.desc = ccq_batch(B, tokens, max_new, max_len, offsets.data_ptr(), lens.data_ptr(), table.data_ptr(), max(table.stride(0), table.shape[1]), table.shape[1])
 
@@ -251,6 +260,7 @@ class Rope:
         _need(table.dtype == torch.float32 and table.is_contiguous() and table.dim() == 2 and table.shape[1] == dims, "rope: a contiguous fp32 table [positions][dims] is needed")
         _need(positions is None or (positions.dtype == torch.int32 and positions.is_contiguous() and positions.dim() == 1 and positions.device == table.device),
               "rope: int32 positions, one per token row, are needed")
+        _int32(table.shape[0], dims)
         self.table, self.positions, self.gpu = table, positions, _gpu(table)
         self.desc = ccq_rope(table.data_ptr(), table.shape[0], dims, int(interleaved), None if positions is None else positions.data_ptr())
 
@@ -263,6 +273,7 @@ def rope_table(rows: int, dims: int, base: float = 10000.0, kind: str = "none", 
     """Cosines and sines of positions 0 .. rows - 1, fp32 [rows][dims], through ccq_rope_table; `kind` is the scaling for contexts longer
     than the trained one: "none", "linear", "base" or "parts"."""
     _need(kind in _KINDS, f"kind is one of {', '.join(_KINDS)}")
+    _int32(rows, dims)
     out = _on(stream, lambda: torch.empty((rows, dims), dtype=torch.float32, device=device))
     s = ccq_rope_scaling(_KINDS[kind], base, factor, original_length, fast, slow, magnitude)
     with torch.cuda.device(out.device):
@@ -288,6 +299,7 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor | None, eps: float = 1e-6, re
     _need(x.dtype == torch.bfloat16 and _rows(x) and x.shape[1] > 0, "x: bf16 rows are needed")
     _on_this_gpu(x, weight, residual, residual_out, out)
     M, N = x.shape
+    _int32(M, N)
     n = ccq_norm(M=M, N=N, eps=eps, x=x.data_ptr(), ldx=_ld(x))
     if weight is not None:
         _need(weight.shape == (N,) and (N == 1 or weight.stride(0) == 1), "weight: one per column is needed")
@@ -319,6 +331,7 @@ def quantize8(x: torch.Tensor, stream=None) -> Rows8:
             return Rows8(*r)
     _need(x.dtype == torch.bfloat16 and _rows(x) and x.shape[1] > 0, "x: bf16 rows are needed")
     _on_this_gpu(x)
+    _int32(*x.shape)
     out = _on(stream, lambda: _new_rows8(*x.shape, x.device))
     d = out.desc()
     _check(_load().ccq_quantize8(_t_ptr(x), _ld(x), x.shape[0], x.shape[1], ctypes.byref(d), _stream_ptr(stream)), "ccq_quantize8")
@@ -336,6 +349,7 @@ def gemm8(w: Weight8, x, out: torch.Tensor | None = None, workspace: torch.Tenso
     held = x.codes if is8 else x
     _on_this_gpu(held, w.codes, out)
     M, N = x.shape[0], w.N
+    _int32(M)
     _need(x.shape[1] == w.K, "x and the weights have another K")
     y = _on(stream, lambda: binding._new_output(M, N, held.device)) if out is None else out
     _need(y.dtype == torch.bfloat16 and y.shape == (M, N) and _rows(y), "out: bf16 rows [M][N] are needed")
@@ -352,6 +366,7 @@ def gemm8(w: Weight8, x, out: torch.Tensor | None = None, workspace: torch.Tenso
 
 
 def gemm8_workspace_bytes(w: Weight8, M: int, bf16_rows: bool = False) -> int:
+    _int32(M)
     f = _load().ccq_gemm8_bf16_workspace_bytes if bf16_rows else _load().ccq_gemm8_workspace_bytes
     need = int(f(ctypes.byref(w.desc), M))
     if need < 0:
@@ -408,6 +423,7 @@ def attention(cache: Cache8, batch: Batch, q: torch.Tensor, scale: float | None 
     hq = _heads(q, T, None, D, "q")
     out = _on(stream, lambda: torch.empty(q.shape, dtype=q.dtype, device=q.device)) if out is None else out
     ho = _heads(out, T, q.shape[1], D, "out")
+    _int32(window, q.shape[1])
     a = ccq_attn(q.shape[1], int(bool(causal)), window, scale)
     if workspace is None:
         need = int(_load().ccq_attention_workspace_bytes(ctypes.byref(cache.desc), ctypes.byref(batch.desc), ctypes.byref(a)))

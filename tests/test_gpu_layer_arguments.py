@@ -88,3 +88,13 @@ def test_rows_of_four_million_values():
         rows = layer.Rows8(torch.full((M, K), 0x38, dtype=torch.uint8, device=r.DEV), torch.full((M, K // 128), 127, dtype=torch.uint8, device=r.DEV))
         assert bool((layer.gemm8(w, rows) == K).all())
         assert bool((layer.gemm8(w, torch.ones(M, K, dtype=torch.bfloat16, device=r.DEV)) == K).all())
+
+
+def test_windows_past_32_bits_are_refused():
+    """Cut off to 32 bits, 2^32 + 5 would be a window of 5."""
+    seq = r.Sequences([(1, 40)], 16)
+    cache, batch, q = r.to_device(r.random_cache(seq, 1, 64, 1)), seq.batch(), torch.zeros(1, 4, 64, dtype=torch.bfloat16, device=r.DEV)
+    for kw in ({}, dict(stream=torch.cuda.current_stream())):
+        with pytest.raises(ValueError, match="31 bits"):
+            layer.attention(cache, batch, q, window=(1 << 32) + 5, **kw)
+        assert layer.attention(cache, batch, q, window=(1 << 31) - 1, **kw).shape == q.shape

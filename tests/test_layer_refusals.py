@@ -49,3 +49,16 @@ def test_workspaces_that_kernels_cannot_write():
             l.binding._given_workspace(ws, like)
     ws = u8(64)
     assert l.binding._given_workspace(ws, u8(1)) is ws
+
+
+def test_numbers_past_32_bits():
+    """ctypes would cut them off: 2^32 + 5 tokens would be 5."""
+    for kw in (dict(tokens=(1 << 32) + 2), dict(max_new=1 << 31), dict(max_len=(1 << 32) + 3), dict(max_len=-(1 << 31) - 1)):
+        with pytest.raises(ValueError, match="31 bits"):
+            l.Batch(i32(3), i32(2), i32(2, 3), **{**dict(tokens=2, max_new=1, max_len=48), **kw})
+    with pytest.raises(ValueError, match="31 bits"):
+        l.rope_table(1 << 32, 2, device="meta")
+    with pytest.raises(ValueError, match="31 bits"):
+        l.Rope(torch.empty((1 << 31, 2), device="meta"))
+    with pytest.raises(ValueError, match="31 bits"):
+        l.Weight8(torch.empty((1, 1 << 31), dtype=torch.uint8, device="meta"), torch.empty((1, 1 << 24), device="meta"))
