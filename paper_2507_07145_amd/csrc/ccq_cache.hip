@@ -28,7 +28,8 @@ struct AppendArgs {
   int32_t rope_rows, dims, interleaved;
   int32_t pages, kv_heads, q_heads, table_width, tokens, max_new, max_len;
   int32_t page_slots;         // pages that the new tokens of a sequence may touch
-  int32_t kv_groups, query_groups, total;   // workgroups of keys (as many of values); a token row's queries; of the launch
+  int32_t kv_groups, query_groups, total;   // workgroups of keys (as many of values); a token row's queries; of the call
+  int32_t first;              // workgroup of the call that is the launch's first
 };
 
 struct Sequence {
@@ -319,7 +320,7 @@ __device__ __forceinline__ void rotate_queries(const AppendArgs& a, int b, int i
 template <int D, int P>
 __global__ __launch_bounds__(256) void ccq_append_kernel(AppendArgs a) {
   __shared__ __align__(16) uint8_t lds[D * (P + 4)];
-  int g = blockIdx.x;
+  int g = a.first + blockIdx.x;
   if (g < 2 * a.kv_groups) {
     const bool keys = g < a.kv_groups;
     if (!keys) g -= a.kv_groups;
@@ -337,10 +338,11 @@ struct TableArgs {
   float* table;
   double base, factor, low, high, magnitude;
   int32_t kind, rows, dims;
+  int64_t first;   // pair of the table that is the launch's first
 };
 __global__ __launch_bounds__(256) void ccq_rope_table_kernel(TableArgs a) {
   const int half = a.dims / 2;
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t at = a.first + (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (at >= (int64_t)a.rows * half) return;
   const int p = (int)(at / half), i = (int)(at % half);
   double f = pow(a.base, -2.0 * i / a.dims);
@@ -357,7 +359,11 @@ __global__ __launch_bounds__(256) void ccq_rope_table_kernel(TableArgs a) {
 
 template <int D, int P>
 void launch(const AppendArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((ccq_append_kernel<D, P>), dim3((unsigned)a.total), dim3(256), 0, s, a);
+  AppendArgs part = a;
+  for (int64_t first = 0; first < a.total; first += most_groups(256)) {
+    part.first = (int)first;
+    hipLaunchKernelGGL((ccq_append_kernel<D, P>), dim3((unsigned)std::min<int64_t>(a.total - first, most_groups(256))), dim3(256), 0, s, part);
+  }
 }
 template <int D>
 int launch_d(const AppendArgs& a, int page_tokens, hipStream_t s) {
@@ -387,8 +393,10 @@ int launch_rope_table(const ccq_rope_scaling* s, int rows, int dims, float* tabl
     a.high = fmin(ceil(scale * log(s->original_length / (turn * s->slow))), dims - 1.0);
   }
   const int64_t blocks = ((int64_t)rows * (dims / 2) + 255) / 256;
-  if (blocks > 0x7FFFFFFF) return CCQ_ERR_BAD_PARAM;
-  hipLaunchKernelGGL(ccq_rope_table_kernel, dim3((unsigned)blocks), dim3(256), 0, static_cast<hipStream_t>(stream), a);
+  for (int64_t first = 0; first < blocks; first += most_groups(256)) {
+    a.first = first * 256;
+    hipLaunchKernelGGL(ccq_rope_table_kernel, dim3((unsigned)std::min(blocks - first, most_groups(256))), dim3(256), 0, static_cast<hipStream_t>(stream), a);
+  }
   return hipGetLastError() == hipSuccess ? CCQ_OK : CCQ_ERR_HIP;
 }
 

@@ -78,6 +78,9 @@ __device__ __forceinline__ void wait_loads() {
   __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4 << 14) | 0x0F70);
 }
 
+// A launch has fewer than 2^32 threads: workgroups of `threads` of one launch; what has more is launched in parts.
+constexpr int64_t most_groups(int threads) { return (int64_t(1) << 31) / threads; }
+
 int launch_norm(const ccq_norm* n, bool norm, void* stream);
 int launch_rope_table(const ccq_rope_scaling* s, int rows, int dims, float* table, void* stream);
 int launch_cache_append(const ccq_cache* c, const ccq_batch* b, const ccq_rope* rope, const ccq_heads* k, const ccq_heads* v, const ccq_heads* q,

@@ -7,6 +7,8 @@
 // four, or sixteen, so that a thread holds at most 32 values of it: eight neighbouring columns at a time (16 bytes of bf16),
 // so that 16 neighbouring lanes hold a scale's block and find its largest magnitude among themselves.
 // 2048 rows of 7168 with a bf16 residual, 8 bits out: 18.7 us, 5.5 TB/s; one row of 8192: 2.9 us, the latency of a launch and two loads.
+#include <type_traits>
+
 #include "ccq_layer.h"
 
 namespace ccq {
@@ -199,12 +201,28 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void ccq_norm_kernel(NormArgs a)
   }
 }
 
+// The same from row `rows` on.
+NormArgs past(NormArgs a, int rows) {
+  auto skip = [&](auto*& p, int64_t ld, int bytes) {
+    if (p) p = reinterpret_cast<std::remove_reference_t<decltype(p)>>((uintptr_t)p + (uintptr_t)(rows * ld * bytes));
+  };
+  const int wide = a.residual_fp32 ? 4 : 2;
+  skip(a.x, a.ldx, 2), skip(a.residual, a.ld_residual, wide), skip(a.sum, a.ld_sum, wide), skip(a.y, a.ldy, 2);
+  skip(a.codes, a.ld_codes, 1), skip(a.scales, a.ld_scales, 1);
+  a.M -= rows;
+  return a;
+}
+
 template <int T, int C>
-void launch(const NormArgs& a, bool norm, hipStream_t s) {
+void launch(const NormArgs& all, bool norm, hipStream_t s) {
   constexpr int kRows = T < 256 ? 256 / T : 1;
+  constexpr int kMost = (int)most_groups(T < 256 ? 256 : T) * kRows;   // rows of a launch
+  NormArgs a = all;
+  a.M = all.M < kMost ? all.M : kMost;
   const dim3 grid((unsigned)((a.M + kRows - 1) / kRows)), block(T < 256 ? 256 : T);
   if (norm) hipLaunchKernelGGL((ccq_norm_kernel<T, C, true>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((ccq_norm_kernel<T, (T * C > 2048 ? 0 : C), false>), grid, block, 0, s, a);   // (long rows: their pieces do not need each other, and with four held at once the compiler spills)
+  if (all.M > kMost) launch<T, C>(past(all, kMost), norm, s);
 }
 
 }  // namespace
