@@ -370,7 +370,7 @@ constexpr int64_t kMostImages = int64_t(4) << 30;   // bytes of workspace; past 
 int64_t image_tiles(const ccq_batch* b, const ccq_attn* at) {   // of a sequence
   return (at->window > 0 ? std::min<int64_t>(b->max_len, (int64_t)at->window + b->max_new) : b->max_len) / kTile + 2;
 }
-int forced = -1;   // (tests: 1 the kernel for many rows, 0 the one for few)
+thread_local int forced = -1;   // (tests: 1 the kernel for many rows, 0 the one for few)
 Plan plan_of(const ccq_cache* c, const ccq_batch* b, const ccq_attn* at) {
   Plan p;
   const int64_t rows = (int64_t)b->max_new * (at->q_heads / c->kv_heads), pairs = (int64_t)b->batch * c->kv_heads;
@@ -462,7 +462,7 @@ int launch_attention(const ccq_cache* c, const ccq_batch* b, const ccq_attn* at,
   return c->head_dim == 64 ? launch_join<64>(a, s) : launch_join<128>(a, s);
 }
 
-// For tests, no part of the interface: all calls from now on take the kernel for many rows (1), the one for few (0), or (-1) what the rule says.
+// For tests, no part of the interface: all calls of this thread from now on take the kernel for many rows (1), the one for few (0), or (-1) what the rule says.
 extern "C" void ccq_attention_force(int32_t kernel) { forced = kernel; }
 
 }  // namespace ccq

@@ -1,4 +1,7 @@
 """Tensors behind the layer operators' descriptors that no kernel may be given.  Host only: nothing is launched."""
+import ctypes
+import threading
+
 import pytest
 import torch
 
@@ -62,3 +65,19 @@ def test_numbers_past_32_bits():
         l.Rope(torch.empty((1 << 31, 2), device="meta"))
     with pytest.raises(ValueError, match="31 bits"):
         l.Weight8(torch.empty((1, 1 << 31), dtype=torch.uint8, device="meta"), torch.empty((1, 1 << 24), device="meta"))
+
+
+def test_a_forced_kernel_is_the_threads_own():
+    """The tests' switch does not reach the calls of other threads."""
+    cache, batch = l.ccq_cache(64, 64, 8, 128, None, None, None, None), l.ccq_batch(1, 2048, 2048, 4096, None, None, None, 64, 64)
+    need = lambda: l._load().ccq_attention_workspace_bytes(ctypes.byref(cache), ctypes.byref(batch), ctypes.byref(l.ccq_attn(56, 1, 0, 1.0)))  # noqa: E731
+    rule, other = need(), []
+    l._load().ccq_attention_force(0)
+    try:
+        assert need() < rule
+        t = threading.Thread(target=lambda: other.append(need()))
+        t.start()
+        t.join()
+    finally:
+        l._load().ccq_attention_force(-1)
+    assert other == [rule]
