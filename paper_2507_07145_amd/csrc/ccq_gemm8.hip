@@ -286,19 +286,32 @@ int launch_gemm8(const ccq_weight8* w, const ccq_rows8* x, int M, void* y, int64
   return run(a, a.ldw > kFarRows || a.ldx > kFarRows ? kFar : plan_of(M, a.N, a.K, false), stream);
 }
 
-// For tests, no part of the interface: how a call of these sizes is served (the numbers of the plan, and the estimate), and a call as a named plan, whose
-// arguments are not checked.
+// For tests, no part of the interface: how a call of these sizes is served (the numbers of the plan, and the estimate).
 extern "C" void ccq_gemm8_plan(int32_t M, int32_t N, int32_t K, int32_t* out, double* time) {
   const Plan8 p = plan_of(M, N, K, false);
   const int v[7] = {p.kind, p.mt, p.shares, p.waves, p.n_rest, p.mt_rest, p.shares_rest};
   for (int i = 0; i < 7; ++i) out[i] = v[i];
   *time = p.time;
 }
-extern "C" int ccq_gemm8_as(const ccq_weight8* w, const ccq_rows8* x, int32_t M, void* y, int64_t ldy, void* workspace, const int32_t* plan, void* stream) {
+
+// Whether there are kernels for a plan, and rows that they reach.
+static bool can_run(const Plan8& p, const Gemm8Args& a) {
+  auto block = [](int mt, int shares) { return (mt == 1 || mt == 2 || mt == 4) && shares >= 1 && shares <= 64; };
+  if (p.n_rest != 0 && (p.kind != kBlock || p.n_rest < 0 || p.n_rest % 256 != 0 || p.n_rest >= a.N || p.shares != 1 || !block(p.mt_rest, p.shares_rest))) return false;
+  if (p.kind == kFew) return p.shares == 1 && (p.mt == 4 ? p.waves == 4 : p.mt == 1 && (p.waves == 4 || p.waves == 16));
+  if (p.kind == kStream)
+    return (p.mt == 6 ? !a.x16 : p.mt >= 1 && p.mt <= 4) && p.shares >= 1 && p.shares <= 64 && stream_lds(p.mt, stream_blocks(a.blocks, p.shares)) <= kMostLds;
+  return p.kind == kBlock && block(p.mt, p.shares) && !a.x16 && a.ldw <= kFarRows && a.ldx <= kFarRows;
+}
+
+// The same: a call as a named plan.  x without scales: bf16 rows.  (`workspace` is as large as the plan's partial results.)
+int launch_gemm8_as(const ccq_weight8* w, const ccq_rows8* x, int M, void* y, int64_t ldy, void* workspace, const int32_t* plan, void* stream) {
   Plan8 p;
   p.kind = plan[0], p.mt = plan[1], p.shares = plan[2], p.waves = plan[3], p.n_rest = plan[4], p.mt_rest = plan[5], p.shares_rest = plan[6];
   Gemm8Args a = args_of(w, x, M, y, ldy, workspace);
-  if (!x->scales) a.x16 = static_cast<const uint16_t*>(x->codes), a.ldx16 = x->ld;   // bf16 rows
+  if (!x->scales) a.x16 = static_cast<const uint16_t*>(x->codes), a.ldx16 = x->ld;
+  if (!can_run(p, a)) return CCQ_ERR_BAD_PARAM;
+  if (workspace_of(p, M, w->N) > 0 && !workspace) return CCQ_ERR_WORKSPACE;
   return run(a, p, stream);
 }
 

@@ -150,6 +150,21 @@ extern "C" int ccq_gemm8_bf16(const ccq_weight8* w, const void* x, int64_t ldx, 
   return launch_gemm8_bf16(w, x, ldx, M, y, ldy, workspace, hip_stream);
 }
 
+// For tests, no part of the interface: ccq_gemm8 (x without scales: ccq_gemm8_bf16) as a named plan.
+extern "C" int ccq_gemm8_as(const ccq_weight8* w, const ccq_rows8* x, int32_t M, void* y, int64_t ldy, void* workspace, const int32_t* plan, void* hip_stream) {
+  if (!x || !plan) return CCQ_ERR_NULL;
+  int rc = check_gemm8(w, M, y, ldy, workspace);
+  if (rc != CCQ_OK || M == 0) return rc;
+  if (x->scales) {
+    if ((rc = check_rows8(*x, w->K)) != CCQ_OK) return rc;
+  } else {
+    if (!x->codes) return CCQ_ERR_NULL;
+    if (x->ld < w->K) return CCQ_ERR_BAD_PARAM;
+    if (off(x->codes, 2)) return CCQ_ERR_ALIGN;
+  }
+  return launch_gemm8_as(w, x, M, y, ldy, workspace, plan, hip_stream);
+}
+
 extern "C" int ccq_rope_table(const ccq_rope_scaling* s, int32_t rows, int32_t dims, float* table, void* hip_stream) {
   if (!s || !table) return CCQ_ERR_NULL;
   if (rows < 0 || dims < 2 || dims % 2 != 0 || s->kind < 0 || s->kind > 3) return CCQ_ERR_BAD_PARAM;

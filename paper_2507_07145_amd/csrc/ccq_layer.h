@@ -90,6 +90,7 @@ int launch_attention(const ccq_cache* c, const ccq_batch* b, const ccq_attn* a, 
 int64_t gemm8_workspace(const ccq_weight8* w, int M);
 int64_t gemm8_bf16_workspace(const ccq_weight8* w, int M);
 int launch_gemm8_bf16(const ccq_weight8* w, const void* x, int64_t ldx, int M, void* y, int64_t ldy, void* workspace, void* stream);
+int launch_gemm8_as(const ccq_weight8* w, const ccq_rows8* x, int M, void* y, int64_t ldy, void* workspace, const int32_t* plan, void* stream);
 int launch_gemm8(const ccq_weight8* w, const ccq_rows8* x, int M, void* y, int64_t ldy, void* workspace, void* stream);
 
 }  // namespace ccq
