@@ -362,7 +362,7 @@ typedef struct {
 typedef struct {
   int32_t batch;           /* sequences; 0 is a no-op                                                    */
   int32_t tokens;          /* token rows of the call                                                     */
-  int32_t max_new;         /* the most new tokens of a sequence                                          */
+  int32_t max_new;         /* the most new tokens of a sequence (attention: max_new x q_heads up to 2^28) */
   int32_t max_len;         /* the greatest length (new tokens included)                                  */
   const int32_t *offsets;  /* DEVICE int32 [batch + 1]                                                   */
   const int32_t *lens;     /* DEVICE int32 [batch]                                                       */

@@ -437,6 +437,8 @@ int64_t attention_workspace(const ccq_cache* c, const ccq_batch* b, const ccq_at
 int launch_attention(const ccq_cache* c, const ccq_batch* b, const ccq_attn* at, const ccq_heads* q, const ccq_heads* out, void* workspace, void* stream) {
   if (b->batch == 0 || b->max_new == 0) return CCQ_OK;
   const Plan p = plan_of(c, b, at);
+  const int threads = p.many ? 2 * kManyRows : 64 * kWaves;
+  if (b->batch > 65535 || (int64_t)c->kv_heads * p.image_tiles > most_groups(threads) || (int64_t)c->kv_heads * p.row_tiles * p.splits > most_groups(threads)) return CCQ_ERR_BAD_PARAM;
   AttnArgs a = {};
   a.k = static_cast<const uint8_t*>(c->k), a.v = static_cast<const uint8_t*>(c->v), a.ks = c->k_scales, a.vs = c->v_scales;
   a.q = static_cast<const uint16_t*>(q->data), a.q_token = q->token_stride, a.q_head = q->head_stride;
@@ -455,7 +457,6 @@ int launch_attention(const ccq_cache* c, const ccq_batch* b, const ccq_attn* at,
     a.image_tiles = p.image_tiles;
     a.image_scales = reinterpret_cast<float*>(a.images + (int64_t)p.image_tiles * b->batch * c->kv_heads * kImageBytes);
   }
-  if ((int64_t)a.kv_heads * a.image_tiles > 0x7FFFFFFF || (int64_t)a.kv_heads * a.row_tiles * a.splits > 0x7FFFFFFF || b->batch > 65535) return CCQ_ERR_BAD_PARAM;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int rc = p.many ? launch_attention_rows(a, stream) : c->head_dim == 64 ? launch_few<64>(a, p, s) : launch_few<128>(a, p, s);
   if (rc != CCQ_OK || p.splits == 1) return rc;

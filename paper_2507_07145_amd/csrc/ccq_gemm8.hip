@@ -93,11 +93,19 @@ Gemm8Args args_of(const ccq_weight8* w, const ccq_rows8* x, int M, void* y, int6
   return a;
 }
 
+// (rows far apart may be many: in parts, for a grid's second dimension ends at 65535)
 template <int MT, int W>
-int launch_few(const Gemm8Args& a, hipStream_t s) {
-  const dim3 grid((unsigned)((a.N + 15) / 16), (unsigned)((a.M + 16 * MT - 1) / (16 * MT)));
-  if (a.x16) hipLaunchKernelGGL((ccq_gemm8_few_kernel<MT, W, true>), grid, dim3(64 * W), 0, s, a);
-  else hipLaunchKernelGGL((ccq_gemm8_few_kernel<MT, W, false>), grid, dim3(64 * W), 0, s, a);
+int launch_few(Gemm8Args a, hipStream_t s) {
+  constexpr int kMost = 65535 * 16 * MT;
+  for (int rows = a.M; rows > 0; rows -= kMost) {
+    a.M = std::min(rows, kMost);
+    const dim3 grid((unsigned)((a.N + 15) / 16), (unsigned)((a.M + 16 * MT - 1) / (16 * MT)));
+    if (a.x16) hipLaunchKernelGGL((ccq_gemm8_few_kernel<MT, W, true>), grid, dim3(64 * W), 0, s, a);
+    else hipLaunchKernelGGL((ccq_gemm8_few_kernel<MT, W, false>), grid, dim3(64 * W), 0, s, a);
+    if (a.x16) a.x16 += (int64_t)kMost * a.ldx16;
+    else a.x += (int64_t)kMost * a.ldx, a.xs += (int64_t)kMost * a.ld_xs;
+    a.y += (int64_t)kMost * a.ldy;
+  }
   return hipGetLastError() == hipSuccess ? CCQ_OK : CCQ_ERR_HIP;
 }
 

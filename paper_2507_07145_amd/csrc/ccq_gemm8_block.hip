@@ -320,6 +320,7 @@ int launch_gemm8_block(const Gemm8Args& a, int mi, int shares, void* stream) {
   p.n_tiles = (a.N + kCols - 1) / kCols;
   p.steps_per_share = (a.blocks + shares - 1) / shares;
   p.shares = (a.blocks + p.steps_per_share - 1) / p.steps_per_share;
+  if ((int64_t)p.m_tiles * p.n_tiles * p.shares > most_groups(64 * kWaves)) return CCQ_ERR_UNSUPPORTED;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int rc = mi == 4 ? launch<4>(p, s) : mi == 2 ? launch<2>(p, s) : launch<1>(p, s);
   if (rc != CCQ_OK) return rc;

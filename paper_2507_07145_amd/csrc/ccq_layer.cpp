@@ -36,6 +36,7 @@ int check_norm(const ccq_norm* n, bool norm) {
   return CCQ_OK;
 }
 
+constexpr int kMostRows = 0x7FFFFF00;   // (rounded up to blocks they stay within 31 bits)
 int check_weight8(const ccq_weight8* w) {
   if (!w) return CCQ_ERR_NULL;
   if (w->K <= 0 || w->N <= 0 || w->K > 0x7FFFFF00 || w->N > 0x7FFFFF00 || w->ldw < w->K || w->ld_scales < blocks_of(w->K)) return CCQ_ERR_BAD_PARAM;
@@ -107,14 +108,14 @@ extern "C" int ccq_quantize8(const void* x, int64_t ldx, int32_t M, int32_t N, c
 }
 
 extern "C" int64_t ccq_gemm8_workspace_bytes(const ccq_weight8* w, int32_t M) {
-  if (check_weight8(w) != CCQ_OK || M < 0) return -1;
+  if (check_weight8(w) != CCQ_OK || M < 0 || M > kMostRows) return -1;
   return gemm8_workspace(w, M);
 }
 
 static int check_gemm8(const ccq_weight8* w, int32_t M, const void* y, int64_t ldy, const void* workspace) {
   const int rc = check_weight8(w);
   if (rc != CCQ_OK) return rc;
-  if (M < 0 || ldy < w->N) return CCQ_ERR_BAD_PARAM;
+  if (M < 0 || M > kMostRows || ldy < w->N) return CCQ_ERR_BAD_PARAM;
   if (ldy % 8 != 0) return CCQ_ERR_ALIGN;
   if (M == 0) return CCQ_OK;
   if (!w->codes || !w->scales || !y) return CCQ_ERR_NULL;
@@ -133,7 +134,7 @@ extern "C" int ccq_gemm8(const ccq_weight8* w, const ccq_rows8* x, int32_t M, vo
 }
 
 extern "C" int64_t ccq_gemm8_bf16_workspace_bytes(const ccq_weight8* w, int32_t M) {
-  if (check_weight8(w) != CCQ_OK || M < 0) return -1;
+  if (check_weight8(w) != CCQ_OK || M < 0 || M > kMostRows) return -1;
   return gemm8_bf16_workspace(w, M);
 }
 

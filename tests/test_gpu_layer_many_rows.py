@@ -44,3 +44,18 @@ def test_append_with_a_bound_on_new_tokens_of_many_workgroups():
     assert torch.equal(got, want)
     for one, other in ((near.k, far.k), (near.v, far.v), (near.k_scales, far.k_scales), (near.v_scales, far.v_scales)):
         assert torch.equal(one, other)
+
+
+def test_many_rows_on_weights_far_apart():
+    """Weights whose rows are 9 MiB apart go to the kernel for few rows, whatever the rows' number: more of them than its grid has."""
+    M, N, K = 65535 * 64 + 77, 16, 48
+    big = torch.zeros(N, 9 << 20, dtype=torch.uint8, device=r.DEV)
+    big[:, :K] = torch.randint(0, 0x60, (N, K), generator=r.gen(0), dtype=torch.uint8).to(r.DEV)
+    far, near = layer.Weight8(big[:, :K], torch.ones(1, 1, device=r.DEV)), layer.Weight8(big[:, :K].contiguous(), torch.ones(1, 1, device=r.DEV))
+    x = torch.randn(1 << 12, K, generator=r.gen(1)).bfloat16().to(r.DEV).repeat(M // (1 << 12) + 1, 1)[:M]
+    want = layer.gemm8(near, x[:1 << 12])
+    for rows in (x, layer.quantize8(x)):
+        y = layer.gemm8(far, rows)
+        for first in (0, 1 << 20, (65535 * 64 >> 12) << 12):
+            n = min(1 << 12, M - first)
+            assert torch.equal(y[first:first + n], want[:n])

@@ -81,3 +81,19 @@ def test_a_forced_kernel_is_the_threads_own():
     finally:
         l._load().ccq_attention_force(-1)
     assert other == [rule]
+
+
+def test_calls_past_what_a_launch_may_have():
+    """2^32 threads and more are refused before the launch."""
+    p = 4096   # a pointer that no call below may look behind
+    cache = l.ccq_cache(4, 16, 2, 64, p, p, p, p)
+    heads = l.ccq_heads(p, 256, 64)
+    a = l.ccq_attn(4, 1, 0, 0.125)
+    for tokens in (1 << 27, (1 << 26) + 64):
+        batch = l.ccq_batch(2, tokens, tokens, 32, p, p, p, 2, 2)
+        assert l._load().ccq_attention(ctypes.byref(cache), ctypes.byref(batch), ctypes.byref(a), ctypes.byref(heads), ctypes.byref(heads), None, 0, None) == -2
+    w = l.ccq_weight8(128, 128, p, 128, p, 1)
+    rows = l.ccq_rows8(p, 128, p, 1)
+    for M in (0x7FFFFFFF, 0x7FFFFF01):
+        assert l._load().ccq_gemm8(ctypes.byref(w), ctypes.byref(rows), M, p, 128, None, 0, None) == -2 and l._load().ccq_gemm8_workspace_bytes(ctypes.byref(w), M) == -1
+        assert l._load().ccq_gemm8_bf16(ctypes.byref(w), p, 128, M, p, 128, p, 1 << 50, None) == -2 and l._load().ccq_gemm8_bf16_workspace_bytes(ctypes.byref(w), M) == -1
