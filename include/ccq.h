@@ -293,8 +293,8 @@ typedef struct {
 typedef enum { CCQ_BF16 = 0, CCQ_FP32 = 1 } ccq_type;
 
 /* h = x + residual;  sum = h;  y = h / sqrt(mean(h^2) + eps) * weight, per row, in fp32 (sums and statistics included; h is not
- * rounded before it is normalised).  Strides are in elements and free (any alignment of rows; multiples of 8 elements on 16-byte
- * aligned arrays are read and written 16 bytes at a time). */
+ * rounded before it is normalised).  Strides are in elements and free; rows may start at any element (eight columns at a time are
+ * read and written in pieces of 16 bytes whatever their address). */
 typedef struct {
   int32_t M, N;            /* M = 0 is a no-op; N >= 1                                                   */
   float eps;               /* >= 0                                                                       */
@@ -311,8 +311,9 @@ typedef struct {
   int64_t ldy;
   ccq_rows8 y8;            /* or codes = NULL.  y, y8 or both                                            */
 } ccq_norm;
-/* A row that holds NaN is NaN in all outputs (in y8: codes and scales).  A row with an infinity is so where h is not finite and
- * zero elsewhere; a block of y8 with a NaN in it has NaN codes and a NaN scale (255). */
+/* A row of h that holds NaN is NaN in all of y and y8 (codes and scales); one with an infinity is so where h is not finite and zero
+ * elsewhere, and so is one whose sum of squares passes fp32's largest number.  A block of y8 with a NaN in it has NaN codes and a NaN scale (255).
+ * `sum` holds h, whatever it is. */
 int ccq_rms_norm(const ccq_norm *n, void *hip_stream);
 
 /* Rows of bf16 [M][ldx] as 8-bit rows: what ccq_rms_norm does to its result.  A block that holds NaN or an infinity becomes NaN
@@ -328,7 +329,9 @@ typedef struct {
   int64_t ld_scales;
 } ccq_weight8;
 
-/* y[m][n] = sum over blocks b of 2^(e[m][b]) s[n / 128][b] sum over k in b of x[m][k] w[n][k], fp32 accumulation.
+/* y[m][n] = sum over blocks b of 2^(e[m][b]) s[n / 128][b] sum over k in b of x[m][k] w[n][k].
+ *   The sums over b are fp32.  Within a block the products are added by the 8-bit matrix instructions, which take groups of eight in units of 2^-13 of
+ *   the group's largest product and drop what is below; the groups are added in fp32.
  *   x: 8-bit rows [M][K]; y DEVICE bf16 [M][ldy], ldy >= N, a multiple of 8; columns N.. of y are not written.
  *   workspace DEVICE, at least ccq_gemm8_workspace_bytes(w, M) bytes (may be NULL if that is 0; -1: invalid arguments).
  *   M = 0 is a no-op. */
@@ -414,7 +417,7 @@ int ccq_cache_append(const ccq_cache *c, const ccq_batch *b, const ccq_rope *rop
 /* out[t][h] = sum over tokens j of softmax_j(scale q[t][h] . k[j][h / g]) v[j][h / g], g = q_heads / kv_heads, over the cached tokens j < lens that
  * the row at position p sees: j <= p when causal, j > p - window when window > 0.  A row that sees none is zero.  Scores, softmax and sums in
  * fp32; the softmax weights enter the second product as fp16, the cached values as they are.  `v` of the tokens that are seen holds no NaN
- * (ccq_cache_append writes none); slots that are not written, and pages outside the window, may hold anything.
+ * (ccq_cache_append writes none); slots that are not written, and pages that no row sees with their scales, may hold anything.
  *   workspace DEVICE, at least ccq_attention_workspace_bytes(...) bytes (may be NULL if that is 0; -1: invalid arguments): partial results where few rows meet
  *   many tokens; for chunks of prompts, heads of 128, four bytes per cached number that max_len and window admit, 4 GiB at most. */
 typedef struct {

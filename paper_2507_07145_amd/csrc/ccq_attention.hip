@@ -8,7 +8,7 @@
 // token after token, are 16-byte loads that need no transposition either.  Nothing passes LDS until the wavefronts' results
 // are joined.  A lane's 16 tokens lie in one page (pages hold multiples of 16): its scales are one value each.
 // Bound by memory: 16 KB a tile (128 dimensions) against 32 MFMAs; keys and scales are asked for a tile ahead, table entries two, values while the scores
-// are formed.  64 sequences of up to 8192 tokens (687 MB): 131 us, 5.2 TB/s; one of 131072 (268 MB): 56 us with the join.
+// are formed.  64 sequences of up to 8192 tokens (687 MB): 130 - 133 us, 5.2 TB/s; one of 131072 (268 MB): 55 - 57 us with the join.
 #include <algorithm>
 
 #include "ccq_attention.h"

@@ -6,7 +6,7 @@
 //   queries of one token row, 16 or 32 heads: rotate.
 // A page's scale depends on nothing but the page's own tokens, so no two workgroups share one.  The values of a page are held
 // in registers between the search for the largest and the writing (eight neighbouring dimensions of a token to a thread).
-// 2048 rows of 56 + 8 heads of 128: 16.2 us, 4.4 TB/s; 64 single tokens of 64 + 8 heads: 6.5 us.  Bound by memory for prompts, by the latency of its dependent loads (lengths, table and positions, values, old scale) for
+// 2048 rows of 56 + 8 heads of 128: 16.2 us, 4.4 TB/s; 64 single tokens of 64 + 8 heads: 6.4 - 6.8 us.  Bound by memory for prompts, by the latency of its dependent loads (lengths, table and positions, values, old scale) for
 // single tokens.
 #include <algorithm>
 
@@ -419,7 +419,8 @@ int launch_cache_append(const ccq_cache* c, const ccq_batch* b, const ccq_rope* 
   const int P = c->page_tokens;
   a.page_slots = (int)(((int64_t)b->max_new + P - 2) / P + 1);
   const int64_t groups = k ? (int64_t)b->batch * a.page_slots * c->kv_heads : 0;
-  // few token rows: a workgroup to every 16 heads (64 rows of 64 heads: 6.3 us, with a workgroup to a row 7.7); many: one to a row (2048 rows of 56: 16.6 us against 22.6)
+  // Few token rows: a workgroup to every 16 heads of 128; many: one to a row.  By workgroups that the first makes, us with it / with one to a row: 32 rows of 64 heads (128 groups) 4.5 / 5.3, 64 of
+  // 64 (256) 6.1 / 7.3, 128 of 128 (1024) 10.8 / 12.1, 256 of 64 (1024) 16.3 / 16.0, 512 of 64 (2048) 7.7 / 7.8, 1024 of 64 (4096) 13.6 / 10.9, 2048 of 64 (8192) 24.3 / 18.1.
   const int64_t rows = (int64_t)b->batch * b->max_new, heads_at_once = c->head_dim == 64 ? kQueryHeads<64> : kQueryHeads<128>;
   const int64_t head_groups = (q_heads + heads_at_once - 1) / heads_at_once;
   a.query_groups = rows * head_groups <= 1024 ? (int)std::max<int64_t>(head_groups, 1) : 1;

@@ -7,7 +7,7 @@
 // is filled again, so that a copy has a step's time to arrive, or two.
 // Products are scaled MFMAs 32x32x64, two for a block of K, into a fresh result that one multiply-add per register adds to the
 // accumulators with the weights' scale.  The vector unit does not reach accumulation registers: 512 registers a wavefront would not help.
-// 2048 rows, 8192 x 8192 (a block to each CU): 120 us, 2.3 PFLOP/s; 18432 x 7168: 276 us, 1.96.  Bound by the way into and out of LDS (64 KB in, 192 KB out a step) and by
+// 2048 rows, 8192 x 8192 (a block to each CU): 133 us, 2.1 PFLOP/s; 18432 x 7168: 276 - 290 us, 1.9.  Bound by the way into and out of LDS (64 KB in, 192 KB out a step) and by
 // power; on 2048 x 16384 x 7168 an earlier form with 262 us took 190 without the copies, 231 with copies that all read one address, no less without
 // waiting for them.
 #include <algorithm>
@@ -194,7 +194,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     lds_barrier();
     __builtin_amdgcn_sched_barrier(0);
     // A wavefront that issues copies waits for the path to LDS, which they keep busy for half a step.  In the largest blocks all eight copy, some before each of
-    // the last two products, and the others' products go on meanwhile (2048 x 18432 x 7168: 318 us, with one wavefront of a SIMD that copies in turn 340); in
+    // the last two products, and the others' products go on meanwhile (2048 x 18432 x 7168, when it was tried, before other steps: 318 us, with one wavefront of a SIMD that copies in turn 340); in
     // smaller ones the barriers lie too close for that, and in turn is faster (256 x 8192 x 8192 in blocks of 128 rows: 74 us against 84).
     if constexpr (decltype(AHEAD)::value && MI < 4) {
       if (turn) {

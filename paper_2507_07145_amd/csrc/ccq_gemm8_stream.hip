@@ -5,7 +5,7 @@
 // LDS, asked for as far ahead as the weights (mixed with copies that pass by the registers the compiler's waits would be for all loads); every
 // wavefront asks for its 4 KB of weights two or three steps ahead, straight into registers: no
 // other wavefront of the workgroup needs them.  Bound by memory: the weights' bytes.  64 rows, 28672 x 8192: 57 us, 4.1 TB/s; 37 rows, 5001 x 7184, six
-// shares: 15.5 us, 3.7 of them for the join (40 blocks of columns alone would leave most of the chip idle).
+// shares: 12.4 - 13.8 us and 3 - 4 for the join (40 blocks of columns alone would leave most of the chip idle).
 #include <type_traits>
 
 #include "ccq_gemm8.h"

@@ -6,7 +6,7 @@
 // Bound by memory: every value is read once and written once, the row lies in registers in between.  A row has a wavefront,
 // four, or sixteen, so that a thread holds at most 32 values of it: eight neighbouring columns at a time (16 bytes of bf16),
 // so that 16 neighbouring lanes hold a scale's block and find its largest magnitude among themselves.
-// 2048 rows of 7168 with a bf16 residual, 8 bits out: 18.7 us, 5.5 TB/s; one row of 8192: 2.9 us, the latency of a launch and two loads.
+// 2048 rows of 7168 with a bf16 residual, 8 bits out: 18 - 20 us, 5.2 - 5.7 TB/s; one row of 8192: 2.9 us, the latency of a launch and two loads.
 #include <type_traits>
 
 #include "ccq_layer.h"
@@ -243,7 +243,12 @@ int launch_norm(const ccq_norm* n, bool norm, void* stream) {
   a.residual_fp32 = n->residual_type == CCQ_FP32, a.weight_fp32 = n->weight_type == CCQ_FP32;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int N = n->N;
-  // few rows leave the chip empty: as many threads to a row as it has pieces of eight columns
+  // Few rows leave the chip empty: as many threads to a row as it has pieces of eight columns.  Many: fewer threads, which hold more of it.  On the GPU, with a residual, us:
+  //   rows x columns      1 x 512    1 x 1024   4096 x 1024   1 x 2048   512 x 2048   4096 x 2048 | 1 x 4096   1 x 8192   256 x 8192   1024 x 8192   4096 x 4096
+  //   64 threads          2.3        3.0        6.2           4.2        5.2          11.0        |
+  //   256                 2.4        2.5        7.6           2.5        3.4          12.0        | 2.9        4.3        5.6          10.6          21.2
+  //   1024                2.7        2.8        20.6          2.8        4.5          21.3        | 2.8        3.0        4.4          13.0          23.7
+  // (The lines lie where most sizes change sides; 512 to 1024 rows of 1024 to 2048 would be faster with 256 threads still.)
   const bool few = n->M < 512;
   if (N <= 512) launch<64, 1>(a, norm, s);
   else if (N <= 2048 && !few) N <= 1024 ? launch<64, 2>(a, norm, s) : launch<64, 4>(a, norm, s);

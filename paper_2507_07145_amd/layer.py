@@ -9,6 +9,9 @@
 
 Argument marshalling only, as in binding.py (include/ccq.h says what each call computes): a native module
 (csrc/python/ccq_layer_call.cpp) takes the plain cases with little host time, ctypes the others, which are checked and reported here.
+
+Weight8, Cache8, Batch and Rope hold tensors of one GPU, and calls are made with that GPU current.  With stream= the work is enqueued there; results that are
+made lie in that stream's memory, and the current stream has to wait for it before it reads them.
 """
 from __future__ import annotations
 
