@@ -103,6 +103,17 @@ __device__ __forceinline__ bf16x8_t values_bf16(uint32_t lo, uint32_t hi, float 
 // A scale's byte.  Pages that no row sees (missing: the first page's is read in their place; in a tile that starts before the window) may hold any byte, and what is masked has to
 // stay finite beside it: 0 would make a masked score of -inf times 0, 255 a sum of weights of 0 times infinity.
 __device__ __forceinline__ int cache_byte(int byte) { return min(max(byte, 127 - kCacheExp), 127 + kCacheExp); }
+// Whether one of the pages of tokens [from, to) has tiny values (kTiny): looked at where a kernel met a small exponent, which may be that of a page no row sees.
+__device__ __forceinline__ bool tiny_pages(const AttnArgs& a, int b, int head, int lane, int from, int to) {
+  bool tiny = false;
+  for (int i = (from >> a.page_shift) + lane; i <= (to - 1) >> a.page_shift; i += 64) {
+    const int page = a.table[b * a.ld_table + i];
+    if (page < 0 || page >= a.pages) continue;
+    const int byte = a.vs[(int64_t)page * a.kv_heads + head];
+    tiny |= byte >= 127 - kCacheExp && byte < 127 + kTiny;
+  }
+  return __any(tiny);
+}
 // The bytes of 16 neighbouring slots from token t0 on whose tokens lie in [lo, hi); the others become zero.
 __device__ __forceinline__ u32x4_t keep_tokens(u32x4_t v, int t0, int lo, int hi) {
 #pragma unroll

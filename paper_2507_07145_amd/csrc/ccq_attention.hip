@@ -33,6 +33,7 @@ __device__ __forceinline__ void weights_again(float* stats) {
   const AttnSequence s = attn_sequence(a, b);
   const AttnTile t = attn_tile(a, s, tile * (16 * NT), 16 * NT);
   const int from = t.begin + split * t.chunk, to = from + min(t.chunk, t.any_hi - from), in_page = (1 << a.page_shift) - 1;
+  if (!tiny_pages(a, b, h, lane, from, to)) return;
   const int32_t* pages = a.table + b * a.ld_table;
   for (int nt = 0; nt < NT; ++nt) {
     const int row = min(t.first_row + nt * 16 + r16, t.last_row), token = row / a.group;

@@ -154,7 +154,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     const int t0 = from + n * kTile;
     const f32x4_t ev = *reinterpret_cast<const f32x4_t*>(lds + 3 * kImage + slot * 256), inv = *reinterpret_cast<const f32x4_t*>(lds + 3 * kImage + slot * 256 + 16);
     __builtin_amdgcn_sched_barrier(0);
-    if (t0 < all_lo || t0 + kTile > all_hi || t0 + kTile > to || gone) {
+    bool masked = t0 < all_lo || t0 + kTile > all_hi || t0 + kTile > to;
+    if (gone) masked |= __any(fminf(fminf(ev[0], ev[1]), fminf(ev[2], ev[3])) == -__builtin_inff());
+    if (masked) {
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
@@ -208,7 +210,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   if (tiles > 0) {
     copy(0, 0);
     if (1 < tiles) copy(1, 1);
-    // (once, beside the first copies: looked for in each tile's exponents it cost 1.7 % of the whole)
+    // (once, beside the first copies: looked for in each tile's exponents alone it cost 1.7 % of the whole)
     for (int i = (from >> a.page_shift) + lane; i <= (to - 1) >> a.page_shift; i += 64) {
       const int page = a.table[b * a.ld_table + i];
       gone |= page < 0 || page >= a.pages;
@@ -249,7 +251,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     read_ahead(0, before, slot);
     multiply(zero, values_end, before, slot);
   }
-  if (__any(least < (float)kTiny)) {   // the sums of weights once more, from the keys of the images as they lie in memory
+  if (__any(least < (float)kTiny) && tiny_pages(a, b, head, lane, from, to)) {   // the sums of weights once more, from the keys of the images as they lie in memory
     l = 0.f;
     for (int n = 0; n < tiles; ++n) {
       const uint8_t* keys = images + (int64_t)n * kImage + key_token * (2 * D);
