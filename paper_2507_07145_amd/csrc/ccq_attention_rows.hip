@@ -7,7 +7,7 @@
 // As in the kernel for few rows, tokens are dealt to the first product's rows so that a lane's scores lie in the order in which the second product wants
 // its operand: the weights stay in registers.  Scales of values and pages that are not there enter as the exponent added to a score
 // (-inf for the latter).  Only tiles that not all of a wavefront's rows see whole are masked.
-// A tile costs a wavefront 32 MFMAs (1024 cycles) and 1065 cycles of vector instructions (32 scores a lane: largest, multiply-add, exp2, sum, fp16).  Left to
+// A tile costs a wavefront 32 MFMAs (1024 cycles) and 1070 cycles of vector instructions (32 scores a lane: largest, multiply-add, exp2, sum, fp16).  Left to
 // themselves the two wavefronts of a SIMD do the same at the same time; so the second four are half a tile behind: while one multiplies (values of the last
 // tile, keys of this one, operands read eight products ahead) the other has its softmax.  One barrier a tile holds them there (two, one a half: 4 % slower).  The
 // weights are pinned to their half, or the compiler moves the exp2 behind the barrier.  Images go to LDS by buffer loads: with global ones to LDS under way the compiler
