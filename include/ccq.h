@@ -430,6 +430,102 @@ int64_t ccq_attention_workspace_bytes(const ccq_cache *c, const ccq_batch *b, co
 int ccq_attention(const ccq_cache *c, const ccq_batch *b, const ccq_attn *a, const ccq_heads *q, const ccq_heads *out, void *workspace,
                   int64_t workspace_bytes, void *hip_stream);
 
+/* ---- Rows that choose their weights ---------------------------------------------------------------------------------------------------
+ *
+ * What stands around products whose rows go to weights of their own: a router's choice of experts with the order of rows that ccq_grouped_gemm
+ * reads, the weighted sum of the experts' rows behind it, and low-rank adapters of a batch's requests beside a projection that all share.  The conventions
+ * above hold.  Device data are not read back; what they may hold is said at each call, and ids, places and rows outside their range are left
+ * out, never followed. */
+
+/* The entries (t, j) of ids [T][k], sorted by id, then t, then j; those whose id is none of the call's experts come after all others. */
+typedef struct {
+  int32_t *rows;      /* DEVICE [T k], 16-byte aligned: the t of each entry                                */
+  int32_t *experts;   /* DEVICE [T k]: its id - first, -1 where it is none; or NULL                        */
+  int32_t *offsets;   /* DEVICE [experts + 1], 16-byte aligned: where each expert's entries begin; the last: how many entries have an expert */
+  int32_t *places;    /* DEVICE [T][k]: where entry (t, j) went, -1 where its id is none; or NULL          */
+} ccq_order;
+
+/* The order of ids DEVICE int32 [T][k], rows ld_ids >= k apart, over the experts first .. first + experts - 1 (first >= 0, experts 1 .. 4096):
+ * other ids, such as -1, are none of them.  T k up to 2^30.  With T = 0 the offsets are set to 0.
+ *   `rows` and `offsets` are the sorted_rows and expert_offsets_dev of ccq_grouped_gemm with P = T k and no host copy; where entries have no expert it
+ *   leaves out the rows of y from offsets[experts] on.
+ *   workspace DEVICE, at least ccq_sort_rows_workspace_bytes(...) bytes (may be NULL if that is 0; -1: invalid arguments). */
+int64_t ccq_sort_rows_workspace_bytes(int32_t T, int32_t k, int32_t experts);
+int ccq_sort_rows(const int32_t *ids, int64_t ld_ids, int32_t T, int32_t k, int32_t first, int32_t experts, const ccq_order *order, void *workspace,
+                  int64_t workspace_bytes, void *hip_stream);
+
+typedef enum { CCQ_SOFTMAX = 0, CCQ_SIGMOID = 1 } ccq_scoring;
+
+/* A router's choice.  Expert e is open to row t unless logits[t][e] or bias[e] is NaN or -infinity.
+ *   score[t][e]: exp(logit - top) / sum of the row's exp(logit - top), top its largest logit (infinite ones share it evenly; NaN and -infinity count as 0), or
+ *   1 / (1 + exp(-logit)).
+ *   An expert is chosen by score + bias; without a bias by its logit, which has the scores' order.  With groups > 1 (of experts / groups neighbours)
+ *   only the top_groups of largest value stay, a group's value being the sum of the group_best largest score + bias of its open experts (of those there are).
+ *   ids[t]: the top_k open experts with the largest, the largest first; equal ones by the lower index first, groups too.
+ *   weights[t][j]: the chosen expert's score, divided by the sum of the row's chosen scores with `renormalize` (0 where that sum is 0), times scale.
+ *   A row with fewer open experts than top_k has id -1 and weight 0 in the places left.
+ * Scores, sums and comparisons in 64 bits, weights rounded once. */
+typedef struct {
+  int32_t T, experts;       /* T = 0: only an order's offsets are written; experts 1 .. 1024                 */
+  int32_t top_k;            /* 1 .. 32, at most top_groups * experts / groups                            */
+  int32_t scoring;          /* ccq_scoring                                                               */
+  int32_t groups;           /* 1, or a divisor of experts                                                */
+  int32_t top_groups;       /* 1 .. groups                                                               */
+  int32_t group_best;       /* 1 or 2                                                                    */
+  int32_t renormalize;
+  float scale;              /* finite                                                                    */
+  const void *logits;       /* DEVICE [T][ld] of logits_type                                             */
+  int64_t ld;               /* >= experts                                                                */
+  int32_t logits_type;      /* ccq_type                                                                  */
+  const float *bias;        /* DEVICE [experts], or NULL                                                 */
+  int32_t *ids;             /* DEVICE [T][top_k]                                                         */
+  float *weights;           /* DEVICE [T][top_k]                                                         */
+} ccq_router;
+/* order: of the chosen ids (first = 0), or NULL.  workspace: as for ccq_sort_rows, ccq_route_workspace_bytes (0 without an order). */
+int64_t ccq_route_workspace_bytes(const ccq_router *r, int32_t with_order);
+int ccq_route(const ccq_router *r, const ccq_order *order, void *workspace, int64_t workspace_bytes, void *hip_stream);
+
+/* y[t] = base[t] + sum over j of weights[t][j] rows[places[t][j]], in fp32 in this order (each product and sum fused), rounded once; places outside 0 .. P - 1 and
+ * their weights are left out.  Strides are in elements and free; rows may start at any element. */
+typedef struct {
+  int32_t T, k, N;          /* T = 0 is a no-op; k, N >= 1                                               */
+  int32_t P;                /* rows there are                                                            */
+  const void *rows;         /* DEVICE bf16 [P][ld_rows]                                                  */
+  int64_t ld_rows;
+  const int32_t *places;    /* DEVICE [T][ld_places]                                                     */
+  int64_t ld_places;
+  const float *weights;     /* DEVICE [T][ld_weights]                                                    */
+  int64_t ld_weights;
+  const void *base;         /* DEVICE [T][ld_base] of base_type, or NULL (zeros)                         */
+  int64_t ld_base;
+  int32_t base_type;        /* ccq_type                                                                  */
+  void *y;                  /* DEVICE [T][ldy] of y_type; may be base (with the same type and stride)    */
+  int64_t ldy;
+  int32_t y_type;           /* ccq_type                                                                  */
+} ccq_combination;
+int ccq_combine(const ccq_combination *c, void *hip_stream);
+
+/* Low-rank adapters: `count` pairs of matrices beside one projection [N][K]. */
+typedef struct {
+  int32_t count;            /* >= 1                                                                      */
+  int32_t rank;             /* a multiple of 8, up to 256: what the arrays have room for                 */
+  int32_t K, N;             /* K a multiple of 8                                                         */
+  const void *a;            /* DEVICE bf16 [count][rank][K], 16-byte aligned                             */
+  const void *b;            /* DEVICE bf16 [count][N][rank], 16-byte aligned                             */
+  const float *scales;      /* DEVICE [count], or NULL (ones)                                            */
+  const int32_t *ranks;     /* DEVICE [count], 0 .. rank: the ranks in use (what lies behind them in a and b may hold anything), or NULL (rank) */
+} ccq_adapter_set;
+
+/* out[t] = y[t] + scales[i] (x[t] a[i]^T) b[i]^T for rows t with adapter i; the others' out is y.  Sums in fp32 and rounded to bf16 once; x a^T enters the second
+ * product as the sum of two bf16 numbers, within 2^-15 of it.
+ *   rows, experts DEVICE int32 [T]: the order of ids [T][1] (ccq_sort_rows with experts = count), one for all projections of a step.  Each t stands
+ *   in `rows` once; any order is right, rows of one adapter side by side are fast.  An adapter outside 0 .. count - 1 is none.
+ *   x DEVICE bf16 [T][ldx], y and out DEVICE bf16 [T][ldy], [T][ld_out]: strides in elements and free, rows may start at any element; out may be y (with the same stride).
+ *   T = 0 is a no-op.  workspace DEVICE, 16-byte aligned, at least ccq_adapters_workspace_bytes(set, T) bytes (-1: invalid arguments). */
+int64_t ccq_adapters_workspace_bytes(const ccq_adapter_set *set, int32_t T);
+int ccq_adapters(const ccq_adapter_set *set, int32_t T, const int32_t *rows, const int32_t *experts, const void *x, int64_t ldx, const void *y, int64_t ldy,
+                 void *out, int64_t ld_out, void *workspace, int64_t workspace_bytes, void *hip_stream);
+
 /* Human-readable name of a status code. */
 const char *ccq_status_string(int status);
 

@@ -68,7 +68,9 @@ EXPORTS = ["ccq_pack_info", "ccq_pack_codes", "ccq_pack_scales", "ccq_pack_scale
            "ccq_gemm_static", "ccq_gemm_static_max_workspace", "ccq_pack_device",
            # the layer operators (layer.py)
            "ccq_rms_norm", "ccq_quantize8", "ccq_gemm8", "ccq_gemm8_workspace_bytes", "ccq_gemm8_bf16", "ccq_gemm8_bf16_workspace_bytes", "ccq_rope_table", "ccq_cache_append", "ccq_attention",
-           "ccq_attention_workspace_bytes"]
+           "ccq_attention_workspace_bytes",
+           # rows that choose their weights (routing.py)
+           "ccq_sort_rows", "ccq_sort_rows_workspace_bytes", "ccq_route", "ccq_route_workspace_bytes", "ccq_combine", "ccq_adapters", "ccq_adapters_workspace_bytes"]
 
 _lib = None
 

@@ -1,8 +1,9 @@
 """Builds libccq.so (the C-ABI library: HIP kernels for gfx950 + host layer) in-tree with hipcc.
 
 Every source under csrc/ is compiled to an object file of its own (in parallel) and the objects are linked
-into paper_2507_07145_amd/libccq.so; csrc/python/ccq_call.cpp and ccq_layer_call.cpp, the host paths of the binding's
-multiply calls and of the layer operators, become the Python modules paper_2507_07145_amd/_ccq_call.so and _ccq_layer.so next to it.  `python -m paper_2507_07145_amd.build --incremental` recompiles only the
+into paper_2507_07145_amd/libccq.so; csrc/python/ccq_call.cpp, ccq_layer_call.cpp and ccq_routing_call.cpp, the host paths of the
+binding's multiply calls, of the layer operators and of routing.py's, become the Python modules paper_2507_07145_amd/_ccq_call.so, _ccq_layer.so and
+_ccq_routing.so next to it.  `python -m paper_2507_07145_amd.build --incremental` recompiles only the
 sources that are newer than their objects (headers count for every source).
 """
 from __future__ import annotations
@@ -20,7 +21,8 @@ ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libccq.so")
 CALL_DIR = os.path.join(HERE, "csrc", "python")
 CALL_MODULES = [(os.path.join(CALL_DIR, "ccq_call.cpp"), os.path.join(HERE, "_ccq_call.so")),
-                (os.path.join(CALL_DIR, "ccq_layer_call.cpp"), os.path.join(HERE, "_ccq_layer.so"))]
+                (os.path.join(CALL_DIR, "ccq_layer_call.cpp"), os.path.join(HERE, "_ccq_layer.so")),
+                (os.path.join(CALL_DIR, "ccq_routing_call.cpp"), os.path.join(HERE, "_ccq_routing.so"))]
 OBJ_DIR = os.path.join(HERE, "_build")
 ARCH = "gfx950"
 
@@ -61,7 +63,7 @@ def call_module_command(src: str, out: str) -> list[str]:
 
 
 def build_lib(verbose: bool = False, incremental: bool = False) -> str:
-    """Compile every source under csrc/ and link paper_2507_07145_amd/libccq.so, _ccq_call.so and _ccq_layer.so."""
+    """Compile every source under csrc/ and link paper_2507_07145_amd/libccq.so, _ccq_call.so, _ccq_layer.so and _ccq_routing.so."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     os.makedirs(OBJ_DIR, exist_ok=True)
     newest_header = max(os.path.getmtime(h) for h in headers())

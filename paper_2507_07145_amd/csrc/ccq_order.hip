@@ -1,0 +1,77 @@
+// The order of ids by expert (ccq_order.h has the sort): one workgroup for few entries, else one launch that counts each workgroup's share and
+// one that places it.
+#include "ccq_order.h"
+
+namespace ccq {
+
+namespace {
+
+struct FromIds {
+  const int32_t* ids;
+  int64_t ld;
+  int k, first, E;
+  __device__ __forceinline__ uint32_t operator()(int i) const {
+    const int t = i / k;
+    const int32_t id = ids[(int64_t)t * ld + (i - t * k)];
+    return id >= first && id - first < E ? (uint32_t)(id - first) : (uint32_t)E;
+  }
+};
+
+__global__ __launch_bounds__(1024) void ccq_sort_count_kernel(SortArgs a) {
+  extern __shared__ uint32_t lds[];
+  const int E1 = a.E + 1;
+  for (int x = threadIdx.x; x < E1; x += blockDim.x) lds[x] = 0;
+  __syncthreads();
+  const int64_t begin = (int64_t)blockIdx.x * a.chunk;
+  const int end = (int)min(begin + a.chunk, (int64_t)a.P);
+  const FromIds expert{a.ids, a.ld_ids, a.k, a.first, a.E};
+  for (int64_t i = begin + threadIdx.x; i < end; i += blockDim.x) atomicAdd(lds + expert((int)i), 1u);
+  __syncthreads();
+  for (int x = threadIdx.x; x < E1; x += blockDim.x) a.counts[(int64_t)blockIdx.x * E1 + x] = lds[x];
+}
+
+__global__ __launch_bounds__(1024) void ccq_sort_kernel(SortArgs a) {
+  extern __shared__ uint32_t lds[];
+  const int64_t begin = (int64_t)blockIdx.x * a.chunk;
+  const int end = (int)min(begin + a.chunk, (int64_t)a.P);
+  sort_entries(a, lds, blockDim.x >> 6, (int)begin, end, FromIds{a.ids, a.ld_ids, a.k, a.first, a.E}, gridDim.x > 1 ? a.counts : nullptr, blockIdx.x, gridDim.x);
+}
+
+constexpr int kChunk = 2048, kMostBlocks = 64;
+
+int blocks_of(int64_t P) {
+  const int64_t n = (P + kChunk - 1) / kChunk;
+  return (int)(n < 1 ? 1 : n > kMostBlocks ? kMostBlocks : n);
+}
+
+// As many wavefronts as have their counters in 56 KB of LDS.
+int waves_of(int E) {
+  int waves = 16;
+  while (waves > 1 && sort_words(waves, E) * 4 > 56 * 1024) waves /= 2;
+  return waves;
+}
+
+}  // namespace
+
+int64_t sort_workspace(int T, int k, int experts) {
+  const int blocks = blocks_of((int64_t)T * k);
+  return blocks > 1 ? (int64_t)blocks * (experts + 1) * 4 : 0;
+}
+
+int launch_sort(const int32_t* ids, int64_t ld_ids, int T, int k, int first, int experts, const ccq_order* order, void* workspace, void* stream) {
+  SortArgs a;
+  a.ids = ids, a.ld_ids = ld_ids;
+  a.counts = static_cast<uint32_t*>(workspace);
+  a.rows = order->rows, a.experts = order->experts, a.offsets = order->offsets, a.places = order->places;
+  a.P = T * k, a.k = k, a.first = first, a.E = experts;
+  const int blocks = blocks_of(a.P), waves = waves_of(experts);
+  a.chunk = (int)(((int64_t)a.P + blocks - 1) / blocks);
+  a.stretch = (int)((((int64_t)a.chunk + waves - 1) / waves + 63) / 64 * 64);
+  a.bits = bits_of(experts);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (blocks > 1) hipLaunchKernelGGL(ccq_sort_count_kernel, dim3(blocks), dim3(1024), (size_t)(experts + 1) * 4, s, a);
+  hipLaunchKernelGGL(ccq_sort_kernel, dim3(blocks), dim3(waves * 64), (size_t)sort_words(waves, experts) * 4, s, a);
+  return hipGetLastError() == hipSuccess ? CCQ_OK : CCQ_ERR_HIP;
+}
+
+}  // namespace ccq

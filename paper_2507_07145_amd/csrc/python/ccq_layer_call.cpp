@@ -1,8 +1,7 @@
 // The host path of the functions of layer.py: as ccq_call.cpp for the multiply calls, with the same answers: outputs, a
 // negative ccq_status as an int, or None for arguments that the general path has to look at.
-#include <c10/hip/HIPFunctions.h>
-
 #include "call.h"
+#include "descriptor.h"
 
 namespace {
 
@@ -18,35 +17,6 @@ struct Entry {
   decltype(&ccq_attention_workspace_bytes) attention_workspace = nullptr;
 } entry;
 
-// A ctypes structure of the binding.
-template <typename T>
-class Struct {
- public:
-  explicit Struct(PyObject* o) {
-    held_ = PyObject_GetBuffer(o, &view_, PyBUF_SIMPLE) == 0;
-    if (!held_) PyErr_Clear();
-    else if (view_.len == (Py_ssize_t)sizeof(T)) p = static_cast<const T*>(view_.buf);
-  }
-  ~Struct() {
-    if (held_) PyBuffer_Release(&view_);
-  }
-  Struct(const Struct&) = delete;
-  Struct& operator=(const Struct&) = delete;
-  const T* p = nullptr;
-
- private:
-  Py_buffer view_;
-  bool held_ = false;
-};
-
-bool here(const at::Tensor* t) { return t->is_cuda() && t->device().index() == c10::hip::current_device(); }
-// The GPU that a descriptor's memory is on, as its object has it.
-bool here(PyObject* gpu) {
-  int overflow = 0;
-  return PyLong_Check(gpu) && PyLong_AsLongAndOverflow(gpu, &overflow) == c10::hip::current_device();
-}
-// (what is true without being True, the general path asks for its truth)
-bool is_flag(PyObject* o) { return o == Py_True || o == Py_False; }
 bool is_codes(const at::Tensor* t) { return t->scalar_type() == at::kByte || t->scalar_type() == at::kFloat8_e4m3fn; }
 bool is_scales(const at::Tensor* t) { return t->scalar_type() == at::kByte || t->scalar_type() == at::kFloat8_e8m0fnu; }
 bool rows_like(const at::Tensor* t, const at::Tensor* x) {
