@@ -21,6 +21,7 @@ struct AdapterArgs {
   const int32_t *ranks, *rows, *experts;
   float* v;               // [splits][T][padded rank]
   int64_t ldx, ldy, ld_out, block0;
+  uint32_t blocks;        // of the launch
   int32_t T, K, N, rank, count, padded;
   int32_t together;       // runs of a block that have a workgroup of their own at the same time
   int32_t splits, steps;  // workgroups along K, steps of 32 columns of each
@@ -58,93 +59,106 @@ struct Runs {
 
 __device__ __forceinline__ int rank_of(const AdapterArgs& a, int i) { return a.ranks ? min(max(a.ranks[i], 0), a.rank) : a.rank; }
 
-constexpr int kDownWaves = 8, kAhead = 4;
+// Rows of 128 columns in LDS: 16 pieces of 16 bytes, piece c of row r in place c ^ (r & 15), so that eight rows' reads of one piece meet all banks.
+constexpr int kStageColumns = 128, kStageRow = 256;
+__device__ __forceinline__ uint32_t staged(int row, int piece) { return (uint32_t)(row * kStageRow + ((piece ^ (row & 15)) * 16)); }
 
+// Both operands go through LDS in stages of 128 columns: a matrix operand read from memory directly has its lanes 16 rows apart, a cache line each, which
+// the card's address units take at a quarter of their rate.  Threads hold two stages more, or four, in registers; wavefront w multiplies columns 32 w .. of each
+// stage, the wavefronts' sums are added at the end.
 template <int RT, int TT>
-__global__ __launch_bounds__(64 * kDownWaves) void ccq_adapter_down_kernel(AdapterArgs a) {
-  __shared__ __align__(16) f32x4_t sums[kDownWaves][RT * TT][64];
+__global__ __launch_bounds__(256, RT == 8 ? 2 : 3) void ccq_adapter_down_kernel(AdapterArgs a) {
+  extern __shared__ __align__(256) uint8_t lds[];
+  constexpr int kStage = (RT + TT) * 16 * kStageRow;
   uint32_t g = blockIdx.x;
   const int split = g % a.splits;
   g /= a.splits;
   const int r0 = (int)(g % a.chunks) * 16 * RT;
   g /= a.chunks;
+  const uint32_t later = g / a.blocks, turn = a.together - 1 - later;   // (the runs that few blocks have first: begun last, they would run alone)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i16 = lane & 15, quarter = lane >> 4;
-  const int64_t p0 = (a.block0 + g / a.together) * 16 * TT;
+  const int64_t p0 = (a.block0 + (g - later * a.blocks)) * 16 * TT;
   Runs runs(a, p0, 16 * TT);
-  runs.skip((int)(g % a.together));
+  runs.skip((int)turn);
   if (!runs.starts) return;
+  const int my_row = threadIdx.x >> 4, piece = threadIdx.x & 15;   // rows my_row + 16 j of the stage
   const uint16_t* xr[TT];
 #pragma unroll
-  for (int u = 0; u < TT; ++u) {
-    const int64_t p = p0 + 16 * u + i16;
-    const int t = p < a.T ? a.rows[p] : 0;
-    xr[u] = a.x + ((uint32_t)t < (uint32_t)a.T ? t : 0) * a.ldx + 8 * quarter;   // (rows that are none: their columns of the product are not stored)
+  for (int j = 0; j < TT; ++j) {
+    const int64_t p = p0 + 16 * j + my_row;
+    const int t = p < a.T ? a.rows[p] : -1;
+    xr[j] = (uint32_t)t < (uint32_t)a.T ? a.x + t * a.ldx + 8 * piece : nullptr;
   }
-  const int all = (a.K + 31) / 32;
-  const int step0 = min(split * a.steps, all), step1 = min(step0 + a.steps, all);
-  const int per = (step1 - step0 + kDownWaves - 1) / kDownWaves;
-  const int from = min(step0 + wave * per, step1), to = min(from + per, step1);
+  const int all = (a.K + kStageColumns - 1) / kStageColumns;
+  const int from = min(split * a.steps, all), to = min(from + a.steps, all);
+  const uint32_t write_at = staged(my_row, piece), read_at = staged(i16, 4 * wave + quarter);
   for (; runs.starts; runs.skip(a.together)) {
     const int first = runs.first(), end = runs.end();
     const int i = __builtin_amdgcn_readfirstlane(__shfl(runs.adapter, first));
     if (i < 0) continue;
     const int rank = rank_of(a, i);
     if (r0 >= rank) continue;
-    const uint16_t* ar[RT];
+    const uint16_t* const ar = a.a + ((int64_t)i * a.rank + r0 + my_row) * a.K + 8 * piece;
+    // (rows of other runs and ranks not in use are not read: what LDS holds for them reaches no sum that is kept)
+    auto load = [&](int step, u32x4_t (&x)[TT], u32x4_t (&w)[RT]) {
+      const int k = step * kStageColumns;
+      const bool in = k + 8 * piece < a.K;
 #pragma unroll
-    for (int u = 0; u < RT; ++u) ar[u] = a.a + ((int64_t)i * a.rank + min(r0 + 16 * u + i16, rank - 1)) * a.K + 8 * quarter;   // (past the rank its last row again)
+      for (int j = 0; j < TT; ++j) {
+        x[j] = u32x4_t{0, 0, 0, 0};
+        const int row = 16 * j + my_row;
+        if (in && row >= first && row < end && xr[j]) __builtin_memcpy(&x[j], xr[j] + k, 16);
+      }
+#pragma unroll
+      for (int j = 0; j < RT; ++j) {
+        w[j] = u32x4_t{0, 0, 0, 0};
+        if (in && r0 + 16 * j + my_row < rank) w[j] = *reinterpret_cast<const u32x4_t*>(ar + (int64_t)16 * j * a.K + k);
+      }
+    };
     f32x4_t acc[RT][TT];
 #pragma unroll
     for (int u = 0; u < RT; ++u)
 #pragma unroll
       for (int w = 0; w < TT; ++w) acc[u][w] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    const int whole = min(to, a.K / 32);
-    int step = from;
-    auto steps = [&](auto n) {
-      constexpr int kSteps = decltype(n)::value;
-      u32x4_t xa[kSteps][TT], aa[kSteps][RT];
+    constexpr int kDepth = RT * TT <= 2 ? 4 : 2;   // stages asked for ahead
+    u32x4_t x[kDepth][TT], w[kDepth][RT];
+    auto stage = [&](int s, int d) {
+      uint8_t* const to_lds = lds + ((s - from) & 1) * kStage;
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) {
+      for (int j = 0; j < TT; ++j) *reinterpret_cast<u32x4_t*>(to_lds + write_at + j * 16 * kStageRow) = x[d][j];
 #pragma unroll
-        for (int w = 0; w < TT; ++w) __builtin_memcpy(&xa[s][w], xr[w] + (int64_t)(step + s) * 32, 16);
-#pragma unroll
-        for (int u = 0; u < RT; ++u) aa[s][u] = *reinterpret_cast<const u32x4_t*>(ar[u] + (int64_t)(step + s) * 32);
-      }
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s)
-#pragma unroll
-        for (int u = 0; u < RT; ++u)
-#pragma unroll
-          for (int w = 0; w < TT; ++w) acc[u][w] = mfma(aa[s][u], xa[s][w], acc[u][w]);
-      step += kSteps;
-    };
-    while (step + kAhead <= whole) steps(std::integral_constant<int, kAhead>());
-    while (step < whole) steps(std::integral_constant<int, 1>());
-    if (step < to) {   // the last columns: K is a multiple of 8
-      const bool in = step * 32 + 8 * quarter < a.K;
+      for (int j = 0; j < RT; ++j) *reinterpret_cast<u32x4_t*>(to_lds + write_at + (TT + j) * 16 * kStageRow) = w[d][j];
+      if (s + kDepth < to) load(s + kDepth, x[d], w[d]);
+      __syncthreads();
       u32x4_t xa[TT];
 #pragma unroll
-      for (int w = 0; w < TT; ++w) {
-        xa[w] = u32x4_t{0, 0, 0, 0};
-        if (in) __builtin_memcpy(&xa[w], xr[w] + (int64_t)step * 32, 16);
-      }
+      for (int j = 0; j < TT; ++j) xa[j] = *reinterpret_cast<const u32x4_t*>(to_lds + read_at + j * 16 * kStageRow);
 #pragma unroll
       for (int u = 0; u < RT; ++u) {
-        u32x4_t aa = {0, 0, 0, 0};
-        if (in) aa = *reinterpret_cast<const u32x4_t*>(ar[u] + (int64_t)step * 32);
+        const u32x4_t wa = *reinterpret_cast<const u32x4_t*>(to_lds + read_at + (TT + u) * 16 * kStageRow);
 #pragma unroll
-        for (int w = 0; w < TT; ++w) acc[u][w] = mfma(aa, xa[w], acc[u][w]);
+        for (int j = 0; j < TT; ++j) acc[u][j] = mfma(wa, xa[j], acc[u][j]);
       }
+    };
+#pragma unroll
+    for (int d = 0; d < kDepth; ++d)
+      if (from + d < to) load(from + d, x[d], w[d]);
+    for (int s = from; s < to; s += kDepth) {
+#pragma unroll
+      for (int d = 0; d < kDepth; ++d)
+        if (s + d < to) stage(s + d, d);
     }
+    __syncthreads();
+    f32x4_t* const sums = reinterpret_cast<f32x4_t*>(lds);   // [4][RT TT][64]
 #pragma unroll
     for (int u = 0; u < RT; ++u)
 #pragma unroll
-      for (int w = 0; w < TT; ++w) sums[wave][u * TT + w][lane] = acc[u][w];
+      for (int w = 0; w < TT; ++w) sums[(wave * RT * TT + u * TT + w) * 64 + lane] = acc[u][w];
     __syncthreads();
-    for (int c = wave; c < RT * TT; c += kDownWaves) {
-      f32x4_t sum = sums[0][c][lane];
+    for (int c = wave; c < RT * TT; c += 4) {
+      f32x4_t sum = sums[c * 64 + lane];
 #pragma unroll
-      for (int w = 1; w < kDownWaves; ++w) sum += sums[w][c][lane];
+      for (int w = 1; w < 4; ++w) sum += sums[(w * RT * TT + c) * 64 + lane];
       const int u = c / TT, row = 16 * (c % TT) + i16, r = r0 + 16 * u + 4 * quarter;
       if (row >= first && row < end && r < a.padded) *reinterpret_cast<f32x4_t*>(a.v + ((int64_t)split * a.T + p0 + row) * a.padded + r) = sum;
     }
@@ -152,129 +166,356 @@ __global__ __launch_bounds__(64 * kDownWaves) void ccq_adapter_down_kernel(Adapt
   }
 }
 
-// KK: steps of 32 ranks.
+template <int RT, int TT>
+constexpr int down_lds() {
+  const int stages = 2 * (RT + TT) * 16 * kStageRow, sums = 4 * RT * TT * 1024;
+  return stages > sums ? stages : sums;
+}
+
+// Two neighbouring ranks of a row of v, summed over the workgroups first, first + step, ... of those that shared K.
+typedef __attribute__((ext_vector_type(2))) float f32x2_t;
+__device__ __forceinline__ f32x2_t sum_parts(const AdapterArgs& a, const float* from, int first, int step) {
+  constexpr int kTogether = 8;   // asked for at once: their latency is what a short call waits for
+  f32x2_t v = {0.f, 0.f};
+  for (int s0 = first; s0 < a.splits; s0 += kTogether * step) {
+    f32x2_t part[kTogether];
+#pragma unroll
+    for (int s = 0; s < kTogether; ++s) {
+      part[s] = f32x2_t{0.f, 0.f};
+      if (s0 + s * step < a.splits) part[s] = *reinterpret_cast<const f32x2_t*>(from + (int64_t)(s0 + s * step) * a.T * a.padded);
+    }
+#pragma unroll
+    for (int s = 0; s < kTogether; ++s) v.x += part[s].x, v.y += part[s].y;
+  }
+  return v;
+}
+// As two bf16 numbers each: their upper bits and what is left.
+__device__ __forceinline__ u32x2_t in_two(f32x2_t v) {
+  const float v0 = v.x, v1 = v.y;
+  const uint32_t top0 = __builtin_bit_cast(uint32_t, v0) & 0xFFFF0000u, top1 = __builtin_bit_cast(uint32_t, v1) & 0xFFFF0000u;
+  const float up0 = __builtin_bit_cast(float, top0), up1 = __builtin_bit_cast(float, top1);
+  const float rest0 = up0 == v0 ? 0.f : v0 - up0, rest1 = up1 == v1 ? 0.f : v1 - up1;   // (infinity less infinity would be NaN)
+  return u32x2_t{top1 | top0 >> 16, pack_bf16(rest0, rest1)};
+}
+
+// The rows [first, end) of a block, which have no adapter or one without ranks: out is y.  `waves` wavefronts of a workgroup, columns n_first .. n_end - 1.
+__device__ __forceinline__ void copy_rows(const AdapterArgs& a, int64_t p0, int first, int end, int n_first, int n_end, int wave, int waves, int lane) {
+#pragma unroll 1
+  for (int row = first + wave; row < end; row += waves) {
+    const int t = a.rows[p0 + row];
+    if ((uint32_t)t >= (uint32_t)a.T) continue;
+    const uint16_t* from = a.y + t * a.ldy;
+    uint16_t* to = a.out + t * a.ld_out;
+#pragma unroll 1
+    for (int n = n_first + 8 * lane; n < n_end; n += 512) {
+      if (n + 8 <= a.N) {
+        u32x4_t v;
+        __builtin_memcpy(&v, from + n, 16);
+        __builtin_memcpy(to + n, &v, 16);
+      } else {
+#pragma unroll 1
+        for (int h = n; h < a.N; ++h) to[h] = from[h];
+      }
+    }
+  }
+}
+
+// Sum of v over the G lanes of a row of B, in all of them.
+template <int G>
+__device__ __forceinline__ float over_row(float v) {
+  auto moved = [](float x, auto ctrl) { return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xF, 0xF, false)); };
+  if constexpr (G > 1) v += moved(v, std::integral_constant<int, 0xB1>());    // lane l ^ 1
+  if constexpr (G > 2) v += moved(v, std::integral_constant<int, 0x4E>());    // l ^ 2
+  if constexpr (G > 4) v += moved(v, std::integral_constant<int, 0x141>());   // the other four of eight
+  if constexpr (G > 8) v += moved(v, std::integral_constant<int, 0x140>());   // the other eight of 16
+  if constexpr (G > 16) v += xor16(v);
+  return v;
+}
+
+// The second kernel for runs of few rows: B is read along its memory, 16 bytes a lane, G lanes to a row (8 G >= rank), and each lane multiplies its eight ranks by
+// those of up to four rows of v, which it holds in registers.  No matrix operand is put together and nothing goes through LDS but v, once.
+constexpr int kFewRows = 16;   // of a block
+template <int G>
+__global__ __launch_bounds__(256) void ccq_adapter_few_kernel(AdapterArgs a) {
+  constexpr int kLoads = G < 8 ? G : 8, kRowsOfB = 64 / G, kColumns = kLoads * kRowsOfB, kWide = 8 * G;   // of a step of a wavefront
+  __shared__ __align__(16) float v[kFewRows * kWide];
+  __shared__ f32x2_t shares[256];
+  uint32_t g = blockIdx.x;
+  const int n_first = (int)((g % a.chunks) * (int64_t)a.columns);
+  g /= a.chunks;
+  const uint32_t later = g / a.blocks, turn = a.together - 1 - later;
+  const int64_t p0 = (a.block0 + (g - later * a.blocks)) * kFewRows;
+  const int row_of_lane = (threadIdx.x & 63) < kFewRows && p0 + (threadIdx.x & 63) < a.T ? a.rows[p0 + (threadIdx.x & 63)] : -1;   // (asked for together with the adapters)
+  Runs runs(a, p0, kFewRows);
+  runs.skip((int)turn);
+  if (!runs.starts) return;
+  const int n_end = (int)min(n_first + (int64_t)a.columns, (int64_t)a.N), tid = threadIdx.x, pieces = a.rank / 8;
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), piece = lane % G, sub = lane / G;
+  for (; runs.starts; runs.skip(a.together)) {
+    const int first = runs.first(), end = runs.end();
+    const int i = __builtin_amdgcn_readfirstlane(__shfl(runs.adapter, first));
+    if (i < 0) {
+      if (a.copies) copy_rows(a, p0, first, end, n_first, n_end, wave, 4, lane);
+      continue;
+    }
+    const int rank = rank_of(a, i);
+    if (rank == 0) {
+      if (a.copies) copy_rows(a, p0, first, end, n_first, n_end, wave, 4, lane);
+      continue;
+    }
+    // Of four rows from row0 on: a step's B and y.  (Past N the last column is read again, and not stored; pieces past the rank are masked.)
+    int t[4];
+    auto take_rows = [&](int row0) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        t[j] = row0 + j < end ? __builtin_amdgcn_readlane(row_of_lane, row0 + j) : -1;
+        if ((uint32_t)t[j] >= (uint32_t)a.T) t[j] = -1;
+      }
+    };
+    const uint16_t* const b_all = a.b + (int64_t)i * a.N * a.rank + 8 * min(piece, pieces - 1);
+    auto load = [&](int n, u32x4_t (&b)[kLoads], uint16_t (&y)[4]) {
+#pragma unroll
+      for (int c = 0; c < kLoads; ++c) b[c] = *reinterpret_cast<const u32x4_t*>(b_all + (int64_t)min(n + c * kRowsOfB + sub, a.N - 1) * a.rank);
+      const int column = min(n + piece * kRowsOfB + sub, a.N - 1);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y[j] = t[j] >= 0 ? a.y[t[j] * a.ldy + column] : 0;
+    };
+    const int n_mine = n_first + wave * kColumns;
+    u32x4_t b[kLoads], next[kLoads];
+    uint16_t y[4], y_next[4];
+    take_rows(first);
+    load(n_mine, next, y_next);   // (asked for before v is there)
+    u32x4_t mask;
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      const int r = 8 * piece + 2 * h;
+      mask[h] = (r < rank ? 0xFFFFu : 0u) | (r + 1 < rank ? 0xFFFF0000u : 0u);
+    }
+    // v: pairs of ranks of each row, the workgroups that shared K among as many threads as there are for each pair
+    const float scale = a.scales ? a.scales[i] : 1.f;
+    const int rows = end - first, pairs = rows * (kWide / 2), sharing = max(1, 256 / pairs);
+#pragma unroll 1
+    for (int c0 = 0; c0 < pairs; c0 += 256) {
+      const int c = c0 + tid % min(pairs, 256), share = tid / min(pairs, 256), row = c / (kWide / 2), r = c % (kWide / 2) * 2;
+      f32x2_t two = {0.f, 0.f};
+      if (c < pairs && share < sharing && r < rank) two = sum_parts(a, a.v + (p0 + first + row) * a.padded + r, share, sharing);
+      if (sharing > 1) {
+        shares[tid] = two;
+        __syncthreads();
+        if (tid < pairs)
+          for (int s = 1; s < sharing; ++s) two.x += shares[s * pairs + tid].x, two.y += shares[s * pairs + tid].y;
+      }
+      if (c < pairs && share == 0) *reinterpret_cast<f32x2_t*>(v + row * kWide + r) = f32x2_t{r < rank ? two.x * scale : 0.f, r + 1 < rank ? two.y * scale : 0.f};
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int row0 = first; row0 < end; row0 += 4) {
+      f32x4_t w[4][2];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int row = min(row0 + j, end - 1) - first;
+        w[j][0] = *reinterpret_cast<const f32x4_t*>(v + row * kWide + 8 * piece);
+        w[j][1] = *reinterpret_cast<const f32x4_t*>(v + row * kWide + 8 * piece + 4);
+      }
+      if (row0 > first) {
+        take_rows(row0);
+        load(n_mine, next, y_next);
+      }
+#pragma unroll 1
+      for (int n = n_mine; n < n_end; n += 4 * kColumns) {
+#pragma unroll
+        for (int c = 0; c < kLoads; ++c) b[c] = next[c];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[j] = y_next[j];
+        if (n + 4 * kColumns < n_end) load(n + 4 * kColumns, next, y_next);
+        const int column = n + piece * kRowsOfB + sub;   // whose sum this lane keeps
+        const bool keeps = piece < kLoads && column < n_end;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < kLoads; ++c) {
+          float x[8];
+          const u32x4_t bits = b[c] & mask;
+#pragma unroll
+          for (int h = 0; h < 4; ++h) x[2 * h] = bf16_lo(bits[h]), x[2 * h + 1] = bf16_hi(bits[h]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            if (row0 + j >= end) continue;
+            float d = 0.f;
+#pragma unroll
+            for (int h = 0; h < 8; ++h) d = __builtin_fmaf(x[h], w[j][h >> 2][h & 3], d);
+            d = over_row<G>(d);
+            sum[j] = piece == c ? d : sum[j];
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (keeps && t[j] >= 0) a.out[t[j] * a.ld_out + column] = to_bf16(bf16_lo(y[j]) + sum[j]);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// Columns of a piece of the second kernel, and pieces of 16 bytes between its rows of B in LDS: an odd number, so that eight rows' reads meet all banks.
+constexpr int kRowFloats = 4;   // between a row's results in LDS and the next one's, for the same reason
+constexpr int kUpWaves = 8;
+constexpr int piece_columns(int kk) { return kk <= 2 ? 256 : 128; }
+__host__ __device__ constexpr int b_pitch(int rank) { return (rank / 8 | 1) * 16; }
 template <int KK, int TT>
-__global__ __launch_bounds__(256) void ccq_adapter_up_kernel(AdapterArgs a) {
-  __shared__ __align__(16) u32x4_t parts[2][TT * KK][64];   // v as matrix operands: its upper and its lower bits
+constexpr int up_lds(int rank) {
+  return 2 * TT * KK * 1024 + 16 * TT * (piece_columns(KK) + kRowFloats) * 4 + piece_columns(KK) * b_pitch(rank);
+}
+
+// KK: steps of 32 ranks.  A workgroup takes its columns in pieces; B and y of the next piece are asked for while one is worked on.  B goes through LDS for the
+// reason given above, the products go through LDS to meet y, and y and out are read and written along their rows.
+template <int KK, int TT>
+__global__ __launch_bounds__(64 * kUpWaves, 4) void ccq_adapter_up_kernel(AdapterArgs a) {
+  extern __shared__ __align__(256) uint8_t lds[];
+  constexpr int kThreads = 64 * kUpWaves, kColumns = piece_columns(KK), kTiles = kColumns / (16 * kUpWaves);   // of 16 columns for each wavefront
+  constexpr int kPitch = kColumns + kRowFloats;
+  constexpr int kRowPieces = kColumns / 8, kRowsAtOnce = kThreads / kRowPieces, kMyRows = 16 * TT < kRowsAtOnce ? 1 : 16 * TT / kRowsAtOnce;
+  constexpr int kMyB = kColumns * KK * 4 / kThreads;   // pieces of 16 bytes of B, at most
+  u32x4_t* const parts = reinterpret_cast<u32x4_t*>(lds);                                   // [2][TT KK][64]: v as matrix operands, its upper and its lower bits
+  float* const products = reinterpret_cast<float*>(lds + 2 * TT * KK * 1024);              // [16 TT][kPitch]
+  uint8_t* const b_lds = lds + 2 * TT * KK * 1024 + 16 * TT * kPitch * 4;
   uint32_t g = blockIdx.x;
   const int64_t n_first = (int64_t)(g % a.chunks) * a.columns;
   g /= a.chunks;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i16 = lane & 15, quarter = lane >> 4;
-  const int64_t p0 = (a.block0 + g / a.together) * 16 * TT;
+  const uint32_t later = g / a.blocks, turn = a.together - 1 - later;   // (the runs that few blocks have first: begun last, they would run alone)
+  const int64_t p0 = (a.block0 + (g - later * a.blocks)) * 16 * TT;
   Runs runs(a, p0, 16 * TT);
-  runs.skip((int)(g % a.together));
+  runs.skip((int)turn);
   if (!runs.starts) return;
-  int64_t t[TT];
-#pragma unroll
-  for (int w = 0; w < TT; ++w) {
-    const int64_t p = p0 + 16 * w + i16;
-    const int row = p < a.T ? a.rows[p] : -1;
-    t[w] = (uint32_t)row < (uint32_t)a.T ? row : -1;
-  }
+  const int pitch = b_pitch(a.rank), row_pieces = a.rank / 8;
   const int n_end = (int)min(n_first + a.columns, (int64_t)a.N);
   for (; runs.starts; runs.skip(a.together)) {
     const int first = runs.first(), end = runs.end();
     const int i = __builtin_amdgcn_readfirstlane(__shfl(runs.adapter, first));
     const int rank = i < 0 ? 0 : rank_of(a, i);
-    if (rank == 0 && !a.copies) continue;
-    const int last = (rank - 1) >> 5;   // (arithmetic: -1 without ranks)
-    if (rank > 0) {
-      const float scale = a.scales ? a.scales[i] : 1.f;
-      for (int c = wave; c < TT * KK; c += 4) {
-        const int row = 16 * (c / KK) + i16, r = 32 * (c % KK) + 8 * quarter;
-        f32x4_t v0 = {0.f, 0.f, 0.f, 0.f}, v1 = v0;
-        if (row >= first && row < end && r < rank) {
-          const float* from = a.v + (p0 + row) * a.padded + r;
-          for (int s = 0; s < a.splits; ++s, from += (int64_t)a.T * a.padded) {
-            v0 += *reinterpret_cast<const f32x4_t*>(from);
-            v1 += *reinterpret_cast<const f32x4_t*>(from + 4);
-          }
-        }
-        u32x4_t hi, lo;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          uint32_t h = 0, l = 0;
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            const int at = 2 * j + half;
-            float v = (at < 4 ? v0[at & 3] : v1[at & 3]) * scale;
-            if (r + at >= rank) v = 0.f;
-            const uint32_t top = __builtin_bit_cast(uint32_t, v) & 0xFFFF0000u;
-            const float top_v = __builtin_bit_cast(float, top), rest = top_v == v ? 0.f : v - top_v;   // (infinity less infinity would be NaN)
-            h |= half ? top : top >> 16;
-            l |= (uint32_t)to_bf16(rest) << (16 * half);
-          }
-          hi[j] = h, lo[j] = l;
-        }
-        parts[0][c][lane] = hi;
-        parts[1][c][lane] = lo;
-      }
+    int thread = threadIdx.x;
+    asm volatile("" : "+v"(thread));   // (what follows from it is formed in the run, not kept in registers over all of them)
+    const int lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6), i16 = lane & 15, quarter = lane >> 4;
+    if (rank == 0) {   // out is y
+      if (a.copies) copy_rows(a, p0, first, end, (int)n_first, n_end, wave, kUpWaves, lane);
+      continue;
     }
-    __syncthreads();
-    u32x4_t v[2][TT][KK];
+    const int last = (rank - 1) >> 5;
+    const int column = thread % kRowPieces * 8, row0 = thread / kRowPieces;   // this thread's part of y and out: rows row0 + kRowsAtOnce j
+    int t[kMyRows];
+    bool mine[kMyRows];   // rows of this run
 #pragma unroll
-    for (int w = 0; w < TT; ++w)
+    for (int j = 0; j < kMyRows; ++j) {
+      const int row = row0 + kRowsAtOnce * j;
+      const int at = row >= first && row < end ? a.rows[p0 + row] : -1;
+      mine[j] = (uint32_t)at < (uint32_t)a.T;
+      t[j] = at;
+    }
+
+    u32x4_t b[kMyB], y[kMyRows], y_next[kMyRows];
+    const uint16_t* const b_all = a.b + (int64_t)i * a.N * a.rank;
+    const int b_row = thread / row_pieces, b_piece = thread - b_row * row_pieces, rows_on = kThreads / row_pieces, pieces_on = kThreads - rows_on * row_pieces;
+    // f(j, row, piece) for this thread's pieces of B
+    auto my_b = [&](auto f) {
+      int row = b_row, c = b_piece;
 #pragma unroll
-      for (int k = 0; k < KK; ++k) {
-        v[0][w][k] = parts[0][w * KK + k][lane];
-        v[1][w][k] = parts[1][w * KK + k][lane];
+      for (int j = 0; j < kMyB; ++j) {
+        f(j, row, c);
+        row += rows_on, c += pieces_on;
+        if (c >= row_pieces) c -= row_pieces, ++row;
       }
+    };
+    // (past the piece, N and the ranks in use the last ones are read again: they are in the caches, and no sum that is kept meets them)
+    const int top_piece = (rank - 1) >> 3;
+    auto load_b = [&](int n0) {
+      const int top_row = min(kColumns, a.N - n0) - 1;
+      const uint16_t* const from = b_all + (int64_t)n0 * a.rank;
+      my_b([&](int j, int row, int c) { b[j] = *reinterpret_cast<const u32x4_t*>(from + (uint32_t)(min(row, top_row) * a.rank + 8 * min(c, top_piece))); });
+    };
+    auto load_y = [&](int n0) {
+      const int n = n0 + column;
+#pragma unroll
+      for (int j = 0; j < kMyRows; ++j)
+        if (mine[j] && n + 8 <= a.N) y_next[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(a.y + (int64_t)t[j] * a.ldy + n));
+    };
+    auto store = [&](int n0) {
+      const int n = n0 + column;
+#pragma unroll
+      for (int j = 0; j < kMyRows; ++j) {
+        if (!mine[j] || n >= a.N) continue;
+        const float* d = products + (row0 + kRowsAtOnce * j) * kPitch + column;
+        uint16_t* o = a.out + (int64_t)t[j] * a.ld_out + n;
+        if (n + 8 <= a.N) {
+          const f32x4_t d0 = *reinterpret_cast<const f32x4_t*>(d), d1 = *reinterpret_cast<const f32x4_t*>(d + 4);
+#pragma unroll
+          for (int h = 0; h < 4; ++h)
+            y[j][h] = pack_bf16(bf16_lo(y[j][h]) + (h < 2 ? d0[2 * h] : d1[2 * h - 4]), bf16_hi(y[j][h]) + (h < 2 ? d0[2 * h + 1] : d1[2 * h - 3]));
+          __builtin_nontemporal_store(y[j], reinterpret_cast<u32x4_t*>(o));
+        } else {   // the last columns
+          const uint16_t* from = a.y + (int64_t)t[j] * a.ldy + n;
+#pragma unroll 1
+          for (int h = 0; h < a.N - n; ++h) o[h] = to_bf16(bf16_lo(from[h]) + d[h]);
+        }
+      }
+    };
+    load_b((int)n_first);   // (asked for before v is there)
+    load_y((int)n_first);
+
+    const float scale = a.scales ? a.scales[i] : 1.f;
+#pragma unroll 1
+    for (int c = thread; c < TT * KK * 256; c += kThreads) {   // rows, and 16 KK pairs of ranks of each
+      const int row = c / (16 * KK), r = c % (16 * KK) * 2;
+      f32x2_t two = {0.f, 0.f};
+      if (row >= first && row < end && r < rank) two = sum_parts(a, a.v + (p0 + row) * a.padded + r, 0, 1);
+      two.x *= scale, two.y = r + 1 < rank ? two.y * scale : 0.f;
+      const u32x2_t halves = in_two(two);
+      const int at = (row / 16 * KK + r / 32) * 256 + (r / 8 % 4 * 16 + row % 16) * 4 + r / 2 % 4;
+      reinterpret_cast<uint32_t*>(parts)[at] = halves.x;
+      reinterpret_cast<uint32_t*>(parts)[TT * KK * 256 + at] = halves.y;
+    }
     u32x4_t mask;   // of the last step: ranks in use
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int r = 32 * last + 8 * quarter + 2 * j;
       mask[j] = (r < rank ? 0xFFFFu : 0u) | (r + 1 < rank ? 0xFFFF0000u : 0u);
     }
-    for (int n0 = (int)n_first + 64 * wave; n0 < n_end; n0 += 256) {
-      f32x4_t acc[TT][4];
+    for (int n0 = (int)n_first; n0 < n_end; n0 += kColumns) {
+      my_b([&](int j, int row, int c) {
+        if (row < kColumns) *reinterpret_cast<u32x4_t*>(b_lds + row * pitch + c * 16) = b[j];
+      });
+      __syncthreads();   // (before the first piece v is in LDS too)
+#pragma unroll
+      for (int j = 0; j < kMyRows; ++j) y[j] = y_next[j];
+      if (n0 + kColumns < n_end) {
+        load_b(n0 + kColumns);
+        load_y(n0 + kColumns);
+      }
+      f32x4_t acc[TT][kTiles];
 #pragma unroll
       for (int w = 0; w < TT; ++w)
 #pragma unroll
-        for (int u = 0; u < 4; ++u) acc[w][u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-      const uint16_t* br[4];   // lane's rows of B: 16 (i / 4) + 4 u + i % 4, so that a lane has 16 neighbouring columns of the result
+        for (int u = 0; u < kTiles; ++u) acc[w][u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+      for (int k = 0; k <= last; ++k) {
+        u32x4_t hi[TT], lo[TT];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) br[u] = a.b + ((int64_t)max(i, 0) * a.N + min(n0 + 16 * (i16 >> 2) + 4 * u + (i16 & 3), a.N - 1)) * a.rank + 8 * quarter;
+        for (int w = 0; w < TT; ++w) hi[w] = parts[(w * KK + k) * 64 + lane], lo[w] = parts[(TT * KK + w * KK + k) * 64 + lane];
 #pragma unroll
-      for (int k = 0; k < KK; ++k) {
-        if (k > last) break;
-        u32x4_t bb[4];
-        const bool in = 32 * k + 8 * quarter < a.rank;
+        for (int u = 0; u < kTiles; ++u) {
+          u32x4_t bb = *reinterpret_cast<const u32x4_t*>(b_lds + ((wave * kTiles + u) * 16 + i16) * pitch + min(4 * k + quarter, row_pieces - 1) * 16);
+          if (k == last) bb &= mask;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          bb[u] = u32x4_t{0, 0, 0, 0};
-          if (in) bb[u] = *reinterpret_cast<const u32x4_t*>(br[u] + 32 * k);
-          if (k == last) bb[u] &= mask;
-        }
-#pragma unroll
-        for (int w = 0; w < TT; ++w)
-#pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            acc[w][u] = mfma(bb[u], v[1][w][k], acc[w][u]);
-            acc[w][u] = mfma(bb[u], v[0][w][k], acc[w][u]);
+          for (int w = 0; w < TT; ++w) {
+            acc[w][u] = mfma(bb, lo[w], acc[w][u]);
+            acc[w][u] = mfma(bb, hi[w], acc[w][u]);
           }
-      }
-      const int n = n0 + 16 * quarter;
-#pragma unroll
-      for (int w = 0; w < TT; ++w) {
-        const int row = 16 * w + i16;
-        if (row < first || row >= end || t[w] < 0 || n >= a.N) continue;
-        const uint16_t* yr = a.y + t[w] * a.ldy + n;
-        uint16_t* o = a.out + t[w] * a.ld_out + n;
-        if (n + 16 <= a.N) {
-          u32x4_t y[2];
-          __builtin_memcpy(y, yr, 32);
-          if (rank > 0) {
-#pragma unroll
-            for (int h = 0; h < 8; ++h)
-              y[h >> 2][h & 3] = pack_bf16(bf16_lo(y[h >> 2][h & 3]) + acc[w][h >> 1][2 * (h & 1)], bf16_hi(y[h >> 2][h & 3]) + acc[w][h >> 1][2 * (h & 1) + 1]);
-          }
-          __builtin_memcpy(o, y, 32);
-        } else {
-#pragma unroll
-          for (int h = 0; h < 16; ++h)
-            if (n + h < a.N) o[h] = rank > 0 ? to_bf16(bf16_lo(yr[h]) + acc[w][h >> 2][h & 3]) : yr[h];
         }
       }
+#pragma unroll
+      for (int w = 0; w < TT; ++w)
+#pragma unroll
+        for (int u = 0; u < kTiles; ++u) *reinterpret_cast<f32x4_t*>(products + (16 * w + i16) * kPitch + (wave * kTiles + u) * 16 + 4 * quarter) = acc[w][u];
+      __syncthreads();
+      store(n0);
     }
     __syncthreads();
   }
@@ -285,12 +526,14 @@ struct Plan {
   int tiles;       // of 16 rows in a block
   int64_t blocks;
   int together, splits, steps, rank_tiles, chunks, padded;
+  bool few;        // the second kernel for few rows
   int columns, column_chunks;
 };
 
 Plan plan_of(const ccq_adapter_set* s, int T) {
   Plan p;
-  p.tiles = T > 256 && s->rank <= 64 ? 2 : 1;
+  p.few = (int64_t)T * s->rank <= 8192 && T <= 4 * (int64_t)s->count;   // (runs of four rows or so, as far as one can tell here)
+  p.tiles = T > 256 && s->rank <= 64 && !p.few ? 2 : 1;
   const int rows = 16 * p.tiles;
   p.blocks = ((int64_t)T + rows - 1) / rows;
   // every adapter that begins inside a block makes one more run
@@ -299,32 +542,38 @@ Plan plan_of(const ccq_adapter_set* s, int T) {
   p.together = (int)(runs < rows ? runs : rows);
   if (p.together > T) p.together = T;
   p.padded = (s->rank + 15) / 16 * 16;
-  p.rank_tiles = p.padded >= 64 ? 4 : p.padded >= 32 ? 2 : 1;
+  p.rank_tiles = p.padded > 64 ? 8 : p.padded > 32 ? 4 : p.padded > 16 ? 2 : 1;
   p.chunks = (p.padded + 16 * p.rank_tiles - 1) / (16 * p.rank_tiles);
-  const int steps = (s->K + 31) / 32;
+  const int steps = (s->K + kStageColumns - 1) / kStageColumns;
   const int64_t busy = p.blocks + begins < p.blocks * p.together ? p.blocks + begins : p.blocks * p.together;   // workgroups with work
-  int64_t splits = 512 / (busy * p.chunks);
-  const int most = steps / (2 * kDownWaves);   // two steps a wavefront at least
-  if (splits > most) splits = most;
-  if (splits < 1) splits = 1;
-  if (splits > 32) splits = 32;
-  p.steps = (int)((steps + splits - 1) / splits);
+  // K is shared by a power of two of workgroups, neighbours in the grid: with eight and more of them an XCD's L2 meets the same columns of all A.
+  int splits = 1;
+  while (splits < 32 && busy * p.chunks * splits < 512 && steps >= splits * 4) splits *= 2;
+  p.steps = (steps + splits - 1) / splits;
   p.splits = (steps + p.steps - 1) / p.steps;
-  int64_t column_chunks = (2048 + busy - 1) / busy;
-  const int64_t pieces = ((int64_t)s->N + 255) / 256;
-  if (column_chunks > pieces) column_chunks = pieces;
-  p.columns = (int)((pieces + column_chunks - 1) / column_chunks * 256);
+  // Columns: in a multiple of eight parts, for the same reason
+  const int width = p.few || p.padded <= 64 ? 256 : 128;
+  const int64_t pieces = ((int64_t)s->N + width - 1) / width;
+  int64_t parts = ((p.blocks >= 64 ? 1024 : 512) + busy - 1) / busy;
+  parts = (parts + 7) / 8 * 8;
+  p.columns = (int)((pieces + parts - 1) / parts * width);
   p.column_chunks = (int)(((int64_t)s->N + p.columns - 1) / p.columns);
   return p;
 }
 
+template <typename K>
+bool launch(K kernel, const AdapterArgs& a, unsigned groups, int threads, int lds, hipStream_t s) {
+  if (lds > 48 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess) return false;
+  hipLaunchKernelGGL(kernel, dim3(groups), dim3(threads), (size_t)lds, s, a);
+  return true;
+}
 template <int RT, int TT>
-void down(const AdapterArgs& a, unsigned groups, hipStream_t s) {
-  hipLaunchKernelGGL((ccq_adapter_down_kernel<RT, TT>), dim3(groups), dim3(64 * kDownWaves), 0, s, a);
+bool down(const AdapterArgs& a, unsigned groups, hipStream_t s) {
+  return launch(ccq_adapter_down_kernel<RT, TT>, a, groups, 256, down_lds<RT, TT>(), s);
 }
 template <int KK, int TT>
-void up(const AdapterArgs& a, unsigned groups, hipStream_t s) {
-  hipLaunchKernelGGL((ccq_adapter_up_kernel<KK, TT>), dim3(groups), dim3(256), 0, s, a);
+bool up(const AdapterArgs& a, unsigned groups, hipStream_t s) {
+  return launch(ccq_adapter_up_kernel<KK, TT>, a, groups, 64 * kUpWaves, up_lds<KK, TT>(a.rank), s);
 }
 
 }  // namespace
@@ -349,27 +598,36 @@ int launch_adapters(const ccq_adapter_set* set, int T, const int32_t* rows, cons
   a.copies = out != y;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const bool two = p.tiles == 2;
-  auto parts = [&](int64_t per_block, int threads, auto launch) {   // blocks at a time that a launch has room for
+  bool ok = true;
+  auto in_parts = [&](int64_t per_block, int threads, auto part) {   // as many blocks at a time as a launch has room for
     const int64_t most = most_groups(threads) / per_block;
-    for (int64_t b = 0; b < p.blocks; b += most) {
+    for (int64_t b = 0; b < p.blocks && ok; b += most) {
       a.block0 = b;
-      launch((unsigned)((p.blocks - b < most ? p.blocks - b : most) * per_block));
+      a.blocks = (uint32_t)(p.blocks - b < most ? p.blocks - b : most);
+      ok = part((unsigned)(a.blocks * per_block));
     }
   };
   a.chunks = p.chunks;
-  parts((int64_t)p.together * p.chunks * p.splits, 64 * kDownWaves, [&](unsigned n) {
-    if (p.rank_tiles == 1) two ? down<1, 2>(a, n, s) : down<1, 1>(a, n, s);
-    else if (p.rank_tiles == 2) two ? down<2, 2>(a, n, s) : down<2, 1>(a, n, s);
-    else two ? down<4, 2>(a, n, s) : down<4, 1>(a, n, s);
+  in_parts((int64_t)p.together * p.chunks * p.splits, 256, [&](unsigned n) {
+    if (p.rank_tiles == 1) return two ? down<1, 2>(a, n, s) : down<1, 1>(a, n, s);
+    if (p.rank_tiles == 2) return two ? down<2, 2>(a, n, s) : down<2, 1>(a, n, s);
+    if (p.rank_tiles == 4) return two ? down<4, 2>(a, n, s) : down<4, 1>(a, n, s);
+    return down<8, 1>(a, n, s);
   });
   a.chunks = p.column_chunks;
-  parts((int64_t)p.together * p.column_chunks, 256, [&](unsigned n) {
-    if (p.padded <= 32) two ? up<1, 2>(a, n, s) : up<1, 1>(a, n, s);
-    else if (p.padded <= 64) two ? up<2, 2>(a, n, s) : up<2, 1>(a, n, s);
-    else if (p.padded <= 128) up<4, 1>(a, n, s);
-    else up<8, 1>(a, n, s);
+  in_parts((int64_t)p.together * p.column_chunks, p.few ? 256 : 64 * kUpWaves, [&](unsigned n) {
+    if (p.few) {
+      if (a.rank <= 8) return launch(ccq_adapter_few_kernel<1>, a, n, 256, 0, s);
+      if (a.rank <= 16) return launch(ccq_adapter_few_kernel<2>, a, n, 256, 0, s);
+      if (a.rank <= 32) return launch(ccq_adapter_few_kernel<4>, a, n, 256, 0, s);
+      if (a.rank <= 64) return launch(ccq_adapter_few_kernel<8>, a, n, 256, 0, s);
+      return a.rank <= 128 ? launch(ccq_adapter_few_kernel<16>, a, n, 256, 0, s) : launch(ccq_adapter_few_kernel<32>, a, n, 256, 0, s);
+    }
+    if (p.padded <= 32) return two ? up<1, 2>(a, n, s) : up<1, 1>(a, n, s);
+    if (p.padded <= 64) return two ? up<2, 2>(a, n, s) : up<2, 1>(a, n, s);
+    return p.padded <= 128 ? up<4, 1>(a, n, s) : up<8, 1>(a, n, s);
   });
-  return hipGetLastError() == hipSuccess ? CCQ_OK : CCQ_ERR_HIP;
+  return ok && hipGetLastError() == hipSuccess ? CCQ_OK : CCQ_ERR_HIP;
 }
 
 }  // namespace ccq
