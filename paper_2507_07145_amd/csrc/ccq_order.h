@@ -50,67 +50,107 @@ __device__ __forceinline__ uint32_t count_64(uint32_t* mine, int i0, int end, in
 }
 
 // LDS words that sort_entries needs.
-inline __host__ __device__ int sort_words(int waves, int E) { return (waves + 1) * (E + 1); }
+inline __host__ __device__ int sort_words(int waves, int E) { return (waves + 2) * (E + 1) + 66; }
 
-// All threads of a workgroup of `waves` wavefronts: the entries [begin, end), expert(i) 0 .. E (E: none).  `mine_of_all`: with several
-// workgroups their counts, this one's number and how many there are.
-template <typename Expert>
+// Sum of v over the lanes up to this one, by moves between lanes.
+__device__ __forceinline__ uint32_t up_to_lane(uint32_t v) {
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xF, 0xF, false);   // from one lane, two, four and eight below, within 16
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xF, 0xF, false);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xF, 0xF, false);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xF, 0xF, false);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xA, 0xF, false);   // the last lane of 16 to the next 16, of 32 to the next 32
+  return v + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xC, 0xF, false);
+}
+
+// All threads of a workgroup of `waves` wavefronts: the entries [begin, end), expert(i) 0 .. E (E: none).  With several workgroups `all_counts` are their
+// counts, `block` is this one's number.  ROUNDS > 0: a stretch has at most 64 ROUNDS entries, which stay in registers between the passes.
+template <int ROUNDS, typename Expert>
 __device__ __forceinline__ void sort_entries(const SortArgs& a, uint32_t* lds, int waves, int begin, int end, const Expert& expert, const uint32_t* all_counts, int block,
                                              int blocks) {
-  const int E1 = a.E + 1, tid = threadIdx.x, threads = waves * 64, wave = tid >> 6;
+  const int E1 = a.E + 1, tid = threadIdx.x, threads = waves * 64, wave = tid >> 6, lane = tid & 63;
   uint32_t* const mine = lds + wave * E1;
   uint32_t* const total = lds + waves * E1;
+  uint32_t* const below = total + E1;
+  uint32_t* const parts = below + E1;   // sums of 64 experts each
   const int64_t from64 = (int64_t)begin + (int64_t)wave * a.stretch, to64 = from64 + a.stretch;
   const int from = (int)min(from64, (int64_t)end), to = (int)min(to64, (int64_t)end);
-  for (int i = tid; i < waves * E1; i += threads) lds[i] = 0;
+  for (int i = tid; i < (waves + 2) * E1; i += threads) lds[i] = 0;
   __syncthreads();
-  uint32_t e;
-  for (int i = from; i < to; i += 64) count_64(mine, i, to, a.bits, expert, &e);
-  __syncthreads();
-  for (int x = tid; x < E1; x += threads) {
-    uint32_t below = 0, all = 0;
-    for (int b = 0; b < blocks && all_counts; ++b) {
-      const uint32_t c = all_counts[(int64_t)b * E1 + x];
-      if (b < block) below += c;
-      all += c;
+  if (all_counts) {   // as many threads to an expert as there are, each with every n-th workgroup's counts
+    const int n = max(1, threads / E1);
+    for (int x = tid % min(E1, threads); x < E1; x += threads) {
+      uint32_t sum = 0, before = 0;
+      const int b0 = tid / min(E1, threads);
+      if (b0 >= n) break;
+#pragma unroll 8
+      for (int b = b0; b < blocks; b += n) {
+        const uint32_t c = all_counts[(int64_t)b * E1 + x];
+        before += b < block ? c : 0;
+        sum += c;
+      }
+      atomicAdd(total + x, sum);
+      atomicAdd(below + x, before);
     }
-    uint32_t sum = below;
-    for (int w = 0; w < waves; ++w) {
-      const uint32_t c = lds[w * E1 + x];
-      lds[w * E1 + x] = sum;
-      sum += c;
-    }
-    total[x] = all_counts ? all : sum;
   }
-  __syncthreads();
-  if (wave == 0) {   // sums over the experts before each
-    uint32_t before = 0;
-    for (int x0 = 0; x0 < E1; x0 += 64) {
-      const int x = x0 + tid;
-      const uint32_t c = x < E1 ? total[x] : 0;
-      uint32_t sum = c;
+  uint32_t kept[ROUNDS > 0 ? ROUNDS : 1], e;   // expert << 16 | entries of the stretch before this one with the same
+  if constexpr (ROUNDS > 0) {
 #pragma unroll
-      for (int d = 1; d < 64; d *= 2) {
-        const uint32_t other = (uint32_t)__shfl_up((int)sum, d);
-        if (tid >= d) sum += other;
+    for (int r = 0; r < ROUNDS; ++r) {
+      kept[r] = 0;
+      if (from + 64 * r < to) {
+        const uint32_t had = count_64(mine, from + 64 * r, to, a.bits, expert, &e);
+        kept[r] = e << 16 | had;
       }
-      if (x < E1) {
-        total[x] = before + sum - c;
-        if (block == 0) a.offsets[x] = (int32_t)(before + sum - c);
+    }
+  } else {
+    for (int i = from; i < to; i += 64) count_64(mine, i, to, a.bits, expert, &e);
+  }
+  __syncthreads();
+  // the entries of each expert before each wavefront's, and of the experts before: sums within 64 experts first
+  for (int x0 = wave * 64; x0 < E1; x0 += threads) {
+    const int x = x0 + lane;
+    uint32_t all = 0;
+    if (x < E1) {
+      uint32_t sum = below[x];
+      for (int w = 0; w < waves; ++w) {
+        const uint32_t c = lds[w * E1 + x];
+        lds[w * E1 + x] = sum;
+        sum += c;
       }
-      before += (uint32_t)__shfl((int)sum, 63);
+      all = all_counts ? total[x] : sum;
+    }
+    const uint32_t upto = up_to_lane(all);
+    if (x < E1) total[x] = upto - all;
+    if (lane == 63) parts[x0 / 64] = upto;
+  }
+  __syncthreads();
+  for (int x0 = wave * 64; x0 < E1; x0 += threads) {
+    const int x = x0 + lane;
+    const uint32_t before = (uint32_t)__builtin_amdgcn_readlane((int)up_to_lane(lane < x0 / 64 ? parts[lane] : 0), 63);
+    if (x < E1) {
+      total[x] += before;
+      if (block == 0) a.offsets[x] = (int32_t)total[x];
     }
   }
   __syncthreads();
-  for (int i0 = from; i0 < to; i0 += 64) {
-    const uint32_t at = count_64(mine, i0, to, a.bits, expert, &e);
-    const int i = i0 + (tid & 63);
-    if (i >= to) continue;
+  auto place = [&](int i, uint32_t e, uint32_t at) {
     const int32_t p = (int32_t)(total[e] + at);
     const bool has = e < (uint32_t)a.E;
     a.rows[p] = i / a.k;
     if (a.experts) a.experts[p] = has ? (int32_t)e : -1;
     if (a.places) a.places[i] = has ? p : -1;
+  };
+  if constexpr (ROUNDS > 0) {
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+      const int i = from + 64 * r + lane;
+      if (i < to) place(i, kept[r] >> 16, mine[kept[r] >> 16] + (kept[r] & 0xFFFF));
+    }
+  } else {   // the counters go on from where each stretch's entries begin
+    for (int i0 = from; i0 < to; i0 += 64) {
+      const uint32_t at = count_64(mine, i0, to, a.bits, expert, &e);
+      if (i0 + lane < to) place(i0 + lane, e, at);
+    }
   }
 }
 

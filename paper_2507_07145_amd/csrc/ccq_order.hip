@@ -30,24 +30,27 @@ __global__ __launch_bounds__(1024) void ccq_sort_count_kernel(SortArgs a) {
   for (int x = threadIdx.x; x < E1; x += blockDim.x) a.counts[(int64_t)blockIdx.x * E1 + x] = lds[x];
 }
 
+template <int ROUNDS>
 __global__ __launch_bounds__(1024) void ccq_sort_kernel(SortArgs a) {
   extern __shared__ uint32_t lds[];
   const int64_t begin = (int64_t)blockIdx.x * a.chunk;
   const int end = (int)min(begin + a.chunk, (int64_t)a.P);
-  sort_entries(a, lds, blockDim.x >> 6, (int)begin, end, FromIds{a.ids, a.ld_ids, a.k, a.first, a.E}, gridDim.x > 1 ? a.counts : nullptr, blockIdx.x, gridDim.x);
+  sort_entries<ROUNDS>(a, lds, blockDim.x >> 6, (int)begin, end, FromIds{a.ids, a.ld_ids, a.k, a.first, a.E}, gridDim.x > 1 ? a.counts : nullptr, blockIdx.x, gridDim.x);
 }
 
-constexpr int kChunk = 2048, kMostBlocks = 64;
+// One workgroup up to 8192 entries, then workgroups of 2048 and more, 64 at most (each adds up the counts of all).
+constexpr int kOneBlock = 8192, kChunk = 2048, kMostBlocks = 64;
 
 int blocks_of(int64_t P) {
+  if (P <= kOneBlock) return 1;
   const int64_t n = (P + kChunk - 1) / kChunk;
-  return (int)(n < 1 ? 1 : n > kMostBlocks ? kMostBlocks : n);
+  return (int)(n > kMostBlocks ? kMostBlocks : n);
 }
 
-// As many wavefronts as have their counters in 56 KB of LDS.
-int waves_of(int E) {
+// As many wavefronts as have 64 entries each, and their counters in 56 KB of LDS.
+int waves_of(int E, int chunk) {
   int waves = 16;
-  while (waves > 1 && sort_words(waves, E) * 4 > 56 * 1024) waves /= 2;
+  while (waves > 1 && (sort_words(waves, E) * 4 > 56 * 1024 || (waves - 1) * 64 >= chunk)) waves /= 2;
   return waves;
 }
 
@@ -64,13 +67,15 @@ int launch_sort(const int32_t* ids, int64_t ld_ids, int T, int k, int first, int
   a.counts = static_cast<uint32_t*>(workspace);
   a.rows = order->rows, a.experts = order->experts, a.offsets = order->offsets, a.places = order->places;
   a.P = T * k, a.k = k, a.first = first, a.E = experts;
-  const int blocks = blocks_of(a.P), waves = waves_of(experts);
+  const int blocks = blocks_of(a.P);
   a.chunk = (int)(((int64_t)a.P + blocks - 1) / blocks);
+  const int waves = waves_of(experts, a.chunk);
   a.stretch = (int)((((int64_t)a.chunk + waves - 1) / waves + 63) / 64 * 64);
   a.bits = bits_of(experts);
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (blocks > 1) hipLaunchKernelGGL(ccq_sort_count_kernel, dim3(blocks), dim3(1024), (size_t)(experts + 1) * 4, s, a);
-  hipLaunchKernelGGL(ccq_sort_kernel, dim3(blocks), dim3(waves * 64), (size_t)sort_words(waves, experts) * 4, s, a);
+  const auto sort = a.stretch <= 64 ? ccq_sort_kernel<1> : a.stretch <= 128 ? ccq_sort_kernel<2> : a.stretch <= 512 ? ccq_sort_kernel<8> : ccq_sort_kernel<0>;
+  hipLaunchKernelGGL(sort, dim3(blocks), dim3(waves * 64), (size_t)sort_words(waves, experts) * 4, s, a);
   return hipGetLastError() == hipSuccess ? CCQ_OK : CCQ_ERR_HIP;
 }
 

@@ -29,18 +29,43 @@ bool rows_of(const at::Tensor* t, at::ScalarType type) { return t && t->dim() ==
 // (a single row's stride is whatever it is)
 int64_t ld(const at::Tensor* t) { return t->size(0) > 1 ? t->stride(0) : std::max(t->stride(0), t->size(1)); }
 
-// The four tensors of an order, in one piece of memory: offsets first, each from a multiple of 16 bytes on.
-struct MadeOrder {
-  at::Tensor rows, experts, offsets, places;
-  void make(int64_t T, int64_t k, int64_t E, c10::Device device) {
-    rows = at::detail::empty_cuda({T * k}, at::kInt, device, std::nullopt);
-    experts = at::detail::empty_cuda({T * k}, at::kInt, device, std::nullopt);
-    offsets = at::detail::empty_cuda({E + 1}, at::kInt, device, std::nullopt);
-    places = at::detail::empty_cuda({T, k}, at::kInt, device, std::nullopt);
+// Tensors in one piece of memory, each from a multiple of 16 bytes on: one allocation costs the host what each of six would.
+class Pieces {
+ public:
+  int64_t add(int64_t bytes) {
+    const int64_t at = bytes_;
+    bytes_ += (bytes + 15) / 16 * 16;
+    return at;
   }
-  ccq_order order() const {
-    return {static_cast<int32_t*>(rows.data_ptr()), static_cast<int32_t*>(experts.data_ptr()), static_cast<int32_t*>(offsets.data_ptr()),
-            static_cast<int32_t*>(places.data_ptr())};
+  void make(c10::Device device) { held_ = at::detail::empty_cuda({std::max<int64_t>(bytes_, 16)}, at::kByte, device, std::nullopt); }
+  void* at(int64_t offset) const { return static_cast<char*>(held_.data_ptr()) + offset; }
+  PyObject* tensor(int64_t offset, at::ScalarType type, at::IntArrayRef sizes) const {
+    auto impl = c10::make_intrusive<at::TensorImpl>(c10::Storage(held_.storage()), held_.key_set(), c10::scalarTypeToTypeMeta(type));
+    impl->set_storage_offset(offset / 4);   // (all are of four bytes)
+    impl->set_sizes_contiguous(sizes);
+    return THPVariable_Wrap(at::Tensor(std::move(impl)));
+  }
+
+ private:
+  at::Tensor held_;
+  int64_t bytes_ = 0;
+};
+
+// The four tensors of an order among them.
+struct MadeOrder {
+  int64_t T, k, E, rows, experts, offsets, places;
+  MadeOrder(Pieces& p, int64_t T_, int64_t k_, int64_t E_) : T(T_), k(k_), E(E_) {
+    rows = p.add(T * k * 4), experts = p.add(T * k * 4), offsets = p.add((E + 1) * 4), places = p.add(T * k * 4);
+  }
+  ccq_order order(const Pieces& p) const {
+    return {static_cast<int32_t*>(p.at(rows)), static_cast<int32_t*>(p.at(experts)), static_cast<int32_t*>(p.at(offsets)), static_cast<int32_t*>(p.at(places))};
+  }
+  // new references, or an exception and NULL for what could not be made
+  void tensors(const Pieces& p, PyObject* (&out)[4]) const {
+    out[0] = p.tensor(rows, at::kInt, {T * k});
+    out[1] = p.tensor(experts, at::kInt, {T * k});
+    out[2] = p.tensor(offsets, at::kInt, {E + 1});
+    out[3] = p.tensor(places, at::kInt, {T, k});
   }
 };
 
@@ -62,27 +87,27 @@ PyObject* call_route(PyObject*, PyObject* const* a, Py_ssize_t n) {
   r.bias = bias ? static_cast<const float*>(bias->data_ptr()) : nullptr;
   const int64_t need = entry.route_workspace(&r, ordered);
   if (need < 0) return general();
-  at::Tensor ids, weights;
-  MadeOrder made;
+  Pieces pieces;
+  const int64_t ids = pieces.add(T * r.top_k * 4), weights = pieces.add(T * r.top_k * 4);
+  std::optional<MadeOrder> made;
+  if (ordered) made.emplace(pieces, T, r.top_k, E);
   Workspace ws;
   int rc;
   {
     Unlocked u;
-    ids = at::detail::empty_cuda({T, r.top_k}, at::kInt, x->device(), std::nullopt);
-    weights = at::detail::empty_cuda({T, r.top_k}, at::kFloat, x->device(), std::nullopt);
-    r.ids = static_cast<int32_t*>(ids.data_ptr()), r.weights = static_cast<float*>(weights.data_ptr());
+    pieces.make(x->device());
+    r.ids = static_cast<int32_t*>(pieces.at(ids)), r.weights = static_cast<float*>(pieces.at(weights));
     ccq_order order;
-    if (ordered) {
-      made.make(T, r.top_k, E, x->device());
-      order = made.order();
-    }
+    if (ordered) order = made->order(pieces);
     ws.make(need, x->device());
     rc = entry.route(&r, ordered ? &order : nullptr, ws.ptr, ws.bytes, current_stream());
   }
   if (rc != CCQ_OK) return PyLong_FromLong(rc);
-  if (!ordered) return Py_BuildValue("(NN)", THPVariable_Wrap(std::move(ids)), THPVariable_Wrap(std::move(weights)));
-  return Py_BuildValue("(NNNNNN)", THPVariable_Wrap(std::move(ids)), THPVariable_Wrap(std::move(weights)), THPVariable_Wrap(std::move(made.rows)),
-                       THPVariable_Wrap(std::move(made.experts)), THPVariable_Wrap(std::move(made.offsets)), THPVariable_Wrap(std::move(made.places)));
+  PyObject *made_ids = pieces.tensor(ids, at::kInt, {T, r.top_k}), *made_weights = pieces.tensor(weights, at::kFloat, {T, r.top_k});
+  if (!ordered) return Py_BuildValue("(NN)", made_ids, made_weights);
+  PyObject* o[4];
+  made->tensors(pieces, o);
+  return Py_BuildValue("(NNNNNN)", made_ids, made_weights, o[0], o[1], o[2], o[3]);
   END_HANDLE_TH_ERRORS
 }
 
@@ -97,19 +122,21 @@ PyObject* call_sort(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (T > INT32_MAX || k > INT32_MAX) return general();
   const int64_t need = entry.sort_workspace((int32_t)T, (int32_t)k, E);
   if (need < 0) return general();
-  MadeOrder made;
+  Pieces pieces;
+  const MadeOrder made(pieces, T, k, E);
   Workspace ws;
   int rc;
   {
     Unlocked u;
-    made.make(T, k, E, ids->device());
-    const ccq_order order = made.order();
+    pieces.make(ids->device());
+    const ccq_order order = made.order(pieces);
     ws.make(need, ids->device());
     rc = entry.sort(static_cast<const int32_t*>(ids->data_ptr()), ld(ids), (int32_t)T, (int32_t)k, first, E, &order, ws.ptr, ws.bytes, current_stream());
   }
   if (rc != CCQ_OK) return PyLong_FromLong(rc);
-  return Py_BuildValue("(NNNN)", THPVariable_Wrap(std::move(made.rows)), THPVariable_Wrap(std::move(made.experts)), THPVariable_Wrap(std::move(made.offsets)),
-                       THPVariable_Wrap(std::move(made.places)));
+  PyObject* o[4];
+  made.tensors(pieces, o);
+  return Py_BuildValue("(NNNN)", o[0], o[1], o[2], o[3]);
   END_HANDLE_TH_ERRORS
 }
 

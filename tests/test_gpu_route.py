@@ -95,6 +95,26 @@ def test_scores_next_to_each_other():
     check(l, 8, "near sums in groups", scoring="sigmoid", bias=bias, groups=8, top_groups=4)
 
 
+@pytest.mark.parametrize("E,k", [(64, 8), (128, 4), (256, 8), (256, 12), (256, 16), (500, 6), (1000, 32)])
+@pytest.mark.parametrize("T", [6, 2100])
+def test_many_rows_with_equal_and_nearly_equal_values(T, E, k):
+    """Few different logits, biases of 0 or of some 2^-22: order by index, by the last bits, and among more candidates than are looked at first."""
+    if T * E > 600000:
+        T //= 4
+    g = torch.Generator().manual_seed(E + T)
+    steps = torch.randint(0, 7, (T, E), generator=g) * 0.25
+    tiny = torch.randint(-8, 9, (E,), generator=g) * 2.0 ** -24
+    for scoring, bias in (("sigmoid", torch.zeros(E)), ("sigmoid", tiny), ("softmax", tiny), ("softmax", None)):
+        check(steps, k, f"{scoring} {bias is not None}", scoring=scoring, bias=bias, order=False, renormalize=True)
+    near = 1.0 + torch.randint(0, 40, (T, E), generator=g) * 2.0 ** -23     # neighbours in fp32
+    check(near, k, "neighbours", order=False)
+    check(near, k, "neighbours, biased", order=False, scoring="sigmoid", bias=tiny)
+    if E % 8 == 0:
+        for scoring in ("sigmoid", "softmax"):
+            check(steps, min(k, E // 8 * 3), "groups", order=False, scoring=scoring, bias=tiny, groups=8, top_groups=3)
+            check(near, min(k, E // 8 * 3), "groups of neighbours", order=False, scoring=scoring, groups=8, top_groups=3)
+
+
 def test_closed_experts():
     inf, nan = float("inf"), float("nan")
     l = logits_of(9, 40, 5)
