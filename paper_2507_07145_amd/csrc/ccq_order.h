@@ -9,12 +9,28 @@
 
 namespace ccq {
 
+// Division of numbers below 2^31 by one that is known on the host: with s bits in by - 1, the upper half of n ceil(2^(31 + s) / by), shifted by s - 1.
+struct Divisor {
+  int32_t by = 1, shift = 0;
+  uint32_t factor = 0;
+  Divisor() = default;
+  explicit Divisor(int by_) : by(by_) {
+    int s = 0;
+    while ((by - 1) >> s) ++s;
+    if (s == 0) return;
+    shift = s - 1;
+    factor = (uint32_t)(((1ull << (31 + s)) + by - 1) / by);
+  }
+  __device__ __forceinline__ int divide(int n) const { return by == 1 ? n : (int)(__umulhi((uint32_t)n, factor) >> shift); }
+};
+
 struct SortArgs {
   const int32_t* ids;
   int64_t ld_ids;
   uint32_t* counts;    // [workgroups][E + 1] of the workspace: entries of each expert, where there are several workgroups
   int32_t *rows, *experts, *offsets, *places;
-  int32_t P, k, first, E;
+  Divisor k;
+  int32_t P, first, E;
   int32_t chunk;       // entries of a workgroup
   int32_t stretch;     // of a wavefront, a multiple of 64
   int32_t bits;        // of an expert's number, E itself (none) among them
@@ -22,12 +38,14 @@ struct SortArgs {
 
 // Lanes of `active` whose expert is this lane's.
 __device__ __forceinline__ uint64_t peers_of(uint32_t e, int bits, uint64_t active) {
-  uint64_t same = active;
+  uint32_t lo = (uint32_t)active, hi = (uint32_t)(active >> 32);
   for (int b = 0; b < bits; ++b) {
-    const uint64_t with = __ballot((e >> b) & 1);
-    same &= (e >> b) & 1 ? with : ~with;
+    const uint32_t mine = (uint32_t)__builtin_amdgcn_sbfe((int)e, b, 1);   // all ones or none
+    const uint64_t with = __ballot(mine != 0);
+    lo &= ~((uint32_t)with ^ mine);
+    hi &= ~((uint32_t)(with >> 32) ^ mine);
   }
-  return same;
+  return (uint64_t)hi << 32 | lo;
 }
 
 __device__ __forceinline__ int lanes_below(uint64_t mask) {
@@ -136,7 +154,7 @@ __device__ __forceinline__ void sort_entries(const SortArgs& a, uint32_t* lds, i
   auto place = [&](int i, uint32_t e, uint32_t at) {
     const int32_t p = (int32_t)(total[e] + at);
     const bool has = e < (uint32_t)a.E;
-    a.rows[p] = i / a.k;
+    a.rows[p] = a.k.divide(i);
     if (a.experts) a.experts[p] = has ? (int32_t)e : -1;
     if (a.places) a.places[i] = has ? p : -1;
   };

@@ -9,10 +9,15 @@ namespace {
 struct FromIds {
   const int32_t* ids;
   int64_t ld;
-  int k, first, E;
+  Divisor k;
+  int first, E;
   __device__ __forceinline__ uint32_t operator()(int i) const {
-    const int t = i / k;
-    const int32_t id = ids[(int64_t)t * ld + (i - t * k)];
+    int64_t at = i;
+    if (ld != k.by) {
+      const int t = k.divide(i);
+      at = (int64_t)t * ld + (i - t * k.by);
+    }
+    const int32_t id = ids[at];
     return id >= first && id - first < E ? (uint32_t)(id - first) : (uint32_t)E;
   }
 };
@@ -66,7 +71,7 @@ int launch_sort(const int32_t* ids, int64_t ld_ids, int T, int k, int first, int
   a.ids = ids, a.ld_ids = ld_ids;
   a.counts = static_cast<uint32_t*>(workspace);
   a.rows = order->rows, a.experts = order->experts, a.offsets = order->offsets, a.places = order->places;
-  a.P = T * k, a.k = k, a.first = first, a.E = experts;
+  a.P = T * k, a.k = Divisor(k), a.first = first, a.E = experts;
   const int blocks = blocks_of(a.P);
   a.chunk = (int)(((int64_t)a.P + blocks - 1) / blocks);
   const int waves = waves_of(experts, a.chunk);

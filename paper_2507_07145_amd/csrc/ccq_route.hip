@@ -384,9 +384,10 @@ __global__ __launch_bounds__(256) void ccq_route_kernel(RouteArgs a) {
 // A few rows and their order in one launch, a wavefront for each row.
 struct FromLds {
   const int32_t (*rows)[kPlaces];
-  int k, E;
+  Divisor k;
+  int E;
   __device__ __forceinline__ uint32_t operator()(int i) const {
-    const int t = i / k, id = rows[t][i - t * k];
+    const int t = k.divide(i), id = rows[t][i - t * k.by];
     return id >= 0 ? (uint32_t)id : (uint32_t)E;
   }
 };
@@ -398,7 +399,7 @@ __global__ __launch_bounds__(64 * kFewRows) void ccq_route_few_kernel(RouteArgs 
   const int row = threadIdx.x / 64;
   choose<64, V, BIAS>(a, lds + row * row_bytes(a.E, a.groups), chosen[row], row, threadIdx.x & 63);
   __syncthreads();
-  sort_entries<1>(sort, reinterpret_cast<uint32_t*>(lds), blockDim.x / 64, 0, sort.P, FromLds{chosen, a.k, a.E}, nullptr, 0, 1);
+  sort_entries<1>(sort, reinterpret_cast<uint32_t*>(lds), blockDim.x / 64, 0, sort.P, FromLds{chosen, sort.k, a.E}, nullptr, 0, 1);
 }
 
 template <typename Kernel>
@@ -471,7 +472,7 @@ int launch_route(const ccq_router* r, const ccq_order* order, void* workspace, v
     SortArgs sort;
     sort.ids = nullptr, sort.counts = nullptr, sort.ld_ids = 0;
     sort.rows = order->rows, sort.experts = order->experts, sort.offsets = order->offsets, sort.places = order->places;
-    sort.P = a.T * a.k, sort.k = a.k, sort.first = 0, sort.E = a.E, sort.chunk = sort.P;
+    sort.P = a.T * a.k, sort.k = Divisor(a.k), sort.first = 0, sort.E = a.E, sort.chunk = sort.P;
     sort.stretch = 64;   // (top_k is 32 at most)
     sort.bits = bits_of(a.E);
     const bool ok = a.bias ? launch_few_by_size<true>(a, sort, s) : launch_few_by_size<false>(a, sort, s);
