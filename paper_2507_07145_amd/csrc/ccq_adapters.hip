@@ -13,6 +13,7 @@ namespace ccq {
 namespace {
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
+typedef u32x4_t __attribute__((aligned(2))) u32x4_any_t;   // rows may start at any element
 
 struct AdapterArgs {
   const uint16_t *a, *b, *x, *y;
@@ -22,6 +23,8 @@ struct AdapterArgs {
   float* v;               // [splits][T][padded rank]
   int64_t ldx, ldy, ld_out, block0;
   uint32_t blocks;        // of the launch
+  u32x4_t* parts;         // v as matrix operands, where there are many rows
+  int32_t blocks_each;    // blocks of 32 rows of a workgroup then
   int32_t T, K, N, rank, count, padded;
   int32_t together;       // runs of a block that have a workgroup of their own at the same time
   int32_t splits, steps;  // workgroups along K, steps of 32 columns of each
@@ -39,10 +42,15 @@ struct Runs {
   uint64_t starts;
   int adapter;   // lane i: of row i of the block, -1: none
   int rows;      // rows of the block that there are
-  __device__ __forceinline__ Runs(const AdapterArgs& a, int64_t p0, int most) {
+  // the adapter of this lane's row, which the constructor is given
+  static __device__ __forceinline__ int of_lane(const AdapterArgs& a, int64_t p0, int most) {
+    const int lane = threadIdx.x & 63;
+    return lane < most && p0 + lane < a.T ? a.experts[p0 + lane] : -1;
+  }
+  __device__ __forceinline__ Runs(const AdapterArgs& a, int64_t p0, int most) : Runs(a, p0, most, of_lane(a, p0, most)) {}
+  __device__ __forceinline__ Runs(const AdapterArgs& a, int64_t p0, int most, int of_this_lane) : adapter(of_this_lane) {
     const int lane = threadIdx.x & 63;
     rows = (int)min((int64_t)most, (int64_t)a.T - p0);
-    adapter = lane < rows ? a.experts[p0 + lane] : -1;
     if ((uint32_t)adapter >= (uint32_t)a.count) adapter = -1;
     const int before = __shfl_up(adapter, 1);
     starts = __ballot(lane < rows && (lane == 0 || adapter != before));
@@ -361,29 +369,29 @@ constexpr int kRowFloats = 4;   // between a row's results in LDS and the next o
 constexpr int kUpWaves = 8;
 constexpr int piece_columns(int kk) { return kk <= 2 ? 256 : 128; }
 __host__ __device__ constexpr int b_pitch(int rank) { return (rank / 8 | 1) * 16; }
-template <int KK, int TT>
+template <int KK>
 constexpr int up_lds(int rank) {
-  return 2 * TT * KK * 1024 + 16 * TT * (piece_columns(KK) + kRowFloats) * 4 + piece_columns(KK) * b_pitch(rank);
+  return 2 * KK * 1024 + 16 * (piece_columns(KK) + kRowFloats) * 4 + piece_columns(KK) * b_pitch(rank);
 }
 
 // KK: steps of 32 ranks.  A workgroup takes its columns in pieces; B and y of the next piece are asked for while one is worked on.  B goes through LDS for the
 // reason given above, the products go through LDS to meet y, and y and out are read and written along their rows.
-template <int KK, int TT>
+template <int KK>
 __global__ __launch_bounds__(64 * kUpWaves, 4) void ccq_adapter_up_kernel(AdapterArgs a) {
   extern __shared__ __align__(256) uint8_t lds[];
   constexpr int kThreads = 64 * kUpWaves, kColumns = piece_columns(KK), kTiles = kColumns / (16 * kUpWaves);   // of 16 columns for each wavefront
   constexpr int kPitch = kColumns + kRowFloats;
-  constexpr int kRowPieces = kColumns / 8, kRowsAtOnce = kThreads / kRowPieces, kMyRows = 16 * TT < kRowsAtOnce ? 1 : 16 * TT / kRowsAtOnce;
+  constexpr int kRowPieces = kColumns / 8, kRowsAtOnce = kThreads / kRowPieces, kMyRows = 16 < kRowsAtOnce ? 1 : 16 / kRowsAtOnce;
   constexpr int kMyB = kColumns * KK * 4 / kThreads;   // pieces of 16 bytes of B, at most
-  u32x4_t* const parts = reinterpret_cast<u32x4_t*>(lds);                                   // [2][TT KK][64]: v as matrix operands, its upper and its lower bits
-  float* const products = reinterpret_cast<float*>(lds + 2 * TT * KK * 1024);              // [16 TT][kPitch]
-  uint8_t* const b_lds = lds + 2 * TT * KK * 1024 + 16 * TT * kPitch * 4;
+  u32x4_t* const parts = reinterpret_cast<u32x4_t*>(lds);                                   // [2][KK][64]: v as matrix operands, its upper and its lower bits
+  float* const products = reinterpret_cast<float*>(lds + 2 * KK * 1024);              // [16][kPitch]
+  uint8_t* const b_lds = lds + 2 * KK * 1024 + 16 * kPitch * 4;
   uint32_t g = blockIdx.x;
   const int64_t n_first = (int64_t)(g % a.chunks) * a.columns;
   g /= a.chunks;
   const uint32_t later = g / a.blocks, turn = a.together - 1 - later;   // (the runs that few blocks have first: begun last, they would run alone)
-  const int64_t p0 = (a.block0 + (g - later * a.blocks)) * 16 * TT;
-  Runs runs(a, p0, 16 * TT);
+  const int64_t p0 = (a.block0 + (g - later * a.blocks)) * 16;
+  Runs runs(a, p0, 16);
   runs.skip((int)turn);
   if (!runs.starts) return;
   const int pitch = b_pitch(a.rank), row_pieces = a.rank / 8;
@@ -435,7 +443,7 @@ __global__ __launch_bounds__(64 * kUpWaves, 4) void ccq_adapter_up_kernel(Adapte
       const int n = n0 + column;
 #pragma unroll
       for (int j = 0; j < kMyRows; ++j)
-        if (mine[j] && n + 8 <= a.N) y_next[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(a.y + (int64_t)t[j] * a.ldy + n));
+        if (mine[j] && n + 8 <= a.N) y_next[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_any_t*>(a.y + (int64_t)t[j] * a.ldy + n));
     };
     auto store = [&](int n0) {
       const int n = n0 + column;
@@ -449,7 +457,7 @@ __global__ __launch_bounds__(64 * kUpWaves, 4) void ccq_adapter_up_kernel(Adapte
 #pragma unroll
           for (int h = 0; h < 4; ++h)
             y[j][h] = pack_bf16(bf16_lo(y[j][h]) + (h < 2 ? d0[2 * h] : d1[2 * h - 4]), bf16_hi(y[j][h]) + (h < 2 ? d0[2 * h + 1] : d1[2 * h - 3]));
-          __builtin_nontemporal_store(y[j], reinterpret_cast<u32x4_t*>(o));
+          __builtin_nontemporal_store(y[j], reinterpret_cast<u32x4_any_t*>(o));
         } else {   // the last columns
           const uint16_t* from = a.y + (int64_t)t[j] * a.ldy + n;
 #pragma unroll 1
@@ -462,15 +470,15 @@ __global__ __launch_bounds__(64 * kUpWaves, 4) void ccq_adapter_up_kernel(Adapte
 
     const float scale = a.scales ? a.scales[i] : 1.f;
 #pragma unroll 1
-    for (int c = thread; c < TT * KK * 256; c += kThreads) {   // rows, and 16 KK pairs of ranks of each
+    for (int c = thread; c < KK * 256; c += kThreads) {   // rows, and 16 KK pairs of ranks of each
       const int row = c / (16 * KK), r = c % (16 * KK) * 2;
       f32x2_t two = {0.f, 0.f};
       if (row >= first && row < end && r < rank) two = sum_parts(a, a.v + (p0 + row) * a.padded + r, 0, 1);
       two.x *= scale, two.y = r + 1 < rank ? two.y * scale : 0.f;
       const u32x2_t halves = in_two(two);
-      const int at = (row / 16 * KK + r / 32) * 256 + (r / 8 % 4 * 16 + row % 16) * 4 + r / 2 % 4;
+      const int at = r / 32 * 256 + (r / 8 % 4 * 16 + row) * 4 + r / 2 % 4;
       reinterpret_cast<uint32_t*>(parts)[at] = halves.x;
-      reinterpret_cast<uint32_t*>(parts)[TT * KK * 256 + at] = halves.y;
+      reinterpret_cast<uint32_t*>(parts)[KK * 256 + at] = halves.y;
     }
     u32x4_t mask;   // of the last step: ranks in use
 #pragma unroll
@@ -489,31 +497,22 @@ __global__ __launch_bounds__(64 * kUpWaves, 4) void ccq_adapter_up_kernel(Adapte
         load_b(n0 + kColumns);
         load_y(n0 + kColumns);
       }
-      f32x4_t acc[TT][kTiles];
+      f32x4_t acc[kTiles];
 #pragma unroll
-      for (int w = 0; w < TT; ++w)
-#pragma unroll
-        for (int u = 0; u < kTiles; ++u) acc[w][u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      for (int u = 0; u < kTiles; ++u) acc[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
       for (int k = 0; k <= last; ++k) {
-        u32x4_t hi[TT], lo[TT];
-#pragma unroll
-        for (int w = 0; w < TT; ++w) hi[w] = parts[(w * KK + k) * 64 + lane], lo[w] = parts[(TT * KK + w * KK + k) * 64 + lane];
+        const u32x4_t hi = parts[k * 64 + lane], lo = parts[(KK + k) * 64 + lane];
 #pragma unroll
         for (int u = 0; u < kTiles; ++u) {
           u32x4_t bb = *reinterpret_cast<const u32x4_t*>(b_lds + ((wave * kTiles + u) * 16 + i16) * pitch + min(4 * k + quarter, row_pieces - 1) * 16);
           if (k == last) bb &= mask;
-#pragma unroll
-          for (int w = 0; w < TT; ++w) {
-            acc[w][u] = mfma(bb, lo[w], acc[w][u]);
-            acc[w][u] = mfma(bb, hi[w], acc[w][u]);
-          }
+          acc[u] = mfma(bb, lo, acc[u]);
+          acc[u] = mfma(bb, hi, acc[u]);
         }
       }
 #pragma unroll
-      for (int w = 0; w < TT; ++w)
-#pragma unroll
-        for (int u = 0; u < kTiles; ++u) *reinterpret_cast<f32x4_t*>(products + (16 * w + i16) * kPitch + (wave * kTiles + u) * 16 + 4 * quarter) = acc[w][u];
+      for (int u = 0; u < kTiles; ++u) *reinterpret_cast<f32x4_t*>(products + i16 * kPitch + (wave * kTiles + u) * 16 + 4 * quarter) = acc[u];
       __syncthreads();
       store(n0);
     }
@@ -521,19 +520,164 @@ __global__ __launch_bounds__(64 * kUpWaves, 4) void ccq_adapter_up_kernel(Adapte
   }
 }
 
+// The second product for many rows, in two kernels.  The first adds v up, multiplies it by the scales and leaves it as matrix operands, 32 rows at a time: its upper bits and
+// its lower ones, [blocks of 32 rows][2][2 KK][64] pieces of 16 bytes.
+template <int KK>
+__global__ __launch_bounds__(256) void ccq_adapter_join_kernel(AdapterArgs a) {
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, p = at / (16 * KK);
+  const int r = (int)(at % (16 * KK)) * 2;
+  f32x2_t two = {0.f, 0.f};
+  if (p < a.T) {
+    const int i = a.experts[p];
+    if ((uint32_t)i < (uint32_t)a.count) {
+      const int rank = rank_of(a, i);
+      const float scale = a.scales ? a.scales[i] : 1.f;
+      if (r < rank) two = sum_parts(a, a.v + p * a.padded + r, 0, 1);
+      two.x *= scale, two.y = r + 1 < rank ? two.y * scale : 0.f;
+    }
+  }
+  const u32x2_t halves = in_two(two);
+  uint32_t* const to = reinterpret_cast<uint32_t*>(a.parts + p / 32 * (4 * KK * 64)) + ((p % 32 / 16 * KK + r / 32) * 64 + r / 8 % 4 * 16 + p % 16) * 4 + r / 2 % 4;
+  to[0] = halves.x;
+  to[2 * KK * 64 * 4] = halves.y;
+}
+
+// The second: a workgroup keeps 256 columns of an adapter's B in registers, a wavefront 32 of them, and goes along the rows, 32 at a time; y of the next rows is asked for
+// while the products of these go through LDS to meet theirs.  STREAMS: y is not to stay in the caches.  Bound by y and out.
+template <int KK, bool STREAMS>
+__global__ __launch_bounds__(512, KK <= 2 ? 4 : 2) void ccq_adapter_rows_kernel(AdapterArgs a) {
+  constexpr int kColumns = 256, kPitch = kColumns + kRowFloats, kMyRows = 2;   // rows row0 and row0 + 16 of a thread
+  __shared__ __align__(16) float products[32 * kPitch];
+  const int n_first = (int)(blockIdx.x % a.chunks) * kColumns;
+  const int64_t block_from = (int64_t)(blockIdx.x / a.chunks) * a.blocks_each, all_blocks = ((int64_t)a.T + 31) / 32;
+  const int64_t block_to = min(block_from + a.blocks_each, all_blocks);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i16 = lane & 15, quarter = lane >> 4;
+  const int column = threadIdx.x % 32 * 8, row0 = threadIdx.x / 32, n = n_first + column;
+  const bool whole = n + 8 <= a.N;
+  // rows of a block for this thread, and their y
+  auto rows_of = [&](int64_t block, int (&t)[kMyRows]) {
+#pragma unroll
+    for (int j = 0; j < kMyRows; ++j) {
+      const int64_t p = block * 32 + row0 + 16 * j;
+      t[j] = p < a.T ? a.rows[p] : -1;
+      if ((uint32_t)t[j] >= (uint32_t)a.T) t[j] = -1;
+    }
+  };
+  auto load_y = [&](const int (&t)[kMyRows], u32x4_t (&y)[kMyRows]) {
+#pragma unroll
+    for (int j = 0; j < kMyRows; ++j)
+      if (t[j] >= 0 && whole) {
+        const u32x4_any_t* from = reinterpret_cast<const u32x4_any_t*>(a.y + (int64_t)t[j] * a.ldy + n);
+        if constexpr (STREAMS) y[j] = __builtin_nontemporal_load(from);
+        else y[j] = *from;
+      }
+  };
+  int t[kMyRows], t_next[kMyRows];
+  u32x4_t y[kMyRows], y_next[kMyRows], b[KK][2];
+  int t_after[kMyRows], adapters = Runs::of_lane(a, block_from * 32, 32), adapters_next;
+  rows_of(block_from, t_next);
+  rows_of(block_from + 1, t_after);
+  load_y(t_next, y_next);
+  int held = -1, last = -1;   // whose B the registers hold, and its last step of 32 ranks
+  for (int64_t block = block_from; block < block_to; ++block) {
+    // what this block needs from memory was asked for before, but for v, which is asked for first; then the next block's
+    u32x4_t v[KK <= 2 ? 2 * KK : 1][2];
+    const u32x4_t* const parts = a.parts + block * (4 * KK * 64) + lane;
+    if constexpr (KK <= 2) {
+#pragma unroll
+      for (int c = 0; c < 2 * KK; ++c) v[c][0] = parts[c * 64], v[c][1] = parts[(2 * KK + c) * 64];
+    }
+    Runs runs(a, block * 32, 32, adapters);
+    adapters_next = Runs::of_lane(a, (block + 1) * 32, 32);
+#pragma unroll
+    for (int j = 0; j < kMyRows; ++j) t[j] = t_next[j], y[j] = y_next[j], t_next[j] = t_after[j];
+    if (block + 1 < block_to) load_y(t_next, y_next);
+    rows_of(block + 2, t_after);
+    adapters = adapters_next;
+    for (; runs.starts; runs.skip(1)) {
+      const int first = runs.first(), end = runs.end();
+      const int i = __builtin_amdgcn_readfirstlane(__shfl(runs.adapter, first));
+      if (i < 0 && !a.copies) continue;
+      if (i >= 0 && i != held) {
+        held = i;
+        const int rank = rank_of(a, i);
+        last = (rank - 1) >> 5;
+#pragma unroll
+        for (int k = 0; k < KK; ++k)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const int r = 32 * k + 8 * quarter;
+            u32x4_t bits = *reinterpret_cast<const u32x4_t*>(a.b + ((int64_t)i * a.N + min(n_first + 32 * wave + 16 * u + i16, a.N - 1)) * a.rank + min(r, a.rank - 8));
+#pragma unroll
+            for (int h = 0; h < 4; ++h) bits[h] &= (r + 2 * h < rank ? 0xFFFFu : 0u) | (r + 2 * h + 1 < rank ? 0xFFFF0000u : 0u);
+            b[k][u] = bits;
+          }
+      }
+      const bool adds = i >= 0 && last >= 0;
+      if (adds) {
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          f32x4_t acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+          for (int k = 0; k < KK; ++k) {
+            if (k > last) break;
+            u32x4_t hi, lo;
+            if constexpr (KK <= 2) hi = v[w * KK + k][0], lo = v[w * KK + k][1];
+            else hi = parts[(w * KK + k) * 64], lo = parts[(2 * KK + w * KK + k) * 64];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              acc[u] = mfma(b[k][u], lo, acc[u]);
+              acc[u] = mfma(b[k][u], hi, acc[u]);
+            }
+          }
+#pragma unroll
+          for (int u = 0; u < 2; ++u) *reinterpret_cast<f32x4_t*>(products + (16 * w + i16) * kPitch + 32 * wave + 16 * u + 4 * quarter) = acc[u];
+        }
+        __syncthreads();
+      }
+#pragma unroll
+      for (int j = 0; j < kMyRows; ++j) {
+        const int row = row0 + 16 * j;
+        if (row < first || row >= end || t[j] < 0 || n >= a.N || (!adds && !a.copies)) continue;
+        const float* d = products + row * kPitch + column;
+        uint16_t* o = a.out + (int64_t)t[j] * a.ld_out + n;
+        if (whole) {
+          u32x4_t sum = y[j];
+          if (adds) {
+            const f32x4_t d0 = *reinterpret_cast<const f32x4_t*>(d), d1 = *reinterpret_cast<const f32x4_t*>(d + 4);
+#pragma unroll
+            for (int h = 0; h < 4; ++h)
+              sum[h] = pack_bf16(bf16_lo(sum[h]) + (h < 2 ? d0[2 * h] : d1[2 * h - 4]), bf16_hi(sum[h]) + (h < 2 ? d0[2 * h + 1] : d1[2 * h - 3]));
+          }
+          __builtin_nontemporal_store(sum, reinterpret_cast<u32x4_any_t*>(o));
+        } else {   // the last columns
+          const uint16_t* from = a.y + (int64_t)t[j] * a.ldy + n;
+#pragma unroll 1
+          for (int h = 0; h < a.N - n; ++h) o[h] = adds ? to_bf16(bf16_lo(from[h]) + d[h]) : from[h];
+        }
+      }
+      if (adds) __syncthreads();
+    }
+  }
+}
+
+constexpr int kAtOnce = 512;   // workgroups of 512 threads that the chip holds
+
 // How the rows and K of a call are cut.
 struct Plan {
   int tiles;       // of 16 rows in a block
   int64_t blocks;
   int together, splits, steps, rank_tiles, chunks, padded;
-  bool few;        // the second kernel for few rows
+  bool few, many;  // the second kernel for runs of few rows, the kernels for many rows
   int columns, column_chunks;
+  int steps32;     // of 32 ranks: 1, 2, 4 or 8
 };
 
 Plan plan_of(const ccq_adapter_set* s, int T) {
   Plan p;
   p.few = (int64_t)T * s->rank <= 8192 && T <= 4 * (int64_t)s->count;   // (runs of four rows or so, as far as one can tell here)
-  p.tiles = T > 256 && s->rank <= 64 && !p.few ? 2 : 1;
+  p.many = !p.few && T >= 512 && T <= 1 << 22;   // (its workgroups are one launch's)
+  p.tiles = p.many && s->rank <= 64 ? 2 : 1;
   const int rows = 16 * p.tiles;
   p.blocks = ((int64_t)T + rows - 1) / rows;
   // every adapter that begins inside a block makes one more run
@@ -552,12 +696,14 @@ Plan plan_of(const ccq_adapter_set* s, int T) {
   p.steps = (steps + splits - 1) / splits;
   p.splits = (steps + p.steps - 1) / p.steps;
   // Columns: in a multiple of eight parts, for the same reason
-  const int width = p.few || p.padded <= 64 ? 256 : 128;
+  p.steps32 = p.padded <= 32 ? 1 : p.padded <= 64 ? 2 : p.padded <= 128 ? 4 : 8;
+  const int width = p.few || p.many || p.padded <= 64 ? 256 : 128;
   const int64_t pieces = ((int64_t)s->N + width - 1) / width;
   int64_t parts = ((p.blocks >= 64 ? 1024 : 512) + busy - 1) / busy;
   parts = (parts + 7) / 8 * 8;
   p.columns = (int)((pieces + parts - 1) / parts * width);
   p.column_chunks = (int)(((int64_t)s->N + p.columns - 1) / p.columns);
+  if (p.many) p.columns = width, p.column_chunks = (int)pieces;
   return p;
 }
 
@@ -571,17 +717,19 @@ template <int RT, int TT>
 bool down(const AdapterArgs& a, unsigned groups, hipStream_t s) {
   return launch(ccq_adapter_down_kernel<RT, TT>, a, groups, 256, down_lds<RT, TT>(), s);
 }
-template <int KK, int TT>
+template <int KK>
 bool up(const AdapterArgs& a, unsigned groups, hipStream_t s) {
-  return launch(ccq_adapter_up_kernel<KK, TT>, a, groups, 64 * kUpWaves, up_lds<KK, TT>(a.rank), s);
+  return launch(ccq_adapter_up_kernel<KK>, a, groups, 64 * kUpWaves, up_lds<KK>(a.rank), s);
 }
+
+int64_t v_bytes(const Plan& p, int T) { return ((int64_t)p.splits * T * p.padded * 4 + 15) / 16 * 16; }
 
 }  // namespace
 
 int64_t adapters_workspace(const ccq_adapter_set* set, int T) {
   if (T == 0) return 0;
   const Plan p = plan_of(set, T);
-  return (int64_t)p.splits * T * p.padded * 4;
+  return v_bytes(p, T) + (p.many ? ((int64_t)T + 31) / 32 * (p.steps32 * 4 * 1024) : 0);
 }
 
 int launch_adapters(const ccq_adapter_set* set, int T, const int32_t* rows, const int32_t* experts, const void* x, int64_t ldx, const void* y, int64_t ldy, void* out,
@@ -615,6 +763,26 @@ int launch_adapters(const ccq_adapter_set* set, int T, const int32_t* rows, cons
     return down<8, 1>(a, n, s);
   });
   a.chunks = p.column_chunks;
+  if (p.many) {
+    a.parts = reinterpret_cast<u32x4_t*>(static_cast<char*>(workspace) + v_bytes(p, T));
+    // What the caches hold of y, x and v is worth keeping while y and out fit the last of them (256 MB) beside other things: with loads that leave them alone 2048 rows of 8192
+    // take 20.0 us in this kernel and 16.7 with plain ones, 2048 rows of 18432 with x from memory 59.5 us in all and 63.3.
+    const bool streams = (int64_t)T * set->N * 4 > (int64_t)128 << 20;
+    // row by row of 32, in one go where the columns' workgroups fill the chip, else in as many stretches as do
+    const int64_t blocks = ((int64_t)T + 31) / 32, stretches = p.column_chunks < kAtOnce ? kAtOnce / p.column_chunks : 1;
+    a.blocks_each = (int32_t)((blocks + stretches - 1) / stretches);
+    const int64_t groups = (blocks + a.blocks_each - 1) / a.blocks_each * p.column_chunks;
+    auto join_rows = [&](auto kk) {
+      constexpr int KK = decltype(kk)::value;
+      return ok && launch(ccq_adapter_join_kernel<KK>, a, (unsigned)(blocks * 2 * KK), 256, 0, s) &&
+             (streams ? launch(ccq_adapter_rows_kernel<KK, true>, a, (unsigned)groups, 512, 0, s) : launch(ccq_adapter_rows_kernel<KK, false>, a, (unsigned)groups, 512, 0, s));
+    };
+    ok = p.steps32 == 1   ? join_rows(std::integral_constant<int, 1>())
+         : p.steps32 == 2 ? join_rows(std::integral_constant<int, 2>())
+         : p.steps32 == 4 ? join_rows(std::integral_constant<int, 4>())
+                          : join_rows(std::integral_constant<int, 8>());
+    return ok && hipGetLastError() == hipSuccess ? CCQ_OK : CCQ_ERR_HIP;
+  }
   in_parts((int64_t)p.together * p.column_chunks, p.few ? 256 : 64 * kUpWaves, [&](unsigned n) {
     if (p.few) {
       if (a.rank <= 8) return launch(ccq_adapter_few_kernel<1>, a, n, 256, 0, s);
@@ -623,9 +791,7 @@ int launch_adapters(const ccq_adapter_set* set, int T, const int32_t* rows, cons
       if (a.rank <= 64) return launch(ccq_adapter_few_kernel<8>, a, n, 256, 0, s);
       return a.rank <= 128 ? launch(ccq_adapter_few_kernel<16>, a, n, 256, 0, s) : launch(ccq_adapter_few_kernel<32>, a, n, 256, 0, s);
     }
-    if (p.padded <= 32) return two ? up<1, 2>(a, n, s) : up<1, 1>(a, n, s);
-    if (p.padded <= 64) return two ? up<2, 2>(a, n, s) : up<2, 1>(a, n, s);
-    return p.padded <= 128 ? up<4, 1>(a, n, s) : up<8, 1>(a, n, s);
+    return p.steps32 == 1 ? up<1>(a, n, s) : p.steps32 == 2 ? up<2>(a, n, s) : p.steps32 == 4 ? up<4>(a, n, s) : up<8>(a, n, s);
   });
   return ok && hipGetLastError() == hipSuccess ? CCQ_OK : CCQ_ERR_HIP;
 }

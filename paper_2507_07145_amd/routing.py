@@ -95,6 +95,9 @@ class Order(NamedTuple):
     places: torch.Tensor
 
 
+_new = tuple.__new__   # (past the Python code of a named tuple's own)
+
+
 class Routes(NamedTuple):
     """ids int32 [T][k] (-1: none) and weights fp32 [T][k], the best expert first, and their order (None if it was not asked for)."""
     ids: torch.Tensor
@@ -161,7 +164,7 @@ def route(logits: torch.Tensor, top_k: int, scoring: str = "softmax", bias: torc
     if stream is None:
         r = _answer((_native or _calls()).route(logits, top_k, _SCORING[scoring], bias, groups, top_groups, group_best, renormalize, float(scale), order), "ccq_route")
         if r is not None:
-            return Routes(r[0], r[1], Order(*r[2:]) if len(r) > 2 else None)
+            return _new(Routes, (r[0], r[1], _new(Order, r[2:]) if order else None))
     _need(logits.dim() == 2 and logits.shape[1] > 0 and _rows(logits) and logits.dtype in (torch.bfloat16, torch.float32), "logits: bf16 or fp32 rows [T][experts] are needed")
     T, E = logits.shape
     _need(bias is None or (bias.shape == (E,) and bias.dtype == torch.float32 and (E == 1 or bias.stride(0) == 1)), "bias: fp32, one per expert, is needed")
@@ -187,7 +190,7 @@ def sort_rows(ids: torch.Tensor, experts: int, first: int = 0, stream=None) -> O
     if stream is None:
         r = _answer((_native or _calls()).sort(ids, experts, first), "ccq_sort_rows")
         if r is not None:
-            return Order(*r)
+            return _new(Order, r)
     _need(ids.dim() == 2 and ids.dtype == torch.int32 and _rows(ids) and ids.shape[1] > 0, "ids: int32 rows [T][k] are needed")
     _on_this_gpu(ids)
     T, k = ids.shape
