@@ -209,7 +209,8 @@ int ccq_gemm_ex(const ccq_weight *w, const void *x, int32_t M, int64_t ldx, void
  *   Output row p in [expert_offsets[e], expert_offsets[e+1]) is
  *       y[p][:] = x[sorted_rows[p]][:] * W_dq(e)^T.
  *   x DEVICE bf16 [T][ldx]; sorted_rows DEVICE int32 [P], values in [0,T);
- *   expert_offsets_dev DEVICE int32 [E+1] with [0] = 0, monotone, [E] = P;
+ *   expert_offsets_dev DEVICE int32 [E+1] with [0] = 0, monotone, [E] = P, or without a host copy up to P: rows of y from [E] on
+ *   are then left as they are (and what sorted_rows holds for them is not looked at);
  *   expert_offsets_host HOST copy of the same, or NULL: when given it is
  *   validated (CCQ_ERR_ROUTING) and shapes the launch -- it must equal the
  *   device array: experts it shows as empty may not be visited at all, and
@@ -219,7 +220,7 @@ int ccq_gemm_ex(const ccq_weight *w, const void *x, int32_t M, int64_t ldx, void
  *   with other routings must pass NULL here: the launch recorded with a
  *   host copy is tied to that routing (its busy experts, their row counts);
  *   y DEVICE bf16 [P][ldy].  An expert with no rows writes nothing.
- *   The top-k combine and any activation function stay with the caller. */
+ *   ccq_route and ccq_combine below make the order and the top-k sum; any activation function stays with the caller. */
 int ccq_grouped_gemm(const ccq_weight *w0, int32_t E, int64_t codes_stride, int64_t scales_stride,
                      int64_t ab_stride, const void *x, int32_t T, int64_t ldx,
                      const int32_t *sorted_rows, int32_t P, const int32_t *expert_offsets_dev,

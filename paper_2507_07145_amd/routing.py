@@ -241,7 +241,7 @@ def adapters(y: torch.Tensor, x: torch.Tensor, adapters: Adapters, order: Order,
     T = x.shape[0]
     _need(y.dtype == torch.bfloat16 and _rows(y) and y.shape == (T, d.N), "y: bf16 rows [T][N] are needed")
     for t in (order.rows, order.experts):
-        _need(t.dtype == torch.int32 and t.shape == (T,) and (T <= 1 or t.stride(0) == 1), "order: one entry per row is needed")
+        _need(t is not None and t.dtype == torch.int32 and t.shape == (T,) and (T <= 1 or t.stride(0) == 1), "order: one entry per row is needed")
     _on_this_gpu(x, y, adapters.a, order.rows, order.experts, out)
     _int32(T)
     if out is None:

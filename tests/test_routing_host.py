@@ -118,6 +118,10 @@ def test_adapter_sets():
 
 
 def test_host_tensors_and_wrong_types():
+    for call in (lambda: r.route(torch.zeros(2, 8), 2), lambda: r.sort_rows(torch.zeros(2, 8, dtype=torch.int32), 2),
+                 lambda: r.combine(bf16(4, 8), torch.zeros(2, 2, dtype=torch.int32), torch.zeros(2, 2))):
+        with pytest.raises(ValueError, match="GPU"):
+            call()
     with pytest.raises(ValueError, match="scoring"):
         r.route(torch.zeros(2, 8), 2, scoring="tanh")
     with pytest.raises(ValueError, match="logits"):
