@@ -180,10 +180,11 @@ constexpr int down_lds() {
   return stages > sums ? stages : sums;
 }
 
+constexpr int kTogether = 8;   // partial sums asked for at once: their latency is what a short call waits for
+
 // Two neighbouring ranks of a row of v, summed over the workgroups first, first + step, ... of those that shared K.
 typedef __attribute__((ext_vector_type(2))) float f32x2_t;
 __device__ __forceinline__ f32x2_t sum_parts(const AdapterArgs& a, const float* from, int first, int step) {
-  constexpr int kTogether = 8;   // asked for at once: their latency is what a short call waits for
   f32x2_t v = {0.f, 0.f};
   for (int s0 = first; s0 < a.splits; s0 += kTogether * step) {
     f32x2_t part[kTogether];
@@ -206,24 +207,22 @@ __device__ __forceinline__ u32x2_t in_two(f32x2_t v) {
   return u32x2_t{top1 | top0 >> 16, pack_bf16(rest0, rest1)};
 }
 
-// The rows [first, end) of a block, which have no adapter or one without ranks: out is y.  `waves` wavefronts of a workgroup, columns n_first .. n_end - 1.
-__device__ __forceinline__ void copy_rows(const AdapterArgs& a, int64_t p0, int first, int end, int n_first, int n_end, int wave, int waves, int lane) {
+// The rows [first, end) of a block, which have no adapter or one without ranks: out is y, in the columns n_first .. n_end - 1.  A thread copies eight columns of one row at a time.
+__device__ __forceinline__ void copy_rows(const AdapterArgs& a, int64_t p0, int first, int end, int n_first, int n_end, int thread, int threads) {
+  const int pieces = (n_end - n_first + 7) / 8;
 #pragma unroll 1
-  for (int row = first + wave; row < end; row += waves) {
-    const int t = a.rows[p0 + row];
+  for (int at = thread; at < (end - first) * pieces; at += threads) {
+    const int row = at / pieces, n = n_first + (at - row * pieces) * 8, t = a.rows[p0 + first + row];
     if ((uint32_t)t >= (uint32_t)a.T) continue;
     const uint16_t* from = a.y + t * a.ldy;
     uint16_t* to = a.out + t * a.ld_out;
+    if (n + 8 <= a.N) {
+      u32x4_t v;
+      __builtin_memcpy(&v, from + n, 16);
+      __builtin_memcpy(to + n, &v, 16);
+    } else {
 #pragma unroll 1
-    for (int n = n_first + 8 * lane; n < n_end; n += 512) {
-      if (n + 8 <= a.N) {
-        u32x4_t v;
-        __builtin_memcpy(&v, from + n, 16);
-        __builtin_memcpy(to + n, &v, 16);
-      } else {
-#pragma unroll 1
-        for (int h = n; h < a.N; ++h) to[h] = from[h];
-      }
+      for (int h = n; h < a.N; ++h) to[h] = from[h];
     }
   }
 }
@@ -262,13 +261,9 @@ __global__ __launch_bounds__(256) void ccq_adapter_few_kernel(AdapterArgs a) {
   for (; runs.starts; runs.skip(a.together)) {
     const int first = runs.first(), end = runs.end();
     const int i = __builtin_amdgcn_readfirstlane(__shfl(runs.adapter, first));
-    if (i < 0) {
-      if (a.copies) copy_rows(a, p0, first, end, n_first, n_end, wave, 4, lane);
-      continue;
-    }
-    const int rank = rank_of(a, i);
-    if (rank == 0) {
-      if (a.copies) copy_rows(a, p0, first, end, n_first, n_end, wave, 4, lane);
+    const int rank = i < 0 ? 0 : rank_of(a, i);
+    if (i < 0 || rank == 0) {
+      if (a.copies) copy_rows(a, p0, first, end, n_first, n_end, tid, 256);
       continue;
     }
     // Of four rows from row0 on: a step's B and y.  (Past N the last column is read again, and not stored; pieces past the rank are masked.)
@@ -301,7 +296,7 @@ __global__ __launch_bounds__(256) void ccq_adapter_few_kernel(AdapterArgs a) {
     }
     // v: pairs of ranks of each row, the workgroups that shared K among as many threads as there are for each pair
     const float scale = a.scales ? a.scales[i] : 1.f;
-    const int rows = end - first, pairs = rows * (kWide / 2), sharing = max(1, 256 / pairs);
+    const int rows = end - first, pairs = rows * (kWide / 2), sharing = max(1, min(256 / pairs, (a.splits + kTogether - 1) / kTogether));
 #pragma unroll 1
     for (int c0 = 0; c0 < pairs; c0 += 256) {
       const int c = c0 + tid % min(pairs, 256), share = tid / min(pairs, 256), row = c / (kWide / 2), r = c % (kWide / 2) * 2;
@@ -404,7 +399,7 @@ __global__ __launch_bounds__(64 * kUpWaves, 4) void ccq_adapter_up_kernel(Adapte
     asm volatile("" : "+v"(thread));   // (what follows from it is formed in the run, not kept in registers over all of them)
     const int lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6), i16 = lane & 15, quarter = lane >> 4;
     if (rank == 0) {   // out is y
-      if (a.copies) copy_rows(a, p0, first, end, (int)n_first, n_end, wave, kUpWaves, lane);
+      if (a.copies) copy_rows(a, p0, first, end, (int)n_first, n_end, thread, kThreads);
       continue;
     }
     const int last = (rank - 1) >> 5;
@@ -680,9 +675,10 @@ Plan plan_of(const ccq_adapter_set* s, int T) {
   p.tiles = p.many && s->rank <= 64 ? 2 : 1;
   const int rows = 16 * p.tiles;
   p.blocks = ((int64_t)T + rows - 1) / rows;
-  // every adapter that begins inside a block makes one more run
+  // Every adapter that begins inside a block makes one more run.  Few blocks have room for as many as there are rows (a workgroup that finds none ends at once, one
+  // that finds two takes twice as long: 37 rows of 12 adapters 14.6 us with the mean number, 11.1 us so); more have it for the mean number.
   const int64_t begins = s->count < T ? s->count : T;
-  const int64_t runs = 1 + (begins + p.blocks - 1) / p.blocks;
+  const int64_t runs = p.blocks <= 16 ? 1 + begins : 1 + (begins + p.blocks - 1) / p.blocks;
   p.together = (int)(runs < rows ? runs : rows);
   if (p.together > T) p.together = T;
   p.padded = (s->rank + 15) / 16 * 16;
