@@ -24,7 +24,7 @@ struct AdapterArgs {
   int64_t ldx, ldy, ld_out, block0;
   uint32_t blocks;        // of the launch
   u32x4_t* parts;         // v as matrix operands, where there are many rows
-  int32_t blocks_each;    // blocks of 32 rows of a workgroup then
+  int64_t blocks_each;    // pieces of 32 rows and 256 columns of a workgroup then
   int32_t T, K, N, rank, count, padded;
   int32_t together;       // runs of a block that have a workgroup of their own at the same time
   int32_t splits, steps;  // workgroups along K, steps of 32 columns of each
@@ -537,64 +537,81 @@ __global__ __launch_bounds__(256) void ccq_adapter_join_kernel(AdapterArgs a) {
   to[2 * KK * 64 * 4] = halves.y;
 }
 
-// The second: a workgroup keeps 256 columns of an adapter's B in registers, a wavefront 32 of them, and goes along the rows, 32 at a time; y of the next rows is asked for
-// while the products of these go through LDS to meet theirs.  STREAMS: y is not to stay in the caches.  Bound by y and out.
+// The second: a workgroup keeps 256 columns of an adapter's B in registers, a wavefront 32 of them, and goes along the rows, 32 at a time; y of the next kDeep times 32 rows is on
+// its way while the products of these go through LDS to meet theirs.  The work of all columns and rows lies on one line, of which each workgroup has as much.  STREAMS: y is
+// not to stay in the caches.  Bound by y and out.
+constexpr int kRowsColumns = 128, kRowsThreads = 2 * kRowsColumns;
 template <int KK, bool STREAMS>
-__global__ __launch_bounds__(512, KK <= 2 ? 4 : 2) void ccq_adapter_rows_kernel(AdapterArgs a) {
-  constexpr int kColumns = 256, kPitch = kColumns + kRowFloats, kMyRows = 2;   // rows row0 and row0 + 16 of a thread
+__global__ __launch_bounds__(kRowsThreads, KK <= 2 ? 4 : 2) void ccq_adapter_rows_kernel(AdapterArgs a) {
+  constexpr int kColumns = kRowsColumns, kPitch = kColumns + kRowFloats, kMyRows = 2;   // rows row0 and row0 + 16 of a thread
+  constexpr int kDeep = KK <= 2 ? 1 : 2;
+  constexpr bool kAhead = KK <= 2;   // v is asked for before what else a block needs
   __shared__ __align__(16) float products[32 * kPitch];
-  const int n_first = (int)(blockIdx.x % a.chunks) * kColumns;
-  const int64_t block_from = (int64_t)(blockIdx.x / a.chunks) * a.blocks_each, all_blocks = ((int64_t)a.T + 31) / 32;
-  const int64_t block_to = min(block_from + a.blocks_each, all_blocks);
+  const int blocks = (int)(((int64_t)a.T + 31) / 32);
+  // (an XCD's workgroups, every eighth, lie side by side on the line: its L2 meets an eighth of B)
+  const uint32_t turn = gridDim.x % 8 == 0 ? blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8 : blockIdx.x;
+  const int64_t all = (int64_t)blocks * a.chunks, from = (int64_t)turn * a.blocks_each, to = min(from + a.blocks_each, all);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i16 = lane & 15, quarter = lane >> 4;
-  const int column = threadIdx.x % 32 * 8, row0 = threadIdx.x / 32, n = n_first + column;
-  const bool whole = n + 8 <= a.N;
-  // rows of a block for this thread, and their y
-  auto rows_of = [&](int64_t block, int (&t)[kMyRows]) {
+  const int column = threadIdx.x % (kColumns / 8) * 8, row0 = threadIdx.x / (kColumns / 8);
+  struct Place {
+    int piece, block;
+    __device__ __forceinline__ void step(int blocks) {
+      if (++block == blocks) block = 0, ++piece;
+    }
+  };
+  // this thread's rows of a block, and their y
+  auto rows_of = [&](const Place& p, int (&t)[kMyRows]) {
 #pragma unroll
     for (int j = 0; j < kMyRows; ++j) {
-      const int64_t p = block * 32 + row0 + 16 * j;
-      t[j] = p < a.T ? a.rows[p] : -1;
+      const int64_t at = (int64_t)p.block * 32 + row0 + 16 * j;
+      t[j] = at < a.T ? a.rows[at] : -1;
       if ((uint32_t)t[j] >= (uint32_t)a.T) t[j] = -1;
     }
   };
-  auto load_y = [&](const int (&t)[kMyRows], u32x4_t (&y)[kMyRows]) {
+  auto load_y = [&](const Place& p, const int (&t)[kMyRows], u32x4_t (&y)[kMyRows]) {
+    const int n = p.piece * kColumns + column;
 #pragma unroll
     for (int j = 0; j < kMyRows; ++j)
-      if (t[j] >= 0 && whole) {
-        const u32x4_any_t* from = reinterpret_cast<const u32x4_any_t*>(a.y + (int64_t)t[j] * a.ldy + n);
-        if constexpr (STREAMS) y[j] = __builtin_nontemporal_load(from);
-        else y[j] = *from;
+      if (t[j] >= 0 && n + 8 <= a.N) {
+        const u32x4_any_t* at = reinterpret_cast<const u32x4_any_t*>(a.y + (int64_t)t[j] * a.ldy + n);
+        if constexpr (STREAMS) y[j] = __builtin_nontemporal_load(at);
+        else y[j] = *at;
       }
   };
-  int t[kMyRows], t_next[kMyRows];
-  u32x4_t y[kMyRows], y_next[kMyRows], b[KK][2];
-  int t_after[kMyRows], adapters = Runs::of_lane(a, block_from * 32, 32), adapters_next;
-  rows_of(block_from, t_next);
-  rows_of(block_from + 1, t_after);
-  load_y(t_next, y_next);
-  int held = -1, last = -1;   // whose B the registers hold, and its last step of 32 ranks
-  for (int64_t block = block_from; block < block_to; ++block) {
-    // what this block needs from memory was asked for before, but for v, which is asked for first; then the next block's
-    u32x4_t v[KK <= 2 ? 2 * KK : 1][2];
-    const u32x4_t* const parts = a.parts + block * (4 * KK * 64) + lane;
-    if constexpr (KK <= 2) {
+  auto load_v = [&](const Place& p, u32x4_t (&v)[2 * KK][2]) {
+    const u32x4_t* const parts = a.parts + (int64_t)p.block * (4 * KK * 64) + lane;
 #pragma unroll
-      for (int c = 0; c < 2 * KK; ++c) v[c][0] = parts[c * 64], v[c][1] = parts[(2 * KK + c) * 64];
-    }
-    Runs runs(a, block * 32, 32, adapters);
-    adapters_next = Runs::of_lane(a, (block + 1) * 32, 32);
+    for (int c = 0; c < 2 * KK; ++c) v[c][0] = parts[c * 64], v[c][1] = parts[(2 * KK + c) * 64];
+  };
+  // t[d], y[d]: of the block d further on; of one beyond them the rows only
+  Place now = {(int)(from / blocks), (int)(from % blocks)}, ahead = now;
+  int t[kDeep + 1][kMyRows];
+  u32x4_t y[kDeep][kMyRows], b[KK][2], v[kAhead ? 2 * KK : 1][2];
 #pragma unroll
-    for (int j = 0; j < kMyRows; ++j) t[j] = t_next[j], y[j] = y_next[j], t_next[j] = t_after[j];
-    if (block + 1 < block_to) load_y(t_next, y_next);
-    rows_of(block + 2, t_after);
-    adapters = adapters_next;
+  for (int d = 0; d < kDeep; ++d) {
+    rows_of(ahead, t[d]);
+    if (from + d < to) load_y(ahead, t[d], y[d]);
+    ahead.step(blocks);
+  }
+  rows_of(ahead, t[kDeep]);
+  int adapters = Runs::of_lane(a, (int64_t)now.block * 32, 32);
+  int held = -1, held_piece = -1, last = -1;   // whose B the registers hold, and its last step of 32 ranks
+  for (int64_t at = from; at < to; ++at) {
+    const int n_first = now.piece * kColumns, n = n_first + column;
+    const bool whole = n + 8 <= a.N;
+    if constexpr (kAhead) load_v(now, v);
+    Runs runs(a, (int64_t)now.block * 32, 32, adapters);
+    Place next = now;
+    next.step(blocks);
+    adapters = Runs::of_lane(a, (int64_t)next.block * 32, 32);
+    u32x4_t y_next[kMyRows];   // of the block kDeep further on
+    if (at + kDeep < to) load_y(ahead, t[kDeep], y_next);
     for (; runs.starts; runs.skip(1)) {
       const int first = runs.first(), end = runs.end();
       const int i = __builtin_amdgcn_readfirstlane(__shfl(runs.adapter, first));
       if (i < 0 && !a.copies) continue;
-      if (i >= 0 && i != held) {
-        held = i;
+      if (i >= 0 && (i != held || now.piece != held_piece)) {
+        held = i, held_piece = now.piece;
         const int rank = rank_of(a, i);
         last = (rank - 1) >> 5;
 #pragma unroll
@@ -610,6 +627,7 @@ __global__ __launch_bounds__(512, KK <= 2 ? 4 : 2) void ccq_adapter_rows_kernel(
       }
       const bool adds = i >= 0 && last >= 0;
       if (adds) {
+        const u32x4_t* const parts = a.parts + (int64_t)now.block * (4 * KK * 64) + lane;
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
           f32x4_t acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
@@ -617,7 +635,7 @@ __global__ __launch_bounds__(512, KK <= 2 ? 4 : 2) void ccq_adapter_rows_kernel(
           for (int k = 0; k < KK; ++k) {
             if (k > last) break;
             u32x4_t hi, lo;
-            if constexpr (KK <= 2) hi = v[w * KK + k][0], lo = v[w * KK + k][1];
+            if constexpr (kAhead) hi = v[w * KK + k][0], lo = v[w * KK + k][1];
             else hi = parts[(w * KK + k) * 64], lo = parts[(2 * KK + w * KK + k) * 64];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
@@ -633,11 +651,11 @@ __global__ __launch_bounds__(512, KK <= 2 ? 4 : 2) void ccq_adapter_rows_kernel(
 #pragma unroll
       for (int j = 0; j < kMyRows; ++j) {
         const int row = row0 + 16 * j;
-        if (row < first || row >= end || t[j] < 0 || n >= a.N || (!adds && !a.copies)) continue;
+        if (row < first || row >= end || t[0][j] < 0 || n >= a.N || (!adds && !a.copies)) continue;
         const float* d = products + row * kPitch + column;
-        uint16_t* o = a.out + (int64_t)t[j] * a.ld_out + n;
+        uint16_t* o = a.out + (int64_t)t[0][j] * a.ld_out + n;
         if (whole) {
-          u32x4_t sum = y[j];
+          u32x4_t sum = y[0][j];
           if (adds) {
             const f32x4_t d0 = *reinterpret_cast<const f32x4_t*>(d), d1 = *reinterpret_cast<const f32x4_t*>(d + 4);
 #pragma unroll
@@ -646,17 +664,28 @@ __global__ __launch_bounds__(512, KK <= 2 ? 4 : 2) void ccq_adapter_rows_kernel(
           }
           __builtin_nontemporal_store(sum, reinterpret_cast<u32x4_any_t*>(o));
         } else {   // the last columns
-          const uint16_t* from = a.y + (int64_t)t[j] * a.ldy + n;
+          const uint16_t* from_y = a.y + (int64_t)t[0][j] * a.ldy + n;
 #pragma unroll 1
-          for (int h = 0; h < a.N - n; ++h) o[h] = adds ? to_bf16(bf16_lo(from[h]) + d[h]) : from[h];
+          for (int h = 0; h < a.N - n; ++h) o[h] = adds ? to_bf16(bf16_lo(from_y[h]) + d[h]) : from_y[h];
         }
       }
       if (adds) __syncthreads();
     }
+#pragma unroll
+    for (int j = 0; j < kMyRows; ++j) {
+#pragma unroll
+      for (int d = 0; d + 1 < kDeep; ++d) y[d][j] = y[d + 1][j];
+      y[kDeep - 1][j] = y_next[j];
+#pragma unroll
+      for (int d = 0; d < kDeep; ++d) t[d][j] = t[d + 1][j];
+    }
+    now = next;
+    ahead.step(blocks);
+    rows_of(ahead, t[kDeep]);
   }
 }
 
-constexpr int kAtOnce = 512;   // workgroups of 512 threads that the chip holds
+constexpr int at_once(int kk) { return (kk <= 2 ? 512 : 256) * (256 / kRowsColumns); }   // workgroups of the last kernel that the chip holds
 
 // How the rows and K of a call are cut.
 struct Plan {
@@ -699,7 +728,7 @@ Plan plan_of(const ccq_adapter_set* s, int T) {
   parts = (parts + 7) / 8 * 8;
   p.columns = (int)((pieces + parts - 1) / parts * width);
   p.column_chunks = (int)(((int64_t)s->N + p.columns - 1) / p.columns);
-  if (p.many) p.columns = width, p.column_chunks = (int)pieces;
+  if (p.many) p.columns = kRowsColumns, p.column_chunks = (s->N + kRowsColumns - 1) / kRowsColumns;
   return p;
 }
 
@@ -764,14 +793,12 @@ int launch_adapters(const ccq_adapter_set* set, int T, const int32_t* rows, cons
     // What the caches hold of y, x and v is worth keeping while y and out fit the last of them (256 MB) beside other things: with loads that leave them alone 2048 rows of 8192
     // take 20.0 us in this kernel and 16.7 with plain ones, 2048 rows of 18432 with x from memory 59.5 us in all and 63.3.
     const bool streams = (int64_t)T * set->N * 4 > (int64_t)128 << 20;
-    // row by row of 32, in one go where the columns' workgroups fill the chip, else in as many stretches as do
-    const int64_t blocks = ((int64_t)T + 31) / 32, stretches = p.column_chunks < kAtOnce ? kAtOnce / p.column_chunks : 1;
-    a.blocks_each = (int32_t)((blocks + stretches - 1) / stretches);
-    const int64_t groups = (blocks + a.blocks_each - 1) / a.blocks_each * p.column_chunks;
+    const int64_t blocks = ((int64_t)T + 31) / 32, all = blocks * p.column_chunks, most = at_once(p.steps32), groups = all < most ? all : most;
+    a.blocks_each = (all + groups - 1) / groups;
     auto join_rows = [&](auto kk) {
       constexpr int KK = decltype(kk)::value;
       return ok && launch(ccq_adapter_join_kernel<KK>, a, (unsigned)(blocks * 2 * KK), 256, 0, s) &&
-             (streams ? launch(ccq_adapter_rows_kernel<KK, true>, a, (unsigned)groups, 512, 0, s) : launch(ccq_adapter_rows_kernel<KK, false>, a, (unsigned)groups, 512, 0, s));
+             (streams ? launch(ccq_adapter_rows_kernel<KK, true>, a, (unsigned)groups, kRowsThreads, 0, s) : launch(ccq_adapter_rows_kernel<KK, false>, a, (unsigned)groups, kRowsThreads, 0, s));
     };
     ok = p.steps32 == 1   ? join_rows(std::integral_constant<int, 1>())
          : p.steps32 == 2 ? join_rows(std::integral_constant<int, 2>())
