@@ -1,11 +1,15 @@
 // Low-rank adapters of a batch's requests:  out[t] = y[t] + scale (x[t] A^T) B^T, A [rank][K] and B [N][rank] those of t's adapter.
 //
-// Two kernels of MFMA 16x16x32 bf16.  Rows come sorted by adapter; a workgroup takes a block of 16 TT of them and the runs of one adapter in it, one
-// after the other or, where many are to be expected, one each.  The first forms v = x A^T: its wavefronts and, where there are few blocks, several workgroups share K; the wavefronts'
-// sums are added through LDS, the workgroups' are left to the second kernel.  The second adds them up, multiplies by the scale and forms y + v B^T.
-// v is a sum of thousands of products and would lose in bf16 what the result's own rounding keeps: it enters the second product as
-// two bf16 numbers (within 2^-15 of it), which costs a second matrix instruction on operands that are there.
-// Bound by memory: A and B of the adapters in use where rows are few, x, y and out where they are many.
+// The first product, v = x A^T, is one kernel (MFMA 16x16x32 bf16): rows come sorted by adapter, and a workgroup takes a block of 16 or 32 of them with one run of one adapter in it and a
+// share of K; the shares' sums are left to the second product.  That has three forms:
+//   runs of few rows (rank x rows up to 8192, no more than four rows an adapter): B is read along its memory and multiplied by v in fp32, no matrix instruction.
+//     One row of 8192 to 8192, rank 16: 3.6 + 4.4 us; 37 rows, 7184 to 5001, rank 24, 12 adapters: 5.0 + 6.1; 128 rows of 96 adapters, 4096 to 11008, rank 32: 7.2 + 15.8, of
+//     which B's 51 MB alone take 10.
+//   up to 511 rows, or rows x N up to 2^22: MFMA, B and the products through LDS (256 rows, 4096 to 4096, rank 16, four adapters: 4.1 + 6.4 us).
+//   more: v is joined by a kernel of its own, B stays in registers (2048 rows, 7168 to 18432, rank 64, four adapters: 12.6 + 4.8 + 40 us; 4 TB/s of y and out).
+// v is a sum of thousands of products and would lose in bf16 what the result's own rounding keeps: it enters matrix instructions as two bf16 numbers (within 2^-15 of it), which costs a
+// second one on operands that are there.
+// Bound by memory: A and B of the adapters in use where rows are few, x, y and out where they are many; short calls by a chain of four or five dependent loads in each kernel.
 #include "ccq_routing.h"
 
 namespace ccq {
@@ -24,10 +28,10 @@ struct AdapterArgs {
   int64_t ldx, ldy, ld_out, block0;
   uint32_t blocks;        // of the launch
   u32x4_t* parts;         // v as matrix operands, where there are many rows
-  int64_t blocks_each;    // pieces of 32 rows and 256 columns of a workgroup then
+  int64_t blocks_each;    // pieces of 32 rows and 128 columns of a workgroup then
   int32_t T, K, N, rank, count, padded;
   int32_t together;       // runs of a block that have a workgroup of their own at the same time
-  int32_t splits, steps;  // workgroups along K, steps of 32 columns of each
+  int32_t splits, steps;  // workgroups along K, stages of 128 columns of each
   int32_t chunks;         // of ranks (first kernel), of columns (second)
   int32_t columns;        // of a workgroup of the second kernel
   uint8_t copies;         // out is not y
@@ -537,9 +541,10 @@ __global__ __launch_bounds__(256) void ccq_adapter_join_kernel(AdapterArgs a) {
   to[2 * KK * 64 * 4] = halves.y;
 }
 
-// The second: a workgroup keeps 256 columns of an adapter's B in registers, a wavefront 32 of them, and goes along the rows, 32 at a time; y of the next kDeep times 32 rows is on
+// The second: a workgroup keeps 128 columns of an adapter's B in registers, a wavefront 32 of them, and goes along the rows, 32 at a time; y of the next kDeep times 32 rows is on
 // its way while the products of these go through LDS to meet theirs.  The work of all columns and rows lies on one line, of which each workgroup has as much.  STREAMS: y is
-// not to stay in the caches.  Bound by y and out.
+// not to stay in the caches.  Bound by the latency of y: with three times 32 rows ahead and one workgroup on a CU it takes 45 us (2048 x 18432, rank 64), with 64 columns
+// 43, with 256 columns 42, so 40.
 constexpr int kRowsColumns = 128, kRowsThreads = 2 * kRowsColumns;
 template <int KK, bool STREAMS>
 __global__ __launch_bounds__(kRowsThreads, KK <= 2 ? 4 : 2) void ccq_adapter_rows_kernel(AdapterArgs a) {
@@ -699,9 +704,14 @@ struct Plan {
 
 Plan plan_of(const ccq_adapter_set* s, int T) {
   Plan p;
-  p.few = (int64_t)T * s->rank <= 8192 && T <= 4 * (int64_t)s->count;   // (runs of four rows or so, as far as one can tell here)
-  p.many = !p.few && T >= 512 && T <= 1 << 22;   // (its workgroups are one launch's)
-  p.tiles = p.many && s->rank <= 64 ? 2 : 1;
+  // Runs of four rows or so, as far as one can tell here: the second product of 512 rows with 128 adapters of rank 16 (4096 to 4096) takes 8.2 us and by MFMA, with v joined,
+  // 15.2, of 128 rows with 32 adapters 6.7 and 8.8; of 512 rows with 64 adapters 9.5 and 7.5, and with 128 adapters of rank 64 25.0 and 21.0.
+  p.few = (int64_t)T * s->rank <= 8192 && T <= 4 * (int64_t)s->count;
+  // The launch that joins v costs 3 to 4 us: second products without and with it take 7.6 and 9.6 us at 512 rows to 4096, 11.8 and 9.5 at 1024 rows to 4096, 11.3 and 10.5 at 512
+  // rows to 8192, 7.4 and 7.8 at 2048 rows to 1024.  (T: its workgroups are one launch's.)
+  p.many = !p.few && T >= 512 && (int64_t)T * s->N >= 4 << 20 && T <= 1 << 22;
+  // Blocks of 32 rows read A half as often but are half as many: 512 rows of 8192, rank 64, 6.5 us with 16 rows and 9.9 with 32; 4096 rows of 4096, rank 32, 14.3 and 11.3.
+  p.tiles = p.many && T >= 2048 && s->rank <= 64 ? 2 : 1;
   const int rows = 16 * p.tiles;
   p.blocks = ((int64_t)T + rows - 1) / rows;
   // Every adapter that begins inside a block makes one more run.  Few blocks have room for as many as there are rows (a workgroup that finds none ends at once, one

@@ -1,5 +1,5 @@
 // The order of ids by expert (ccq_order.h has the sort): one workgroup for few entries, else one launch that counts each workgroup's share and
-// one that places it.
+// one that places it.  200 entries of 128 experts take 2.6 us, 3066 of 160 7.0, 131072 of 8 experts 3.2 + 5.7, of 256 2.7 to 4.2 + 8.5.
 #include "ccq_order.h"
 
 namespace ccq {
@@ -43,13 +43,17 @@ __global__ __launch_bounds__(1024) void ccq_sort_kernel(SortArgs a) {
   sort_entries<ROUNDS>(a, lds, blockDim.x >> 6, (int)begin, end, FromIds{a.ids, a.ld_ids, a.k, a.first, a.E}, gridDim.x > 1 ? a.counts : nullptr, blockIdx.x, gridDim.x);
 }
 
-// One workgroup up to 8192 entries, then workgroups of 2048 and more, 64 at most (each adds up the counts of all).
-constexpr int kOneBlock = 8192, kChunk = 2048, kMostBlocks = 64;
+// One workgroup up to 4096 entries (8 and 256 experts: 6.5 and 9.0 us, two launches 6.2 and 8.1; 8192 entries 10.5 and 15.5, two launches 6.4 and 7.9, times of a graph's step).
+// Then workgroups of 1024 and more.  Each adds up the counts of all, so that there may be as many as P entries and E experts make worth it: 131072 entries of 1024
+// experts take 20.6 us with 64 workgroups and 26.1 with 128, 2^21 of 256 94 us with 64, 57 with 128, 39 with 256.
+constexpr int kOneBlock = 4096, kChunk = 1024, kMostBlocks = 256, kLeastBlocks = 64;
 
-int blocks_of(int64_t P) {
+int blocks_of(int64_t P, int E) {
   if (P <= kOneBlock) return 1;
+  int most = kMostBlocks;
+  while (most > kLeastBlocks && (int64_t)most * most * E > 32 * P) most /= 2;
   const int64_t n = (P + kChunk - 1) / kChunk;
-  return (int)(n > kMostBlocks ? kMostBlocks : n);
+  return (int)(n > most ? most : n);
 }
 
 // As many wavefronts as have 64 entries each, and their counters in 56 KB of LDS.
@@ -62,7 +66,7 @@ int waves_of(int E, int chunk) {
 }  // namespace
 
 int64_t sort_workspace(int T, int k, int experts) {
-  const int blocks = blocks_of((int64_t)T * k);
+  const int blocks = blocks_of((int64_t)T * k, experts);
   return blocks > 1 ? (int64_t)blocks * (experts + 1) * 4 : 0;
 }
 
@@ -72,7 +76,7 @@ int launch_sort(const int32_t* ids, int64_t ld_ids, int T, int k, int first, int
   a.counts = static_cast<uint32_t*>(workspace);
   a.rows = order->rows, a.experts = order->experts, a.offsets = order->offsets, a.places = order->places;
   a.P = T * k, a.k = Divisor(k), a.first = first, a.E = experts;
-  const int blocks = blocks_of(a.P);
+  const int blocks = blocks_of(a.P, experts);
   a.chunk = (int)(((int64_t)a.P + blocks - 1) / blocks);
   const int waves = waves_of(experts, a.chunk);
   a.stretch = (int)((((int64_t)a.chunk + waves - 1) / waves + 63) / 64 * 64);

@@ -176,3 +176,59 @@ def test_two_calls_with_workspaces_of_their_own():
     assert bool((ws[need:] == 0xAB).all())
     with pytest.raises(routing.CcqError):
         routing.adapters(y, x, adapters, order, workspace=ws[:need - 16])
+
+
+@pytest.mark.parametrize("T,N,n,R,runs", [(600, 7001, 4, 16, 0), (600, 7000, 6, 64, 5), (1300, 3333, 9, 128, 0), (520, 8100, 3, 256, 7), (8100, 520, 50, 32, 90), (2100, 2001, 2, 64, 3),
+                                          (2050, 2056, 3, 24, 0), (4096, 1025, 600, 8, 0), (5000, 841, 1, 136, 1), (4200, 1000, 40, 72, 33)])
+def test_many_rows_and_columns(T, N, n, R, runs):
+    c = Case(T, 264, N, R, n, T, ranks=True, runs=runs)
+    c.check(routing.adapters(c.y.to(DEV), c.x.to(DEV), c.set(), c.order()), f"{T} rows to {N}, {n} adapters of {R}")
+
+
+@pytest.mark.parametrize("T,N", [(900, 4701), (4500, 945)])
+def test_many_in_views_and_any_order(T, N):
+    """In place in columns of wider rows, in an order that is not sorted and has places that are no rows."""
+    c = Case(T, 136, N, 40, 5, T, ranks=True)
+    wide_x, wide_y = torch.randn(T, 150, device=DEV).bfloat16(), torch.randn(T, N + 22, device=DEV).bfloat16()
+    wide_x[:, 5:141], wide_y[:, 3:3 + N] = c.x.to(DEV), c.y.to(DEV)
+    before = wide_y.clone()
+    perm = torch.randperm(T, generator=torch.Generator().manual_seed(T))
+    rows, experts = perm.int().clone(), c.ids[perm].clone()
+    rows[7], rows[800], rows[801] = T, -1, 2 ** 31 - 1
+    experts[3], experts[50], experts[51] = 5, 2 ** 31 - 1, -2 ** 31
+    c.ids[perm[[3, 50, 51, 7, 800, 801]]] = -1
+    routing.adapters(wide_y[:, 3:3 + N], wide_x[:, 5:141], c.set(), routing.Order(rows.to(DEV), experts.to(DEV), None, None), out=wide_y[:, 3:3 + N])
+    c.check(wide_y[:, 3:3 + N], "any order")
+    before[:, 3:3 + N] = wide_y[:, 3:3 + N]
+    assert torch.equal(before, wide_y)
+
+
+def test_many_rows_specials():
+    c = Case(700, 72, 6100, 16, 3, 3, none=0.0)
+    c.x[5, 7], c.x[9, 0], c.y[11, 3] = float("nan"), float("inf"), float("nan")
+    got = routing.adapters(c.y.to(DEV), c.x.to(DEV), c.set(), c.order()).cpu()
+    assert bool(got[5].isnan().all()) and not bool(got[9].isfinite().any()) and bool(got[11, 3].isnan()) and bool(got[11, :3].isfinite().all())
+    for t in (5, 9, 11):
+        c.x[t], c.y[t], got[t] = 0, 0, 0
+    c.check(got, "specials")
+    c.a[:], c.b[:] = c.a.abs(), c.b.abs()
+    c.x[6, 1] = float("inf")
+    assert bool(torch.isposinf(routing.adapters(c.y.to(DEV), c.x.to(DEV), c.set(), c.order())[6]).all())
+
+
+def test_many_rows_captured():
+    c = Case(640, 264, 6600, 32, 6, 6)
+    adapters, x, y, ids = c.set(), c.x.to(DEV), c.y.to(DEV), c.ids.to(DEV)[:, None]
+    call = lambda: routing.adapters(y, x, adapters, routing.sort_rows(ids, 6))  # noqa: E731
+    want = call()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = call()
+    for seed in (7, 8, 9):
+        n = Case(640, 264, 6600, 32, 6, seed)
+        for t, v in ((x, n.x), (y, n.y), (ids, n.ids[:, None]), (adapters.a, n.a), (adapters.b, n.b)):
+            t.copy_(v)
+        graph.replay()
+        want = call()
+        assert torch.equal(out, want)
+        assert torch.equal(call(), want)

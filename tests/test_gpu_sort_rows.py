@@ -75,3 +75,9 @@ def test_behind_the_arrays():
     o = routing.ccq_order(room[0].data_ptr(), None, room[2].data_ptr(), None)   # (experts and places are optional)
     assert routing._load().ccq_sort_rows(ids.data_ptr(), 3, 70, 3, 0, 9, ctypes.byref(o), None, 0, None) == 0
     check_order(routing.Order(room[0][:210], room[1][:210], room[2][:10], room[3][:210].view(70, 3)), ids.cpu().numpy(), 9, "without experts and places")
+
+
+@pytest.mark.parametrize("T,k,experts", [(4096, 1, 7), (4097, 1, 7), (512, 8, 1024), (8192, 1, 300), (131072, 8, 9), (65536, 8, 1024), (262144, 8, 256), (300001, 7, 4096)])
+def test_many_workgroups(T, k, experts):
+    ids = ids_of(T, k, -1, experts, T)
+    check_order(routing.sort_rows(ids.to(DEV), experts), ids.numpy(), experts, f"{T} x {k} over {experts}")
