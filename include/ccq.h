@@ -518,7 +518,7 @@ typedef struct {
 } ccq_adapter_set;
 
 /* out[t] = y[t] + scales[i] (x[t] a[i]^T) b[i]^T for rows t with adapter i; the others' out is y.  Sums in fp32 and rounded to bf16 once; x a^T enters the second
- * product as the sum of two bf16 numbers, within 2^-15 of it.
+ * product as the sum of two bf16 numbers, within 2^-15 of it (an infinite number in b, in the ranks in use, may make NaN of what would be infinite).
  *   rows, experts DEVICE int32 [T]: the order of ids [T][1] (ccq_sort_rows with experts = count), one for all projections of a step.  Each t stands
  *   in `rows` once; any order is right, rows of one adapter side by side are fast.  An adapter outside 0 .. count - 1 is none.
  *   x DEVICE bf16 [T][ldx], y and out DEVICE bf16 [T][ldy], [T][ld_out]: strides in elements and free, rows may start at any element; out may be y (with the same stride).

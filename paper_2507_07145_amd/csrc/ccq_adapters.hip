@@ -473,7 +473,7 @@ __global__ __launch_bounds__(64 * kUpWaves, 4) void ccq_adapter_up_kernel(Adapte
       const int row = c / (16 * KK), r = c % (16 * KK) * 2;
       f32x2_t two = {0.f, 0.f};
       if (row >= first && row < end && r < rank) two = sum_parts(a, a.v + (p0 + row) * a.padded + r, 0, 1);
-      two.x *= scale, two.y = r + 1 < rank ? two.y * scale : 0.f;
+      two.x = r < rank ? two.x * scale : 0.f, two.y = r + 1 < rank ? two.y * scale : 0.f;
       const u32x2_t halves = in_two(two);
       const int at = r / 32 * 256 + (r / 8 % 4 * 16 + row) * 4 + r / 2 % 4;
       reinterpret_cast<uint32_t*>(parts)[at] = halves.x;
@@ -532,7 +532,7 @@ __global__ __launch_bounds__(256) void ccq_adapter_join_kernel(AdapterArgs a) {
       const int rank = rank_of(a, i);
       const float scale = a.scales ? a.scales[i] : 1.f;
       if (r < rank) two = sum_parts(a, a.v + p * a.padded + r, 0, 1);
-      two.x *= scale, two.y = r + 1 < rank ? two.y * scale : 0.f;
+      two.x = r < rank ? two.x * scale : 0.f, two.y = r + 1 < rank ? two.y * scale : 0.f;
     }
   }
   const u32x2_t halves = in_two(two);

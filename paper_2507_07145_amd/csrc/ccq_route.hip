@@ -174,7 +174,7 @@ __device__ __forceinline__ void largest(const RouteArgs& a, int sub, Key (&key)[
 }
 
 // The same on keys of 28 bits, one winner after the other: a number's bits in an order that integers have too, its lowest four replaced by V - 1 - i, so that of a
-// lane's equal ones the lowest index is the largest and no two are the same.  A lane's next best is the largest below its last: one subtraction and half a minimum
+// lane's equal ones the lowest index is the largest and no two are the same (-0 + 0 is 0).  A lane's next best is the largest below its last: one subtraction and half a minimum
 // for each value.
 __device__ __forceinline__ uint32_t ordered(float v) {
   const uint32_t b = __builtin_bit_cast(uint32_t, v);
@@ -191,7 +191,7 @@ struct Picker {
     row = L == 64 ? ~0ull : 0xFFFFull << (threadIdx.x & 48);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      key[i] = value[i] > kNone ? (ordered(value[i]) & ~15u) | (uint32_t)(15 - i) : 0;
+      key[i] = value[i] > kNone ? (ordered(value[i] + 0.f) & ~15u) | (uint32_t)(15 - i) : 0;
       best = max(best, key[i]);
     }
   }

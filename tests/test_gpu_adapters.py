@@ -232,3 +232,28 @@ def test_many_rows_captured():
         want = call()
         assert torch.equal(out, want)
         assert torch.equal(call(), want)
+
+
+@pytest.mark.parametrize("T,N", [(3, 40), (60, 40), (700, 6100)])
+def test_an_infinite_scale_stays_with_the_ranks_in_use(T, N):
+    c = Case(T, 64, N, 16, 2, 5, none=0.0)
+    c.a, c.b, c.x = c.a.abs(), c.b.abs() + 0.5, c.x.abs() + 0.5
+    c.ranks = torch.tensor([5, 16], dtype=torch.int32)
+    c.ids[:] = 0
+    c.scales[0] = float("inf")
+    assert bool(torch.isposinf(routing.adapters(c.y.to(DEV), c.x.to(DEV), c.set(), c.order())).all())
+
+
+@pytest.mark.parametrize("T,N", [((1 << 18) + 40, 16400), ((1 << 22) + 40, 1032)])
+def test_rows_past_32_bits(T, N):
+    """4.3e9 results; x past 32 bits too where there are more rows than one kernel's limit."""
+    K, R, n = 1032 if T > 1 << 22 else 64, 8, 3
+    x, y = (torch.empty(T, c, dtype=torch.bfloat16, device=DEV) for c in (K, N))
+    g = torch.Generator(DEV).manual_seed(T)
+    x.normal_(generator=g), y.normal_(generator=g)
+    ids = (torch.arange(T, device=DEV) % 4 - 1).int()[:, None]
+    c = Case(1, K, N, R, n, 1)
+    got = routing.adapters(y, x, c.set(), routing.sort_rows(ids, n))
+    for t in (0, T // 2, T - 40):
+        c.x, c.y, c.ids = x[t:t + 40].cpu(), y[t:t + 40].cpu(), ids[t:t + 40, 0].cpu()
+        c.check(got[t:t + 40], f"from row {t}")

@@ -100,3 +100,20 @@ def test_captured():
             t.copy_(n)
         graph.replay()
         assert torch.equal(y, routing.combine(rows, places, weights, base=base))
+
+
+def test_rows_past_32_bits():
+    P, N = (1 << 19) + 5, 8200          # 4.3e9 values
+    rows = torch.zeros(P, N, dtype=torch.bfloat16, device=DEV)
+    rows[P - 1], rows[1 << 18], rows[3] = 3.0, 5.0, 0.5
+    places = torch.tensor([[P - 1, 3], [1 << 18, P - 1], [-1, P]], dtype=torch.int32, device=DEV)
+    weights = torch.tensor([[1.0, 2.0], [1.0, 0.25], [1.0, 1.0]], device=DEV)
+    got = routing.combine(rows, places, weights)
+    assert torch.equal(got, torch.tensor([[4.0], [5.75], [0.0]], device=DEV).bfloat16().expand(3, N))
+    T = P
+    places = torch.full((T, 1), 3, dtype=torch.int32, device=DEV)
+    weights = (torch.arange(T, device=DEV) % 128).float()[:, None]
+    got = routing.combine(rows, places, weights, base=rows)
+    want = weights[:, 0] * 0.5 + rows[:, 0].float()
+    for c in (0, 511, 4096, N - 1):
+        assert torch.equal(got[:, c].float(), want)

@@ -181,3 +181,29 @@ def test_captured():
         torch.cuda.synchronize()
         for got, w in zip((r.ids, r.weights, *r.order), (want.ids, want.weights, *want.order)):
             assert torch.equal(got, w)
+
+
+@pytest.mark.parametrize("T", [3, 40, 2100])
+def test_zeros_of_either_sign_are_equal(T):
+    g = torch.Generator().manual_seed(T)
+    l = torch.tensor([0.0, -0.0, 1.0, -1.0])[torch.randint(0, 4, (T, 64), generator=g)]
+    l[0] = torch.tensor([-0.0, 0.0]).repeat(32)
+    for dtype in (torch.bfloat16, torch.float32):
+        for kw in (dict(), dict(scoring="sigmoid", groups=8, top_groups=3), dict(groups=8, top_groups=4, group_best=1), dict(bias=torch.zeros(64))):
+            check(l.to(dtype), 30 if not kw else 8, f"{T} {dtype} {kw.keys()}", **kw)
+
+
+def test_groups_of_one_and_all_experts():
+    for T in (1, 8, 9):
+        check(logits_of(T, 1024, T), 32, f"{T} rows, a group each", groups=1024, top_groups=40, group_best=2, bias=torch.linspace(-0.1, 0.1, 1024))
+        check(logits_of(T, 1024, T), 32, f"{T} rows, two groups", groups=2, top_groups=1, scoring="sigmoid")
+
+
+def test_logits_past_32_bits():
+    T, E = (1 << 22) + 3, 1024
+    l = torch.empty(T, E, dtype=torch.bfloat16, device=DEV).normal_(generator=torch.Generator(DEV).manual_seed(1))
+    r = routing.route(l, 2, renormalize=True)
+    for t in (0, 1 << 21, T - 9):
+        part = check(l[t:t + 9].cpu(), 2, f"from row {t}", renormalize=True)
+        assert torch.equal(r.ids[t:t + 9], part.ids) and torch.equal(r.weights[t:t + 9], part.weights)
+    assert torch.equal(r.order.experts[r.order.places.flatten().long()], r.ids.flatten()) and torch.equal(r.order.offsets[1:], r.ids.flatten().bincount(minlength=E).cumsum(0).int())
