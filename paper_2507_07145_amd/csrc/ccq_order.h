@@ -5,6 +5,8 @@
 // the first place of each wavefront's share of each expert; a second pass over the same entries hands the places out.  Bound by the latency of these
 // steps, not by memory.
 #pragma once
+#include <type_traits>
+
 #include "ccq_routing.h"
 
 namespace ccq {
@@ -52,19 +54,22 @@ __device__ __forceinline__ int lanes_below(uint64_t mask) {
   return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
 }
 
-// Adds the 64 entries from `i0` on to the wavefront's counters; returns what this lane's expert had before, entries of lower lanes included.
-template <typename Expert>
-__device__ __forceinline__ uint32_t count_64(uint32_t* mine, int i0, int end, int bits, const Expert& expert, uint32_t* e_out) {
-  const int lane = threadIdx.x & 63, i = i0 + lane;
-  const bool in = i < end;
-  const uint32_t e = in ? expert(i) : 0;
+// Adds 64 entries to the wavefront's counters, those of the lanes that are `in`.  What a lane's expert had before is had of lane `leader` and the returned lanes below this one.
+__device__ __forceinline__ uint64_t add_64(uint32_t* mine, uint32_t e, bool in, int bits, uint32_t* had, uint32_t* leader) {
+  const int lane = threadIdx.x & 63;
   const uint64_t same = peers_of(e, bits, __ballot(in));
-  const int leader = __builtin_ctzll(same | (1ull << lane));   // (lanes past the end lead themselves, and add nothing)
-  uint32_t had = 0;
-  if (in && leader == lane) had = atomicAdd(mine + e, (uint32_t)__builtin_popcountll(same));
-  had = (uint32_t)__shfl((int)had, leader);
-  *e_out = e;
-  return had + (uint32_t)lanes_below(same);
+  *leader = (uint32_t)__builtin_ctzll(same | (1ull << lane));   // (lanes past the end lead themselves, and add nothing)
+  *had = 0;
+  if (in && *leader == (uint32_t)lane) *had = atomicAdd(mine + e, (uint32_t)__builtin_popcountll(same));
+  return same;
+}
+template <typename Expert>
+__device__ __forceinline__ uint32_t count_64(uint32_t* mine, int i0, int end, int bits, const Expert& expert, uint32_t* e) {
+  const int i = i0 + (threadIdx.x & 63);
+  uint32_t had, leader;
+  *e = i < end ? expert(i) : 0;
+  const uint64_t same = add_64(mine, *e, i < end, bits, &had, &leader);
+  return (uint32_t)__shfl((int)had, (int)leader) + (uint32_t)lanes_below(same);
 }
 
 // LDS words that sort_entries needs.
@@ -92,6 +97,14 @@ __device__ __forceinline__ void sort_entries(const SortArgs& a, uint32_t* lds, i
   uint32_t* const parts = below + E1;   // sums of 64 experts each
   const int64_t from64 = (int64_t)begin + (int64_t)wave * a.stretch, to64 = from64 + a.stretch;
   const int from = (int)min(from64, (int64_t)end), to = (int)min(to64, (int64_t)end);
+  constexpr int kKept = ROUNDS > 0 ? ROUNDS : 1;
+  uint32_t e[kKept];
+  if constexpr (ROUNDS > 0) {   // all are on their way before the first is needed (past the end the last one again)
+    if (a.P > 0) {
+#pragma unroll
+      for (int r = 0; r < ROUNDS; ++r) e[r] = expert(min(from + 64 * r + lane, a.P - 1));
+    }
+  }
   for (int i = tid; i < (waves + 2) * E1; i += threads) lds[i] = 0;
   __syncthreads();
   if (all_counts) {   // as many threads to an expert as there are, each with every n-th workgroup's counts
@@ -100,28 +113,34 @@ __device__ __forceinline__ void sort_entries(const SortArgs& a, uint32_t* lds, i
       uint32_t sum = 0, before = 0;
       const int b0 = tid / min(E1, threads);
       if (b0 >= n) break;
-#pragma unroll 8
-      for (int b = b0; b < blocks; b += n) {
-        const uint32_t c = all_counts[(int64_t)b * E1 + x];
-        before += b < block ? c : 0;
-        sum += c;
-      }
+      auto add = [&](int b1, auto most) {   // so many at once; past the last workgroup the last one's again, which do not count
+        uint32_t c[most.value];
+#pragma unroll
+        for (int j = 0; j < most.value; ++j) c[j] = all_counts[(int64_t)min(b1 + j * n, blocks - 1) * E1 + x];
+#pragma unroll
+        for (int j = 0; j < most.value; ++j) {
+          const int b = b1 + j * n;
+          before += b < block ? c[j] : 0;
+          sum += b < blocks ? c[j] : 0;
+        }
+      };
+      int b = b0;
+      for (; b + 4 * n < blocks; b += 16 * n) add(b, std::integral_constant<int, 16>());
+      for (; b < blocks; b += 4 * n) add(b, std::integral_constant<int, 4>());
       atomicAdd(total + x, sum);
       atomicAdd(below + x, before);
     }
   }
-  uint32_t kept[ROUNDS > 0 ? ROUNDS : 1], e;   // expert << 16 | entries of the stretch before this one with the same
+  uint32_t kept[kKept];   // expert << 16 | entries of the stretch before this one with the same
   if constexpr (ROUNDS > 0) {
+    uint32_t had[kKept], leaders[kKept];
+    uint64_t same[kKept];
 #pragma unroll
-    for (int r = 0; r < ROUNDS; ++r) {
-      kept[r] = 0;
-      if (from + 64 * r < to) {
-        const uint32_t had = count_64(mine, from + 64 * r, to, a.bits, expert, &e);
-        kept[r] = e << 16 | had;
-      }
-    }
+    for (int r = 0; r < ROUNDS; ++r) same[r] = add_64(mine, e[r], from + 64 * r + lane < to, a.bits, &had[r], &leaders[r]);
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) kept[r] = e[r] << 16 | ((uint32_t)__shfl((int)had[r], (int)leaders[r]) + (uint32_t)lanes_below(same[r]));
   } else {
-    for (int i = from; i < to; i += 64) count_64(mine, i, to, a.bits, expert, &e);
+    for (int i = from; i < to; i += 64) count_64(mine, i, to, a.bits, expert, &e[0]);
   }
   __syncthreads();
   // the entries of each expert before each wavefront's, and of the experts before: sums within 64 experts first
@@ -166,8 +185,8 @@ __device__ __forceinline__ void sort_entries(const SortArgs& a, uint32_t* lds, i
     }
   } else {   // the counters go on from where each stretch's entries begin
     for (int i0 = from; i0 < to; i0 += 64) {
-      const uint32_t at = count_64(mine, i0, to, a.bits, expert, &e);
-      if (i0 + lane < to) place(i0 + lane, e, at);
+      const uint32_t at = count_64(mine, i0, to, a.bits, expert, &e[0]);
+      if (i0 + lane < to) place(i0 + lane, e[0], at);
     }
   }
 }

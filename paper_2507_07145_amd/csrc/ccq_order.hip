@@ -1,5 +1,5 @@
 // The order of ids by expert (ccq_order.h has the sort): one workgroup for few entries, else one launch that counts each workgroup's share and
-// one that places it.  200 entries of 128 experts take 2.6 us, 3066 of 160 7.0, 131072 of 8 experts 3.2 + 5.7, of 256 2.7 to 4.2 + 8.5.
+// one that places it.  Alone 200 entries of 128 experts take 2.5 us; in a graph's steps 3066 of 160 take 6.3, 131072 of 8 7.1, of 256 11.9 us.
 #include "ccq_order.h"
 
 namespace ccq {
@@ -43,10 +43,10 @@ __global__ __launch_bounds__(1024) void ccq_sort_kernel(SortArgs a) {
   sort_entries<ROUNDS>(a, lds, blockDim.x >> 6, (int)begin, end, FromIds{a.ids, a.ld_ids, a.k, a.first, a.E}, gridDim.x > 1 ? a.counts : nullptr, blockIdx.x, gridDim.x);
 }
 
-// One workgroup up to 4096 entries (8 and 256 experts: 6.5 and 9.0 us, two launches 6.2 and 8.1; 8192 entries 10.5 and 15.5, two launches 6.4 and 7.9, times of a graph's step).
-// Then workgroups of 1024 and more.  Each adds up the counts of all, so that there may be as many as P entries and E experts make worth it: 131072 entries of 1024
-// experts take 20.6 us with 64 workgroups and 26.1 with 128, 2^21 of 256 94 us with 64, 57 with 128, 39 with 256.
-constexpr int kOneBlock = 4096, kChunk = 1024, kMostBlocks = 256, kLeastBlocks = 64;
+// One workgroup up to 2048 entries (of 8 and 256 experts 4.3 and 5.6 us; 3066 entries in one 5.5 and 7.4, in two launches 5.7 and 6.8; 8192 entries 10.5 and 15.5, and 5.9 and 7.1).
+// Then workgroups of 512 and more, which is 0.5 us less than 1024.  Each adds up the counts of all, so that there may be as many as P entries and E experts make worth it:
+// 131072 entries of 1024 experts take 20.6 us with 64 workgroups and 26.1 with 128, 2^21 of 256 94 us with 64, 57 with 128, 39 with 256.
+constexpr int kOneBlock = 2048, kChunk = 512, kMostBlocks = 256, kLeastBlocks = 32;
 
 int blocks_of(int64_t P, int E) {
   if (P <= kOneBlock) return 1;
@@ -56,10 +56,11 @@ int blocks_of(int64_t P, int E) {
   return (int)(n > most ? most : n);
 }
 
-// As many wavefronts as have 64 entries each, and their counters in 56 KB of LDS.
+// As many wavefronts as have 64 entries or 64 experts each, and their counters in 56 KB of LDS.
 int waves_of(int E, int chunk) {
+  const int work = chunk > E + 1 ? chunk : E + 1;
   int waves = 16;
-  while (waves > 1 && (sort_words(waves, E) * 4 > 56 * 1024 || (waves - 1) * 64 >= chunk)) waves /= 2;
+  while (waves > 1 && (sort_words(waves, E) * 4 > 56 * 1024 || (waves - 1) * 64 >= work)) waves /= 2;
   return waves;
 }
 
@@ -83,7 +84,7 @@ int launch_sort(const int32_t* ids, int64_t ld_ids, int T, int k, int first, int
   a.bits = bits_of(experts);
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (blocks > 1) hipLaunchKernelGGL(ccq_sort_count_kernel, dim3(blocks), dim3(1024), (size_t)(experts + 1) * 4, s, a);
-  const auto sort = a.stretch <= 64 ? ccq_sort_kernel<1> : a.stretch <= 128 ? ccq_sort_kernel<2> : a.stretch <= 512 ? ccq_sort_kernel<8> : ccq_sort_kernel<0>;
+  const auto sort = a.stretch <= 64 ? ccq_sort_kernel<1> : a.stretch <= 128 ? ccq_sort_kernel<2> : a.stretch <= 256 ? ccq_sort_kernel<4> : a.stretch <= 512 ? ccq_sort_kernel<8> : ccq_sort_kernel<0>;
   hipLaunchKernelGGL(sort, dim3(blocks), dim3(waves * 64), (size_t)sort_words(waves, experts) * 4, s, a);
   return hipGetLastError() == hipSuccess ? CCQ_OK : CCQ_ERR_HIP;
 }

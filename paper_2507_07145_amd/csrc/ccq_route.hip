@@ -383,7 +383,7 @@ __global__ __launch_bounds__(256) void ccq_route_kernel(RouteArgs a) {
   choose<L, V, BIAS>(a, lds + row * row_bytes(a.E, a.groups), chosen[row], (int64_t)blockIdx.x * kRows + row, threadIdx.x % L);
 }
 
-// A few rows and their order in one launch, a wavefront for each row.
+// A few rows and their order in one launch, a wavefront for each row and as many more as help the order.
 struct FromLds {
   const int32_t (*rows)[kPlaces];
   Divisor k;
@@ -399,7 +399,7 @@ __global__ __launch_bounds__(64 * kFewRows) void ccq_route_few_kernel(RouteArgs 
   extern __shared__ __align__(16) char lds[];
   __shared__ int32_t chosen[kFewRows][kPlaces];
   const int row = threadIdx.x / 64;
-  choose<64, V, BIAS>(a, lds + row * row_bytes(a.E, a.groups), chosen[row], row, threadIdx.x & 63);
+  if (row < a.T) choose<64, V, BIAS>(a, lds + row * row_bytes(a.E, a.groups), chosen[row], row, threadIdx.x & 63);
   __syncthreads();
   sort_entries<1>(sort, reinterpret_cast<uint32_t*>(lds), blockDim.x / 64, 0, sort.P, FromLds{chosen, sort.k, a.E}, nullptr, 0, 1);
 }
@@ -443,9 +443,10 @@ bool launch_by_size(const RouteArgs& a, hipStream_t s) {
 
 template <int V, bool BIAS>
 bool launch_few(const RouteArgs& a, const SortArgs& sort, hipStream_t s) {
-  const int rows = a.T * row_bytes(a.E, a.groups), words = 4 * sort_words(a.T, a.E), lds = rows > words ? rows : words;
+  const int for_sort = (a.E + 1 + 63) / 64, waves = a.T > for_sort ? a.T : for_sort < kFewRows ? for_sort : kFewRows;   // (the sort's sums go over all experts)
+  const int rows = a.T * row_bytes(a.E, a.groups), words = 4 * sort_words(waves, a.E), lds = rows > words ? rows : words;
   if (!fits(ccq_route_few_kernel<V, BIAS>, lds)) return false;
-  hipLaunchKernelGGL((ccq_route_few_kernel<V, BIAS>), dim3(1), dim3(64 * a.T), (size_t)lds, s, a, sort);
+  hipLaunchKernelGGL((ccq_route_few_kernel<V, BIAS>), dim3(1), dim3(64 * waves), (size_t)lds, s, a, sort);
   return true;
 }
 template <bool BIAS>
