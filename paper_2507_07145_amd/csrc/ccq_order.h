@@ -86,10 +86,11 @@ __device__ __forceinline__ uint32_t up_to_lane(uint32_t v) {
 }
 
 // All threads of a workgroup of `waves` wavefronts: the entries [begin, end), expert(i) 0 .. E (E: none).  With several workgroups `all_counts` are their
-// counts, `block` is this one's number.  ROUNDS > 0: a stretch has at most 64 ROUNDS entries, which stay in registers between the passes.
+// counts, `block` is this one's number; where there are none each counts all entries.  ROUNDS > 0: a stretch has at most 64 ROUNDS entries, which stay in registers between the passes.
 template <int ROUNDS, typename Expert>
 __device__ __forceinline__ void sort_entries(const SortArgs& a, uint32_t* lds, int waves, int begin, int end, const Expert& expert, const uint32_t* all_counts, int block,
                                              int blocks) {
+  const bool counts_others = blocks > 1 && !all_counts;
   const int E1 = a.E + 1, tid = threadIdx.x, threads = waves * 64, wave = tid >> 6, lane = tid & 63;
   uint32_t* const mine = lds + wave * E1;
   uint32_t* const total = lds + waves * E1;
@@ -131,6 +132,19 @@ __device__ __forceinline__ void sort_entries(const SortArgs& a, uint32_t* lds, i
       atomicAdd(below + x, before);
     }
   }
+  if (counts_others) {   // total: the entries from this workgroup's first on
+    constexpr int kAtOnce = 8;
+    for (int i0 = tid; i0 < a.P; i0 += kAtOnce * threads) {
+      uint32_t of[kAtOnce];
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) of[j] = expert(min(i0 + j * threads, a.P - 1));
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) {
+        const int i = i0 + j * threads;
+        if (i < a.P) atomicAdd((i < begin ? below : total) + of[j], 1u);
+      }
+    }
+  }
   uint32_t kept[kKept];   // expert << 16 | entries of the stretch before this one with the same
   if constexpr (ROUNDS > 0) {
     uint32_t had[kKept], leaders[kKept];
@@ -149,12 +163,13 @@ __device__ __forceinline__ void sort_entries(const SortArgs& a, uint32_t* lds, i
     uint32_t all = 0;
     if (x < E1) {
       uint32_t sum = below[x];
+      all = counts_others ? total[x] + sum : total[x];
       for (int w = 0; w < waves; ++w) {
         const uint32_t c = lds[w * E1 + x];
         lds[w * E1 + x] = sum;
         sum += c;
       }
-      all = all_counts ? total[x] : sum;
+      if (blocks == 1) all = sum;
     }
     const uint32_t upto = up_to_lane(all);
     if (x < E1) total[x] = upto - all;

@@ -77,7 +77,7 @@ def test_behind_the_arrays():
     check_order(routing.Order(room[0][:210], room[1][:210], room[2][:10], room[3][:210].view(70, 3)), ids.cpu().numpy(), 9, "without experts and places")
 
 
-@pytest.mark.parametrize("T,k,experts", [(4096, 1, 7), (4097, 1, 7), (512, 8, 1024), (8192, 1, 300), (131072, 8, 9), (65536, 8, 1024), (262144, 8, 256), (300001, 7, 4096)])
+@pytest.mark.parametrize("T,k,experts", [(4096, 1, 7), (4097, 1, 7), (1024, 2, 1), (8192, 1, 3), (8193, 1, 30), (2731, 3, 4096), (512, 8, 1024), (8192, 1, 300), (131072, 8, 9), (65536, 8, 1024), (262144, 8, 256), (300001, 7, 4096)])
 def test_many_workgroups(T, k, experts):
     ids = ids_of(T, k, -1, experts, T)
     check_order(routing.sort_rows(ids.to(DEV), experts), ids.numpy(), experts, f"{T} x {k} over {experts}")
