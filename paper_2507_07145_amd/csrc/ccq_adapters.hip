@@ -6,7 +6,7 @@
 //     One row of 8192 to 8192, rank 16: 3.6 + 4.4 us; 37 rows, 7184 to 5001, rank 24, 12 adapters: 5.0 + 6.1; 128 rows of 96 adapters, 4096 to 11008, rank 32: 7.2 + 15.8, of
 //     which B's 51 MB alone take 10.
 //   up to 511 rows, or rows x N up to 2^22: MFMA, B and the products through LDS (256 rows, 4096 to 4096, rank 16, four adapters: 4.1 + 6.4 us).
-//   more: v is joined by a kernel of its own, B stays in registers (2048 rows, 7168 to 18432, rank 64, four adapters: 12.6 + 4.8 + 40 us; 4 TB/s of y and out).
+//   more: v is joined by a kernel of its own, B stays in registers (2048 rows, 7168 to 18432, rank 64, four adapters: 11.6 + 4.8 + 35 us; 4.3 TB/s of y and out).
 // v is a sum of thousands of products and would lose in bf16 what the result's own rounding keeps: it enters matrix instructions as two bf16 numbers (within 2^-15 of it), which costs a
 // second one on operands that are there.
 // Bound by memory: A and B of the adapters in use where rows are few, x, y and out where they are many; short calls by a chain of four or five dependent loads in each kernel.
@@ -79,7 +79,7 @@ __device__ __forceinline__ uint32_t staged(int row, int piece) { return (uint32_
 // the card's address units take at a quarter of their rate.  Threads hold two stages more, or four, in registers; wavefront w multiplies columns 32 w .. of each
 // stage, the wavefronts' sums are added at the end.
 template <int RT, int TT>
-__global__ __launch_bounds__(256, RT == 8 ? 2 : 3) void ccq_adapter_down_kernel(AdapterArgs a) {
+__global__ __launch_bounds__(256, RT * TT >= 8 ? 2 : 3) void ccq_adapter_down_kernel(AdapterArgs a) {
   extern __shared__ __align__(256) uint8_t lds[];
   constexpr int kStage = (RT + TT) * 16 * kStageRow;
   uint32_t g = blockIdx.x;
@@ -132,7 +132,7 @@ __global__ __launch_bounds__(256, RT == 8 ? 2 : 3) void ccq_adapter_down_kernel(
     for (int u = 0; u < RT; ++u)
 #pragma unroll
       for (int w = 0; w < TT; ++w) acc[u][w] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    constexpr int kDepth = RT * TT <= 2 ? 4 : 2;   // stages asked for ahead
+    constexpr int kDepth = RT * TT <= 2 || RT * TT == 8 && RT < 8 ? 4 : 2;   // stages asked for ahead, as registers allow (2048 x 7168, rank 64: two 12.7 us, three 14.2, four 11.8)
     u32x4_t x[kDepth][TT], w[kDepth][RT];
     auto stage = [&](int s, int d) {
       uint8_t* const to_lds = lds + ((s - from) & 1) * kStage;
@@ -541,17 +541,19 @@ __global__ __launch_bounds__(256) void ccq_adapter_join_kernel(AdapterArgs a) {
   to[2 * KK * 64 * 4] = halves.y;
 }
 
-// The second: a workgroup keeps 128 columns of an adapter's B in registers, a wavefront 32 of them, and goes along the rows, 32 at a time; y of the next kDeep times 32 rows is on
-// its way while the products of these go through LDS to meet theirs.  The work of all columns and rows lies on one line, of which each workgroup has as much.  STREAMS: y is
-// not to stay in the caches.  Bound by the latency of y: with three times 32 rows ahead and one workgroup on a CU it takes 45 us (2048 x 18432, rank 64), with 64 columns
-// 43, with 256 columns 42, so 40.
+// The second: a workgroup keeps 128 columns of an adapter's B in registers, a wavefront 32 of them, and goes along the rows, 32 at a time; y and v of the next 32 rows are on
+// their way, v to LDS since all wavefronts need all of it, while the products of these go through LDS to meet theirs.  The work of all columns and rows lies on one line, of
+// which each workgroup has as much.  STREAMS: y is not to stay in the caches.
+// 2048 x 18432, rank 64: 35 us, 4.3 TB/s of y and out (a large copy 5.1); with v read by every wavefront for itself 39, with y two or three blocks ahead 36 and 37, with 64 columns
+// 43 and with 256 columns 42 where 128 took 40.  Stores that pass the caches by are worth 1 to 2 us of 17 where y is to stay, and cost 1 to 3 of 40 where not.
 constexpr int kRowsColumns = 128, kRowsThreads = 2 * kRowsColumns;
 template <int KK, bool STREAMS>
 __global__ __launch_bounds__(kRowsThreads, KK <= 2 ? 4 : 2) void ccq_adapter_rows_kernel(AdapterArgs a) {
   constexpr int kColumns = kRowsColumns, kPitch = kColumns + kRowFloats, kMyRows = 2;   // rows row0 and row0 + 16 of a thread
   constexpr int kDeep = KK <= 2 ? 1 : 2;
-  constexpr bool kAhead = KK <= 2;   // v is asked for before what else a block needs
+  constexpr int kParts = 4 * KK * 64;   // pieces of v of 32 rows
   __shared__ __align__(16) float products[32 * kPitch];
+  __shared__ u32x4_t v[kParts];
   const int blocks = (int)(((int64_t)a.T + 31) / 32);
   // (an XCD's workgroups, every eighth, lie side by side on the line: its L2 meets an eighth of B)
   const uint32_t turn = gridDim.x % 8 == 0 ? blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8 : blockIdx.x;
@@ -583,15 +585,16 @@ __global__ __launch_bounds__(kRowsThreads, KK <= 2 ? 4 : 2) void ccq_adapter_row
         else y[j] = *at;
       }
   };
-  auto load_v = [&](const Place& p, u32x4_t (&v)[2 * KK][2]) {
-    const u32x4_t* const parts = a.parts + (int64_t)p.block * (4 * KK * 64) + lane;
+  auto load_v = [&](const Place& p, u32x4_t (&part)[KK]) {
+    const u32x4_t* const parts = a.parts + (int64_t)p.block * kParts + threadIdx.x;
 #pragma unroll
-    for (int c = 0; c < 2 * KK; ++c) v[c][0] = parts[c * 64], v[c][1] = parts[(2 * KK + c) * 64];
+    for (int c = 0; c < KK; ++c) part[c] = parts[c * kRowsThreads];
   };
   // t[d], y[d]: of the block d further on; of one beyond them the rows only
   Place now = {(int)(from / blocks), (int)(from % blocks)}, ahead = now;
   int t[kDeep + 1][kMyRows];
-  u32x4_t y[kDeep][kMyRows], b[KK][2], v[kAhead ? 2 * KK : 1][2];
+  u32x4_t y[kDeep][kMyRows], b[KK][2], v_next[KK];
+  load_v(now, v_next);
 #pragma unroll
   for (int d = 0; d < kDeep; ++d) {
     rows_of(ahead, t[d]);
@@ -604,13 +607,17 @@ __global__ __launch_bounds__(kRowsThreads, KK <= 2 ? 4 : 2) void ccq_adapter_row
   for (int64_t at = from; at < to; ++at) {
     const int n_first = now.piece * kColumns, n = n_first + column;
     const bool whole = n + 8 <= a.N;
-    if constexpr (kAhead) load_v(now, v);
     Runs runs(a, (int64_t)now.block * 32, 32, adapters);
     Place next = now;
     next.step(blocks);
+    // (the last block's is read no more: its products were met behind a barrier)
+#pragma unroll
+    for (int c = 0; c < KK; ++c) v[threadIdx.x + c * kRowsThreads] = v_next[c];
+    load_v(next, v_next);
     adapters = Runs::of_lane(a, (int64_t)next.block * 32, 32);
     u32x4_t y_next[kMyRows];   // of the block kDeep further on
     if (at + kDeep < to) load_y(ahead, t[kDeep], y_next);
+    __syncthreads();
     for (; runs.starts; runs.skip(1)) {
       const int first = runs.first(), end = runs.end();
       const int i = __builtin_amdgcn_readfirstlane(__shfl(runs.adapter, first));
@@ -632,16 +639,13 @@ __global__ __launch_bounds__(kRowsThreads, KK <= 2 ? 4 : 2) void ccq_adapter_row
       }
       const bool adds = i >= 0 && last >= 0;
       if (adds) {
-        const u32x4_t* const parts = a.parts + (int64_t)now.block * (4 * KK * 64) + lane;
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
           f32x4_t acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
           for (int k = 0; k < KK; ++k) {
             if (k > last) break;
-            u32x4_t hi, lo;
-            if constexpr (kAhead) hi = v[w * KK + k][0], lo = v[w * KK + k][1];
-            else hi = parts[(w * KK + k) * 64], lo = parts[(2 * KK + w * KK + k) * 64];
+            const u32x4_t hi = v[(w * KK + k) * 64 + lane], lo = v[(2 * KK + w * KK + k) * 64 + lane];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
               acc[u] = mfma(b[k][u], lo, acc[u]);
@@ -667,7 +671,8 @@ __global__ __launch_bounds__(kRowsThreads, KK <= 2 ? 4 : 2) void ccq_adapter_row
             for (int h = 0; h < 4; ++h)
               sum[h] = pack_bf16(bf16_lo(sum[h]) + (h < 2 ? d0[2 * h] : d1[2 * h - 4]), bf16_hi(sum[h]) + (h < 2 ? d0[2 * h + 1] : d1[2 * h - 3]));
           }
-          __builtin_nontemporal_store(sum, reinterpret_cast<u32x4_any_t*>(o));
+          if constexpr (STREAMS) *reinterpret_cast<u32x4_any_t*>(o) = sum;
+          else __builtin_nontemporal_store(sum, reinterpret_cast<u32x4_any_t*>(o));
         } else {   // the last columns
           const uint16_t* from_y = a.y + (int64_t)t[0][j] * a.ldy + n;
 #pragma unroll 1
@@ -711,7 +716,7 @@ Plan plan_of(const ccq_adapter_set* s, int T) {
   // rows to 8192, 7.4 and 7.8 at 2048 rows to 1024.  (T: its workgroups are one launch's.)
   p.many = !p.few && T >= 512 && (int64_t)T * s->N >= 4 << 20 && T <= 1 << 22;
   // Blocks of 32 rows read A half as often but are half as many: 512 rows of 8192, rank 64, 6.5 us with 16 rows and 9.9 with 32; 4096 rows of 4096, rank 32, 14.3 and 11.3.
-  p.tiles = p.many && T >= 2048 && s->rank <= 64 ? 2 : 1;
+  p.tiles = p.many && T >= 2048 ? 2 : 1;
   const int rows = 16 * p.tiles;
   p.blocks = ((int64_t)T + rows - 1) / rows;
   // Every adapter that begins inside a block makes one more run.  Few blocks have room for as many as there are rows (a workgroup that finds none ends at once, one
@@ -726,8 +731,10 @@ Plan plan_of(const ccq_adapter_set* s, int T) {
   const int steps = (s->K + kStageColumns - 1) / kStageColumns;
   const int64_t busy = p.blocks + begins < p.blocks * p.together ? p.blocks + begins : p.blocks * p.together;   // workgroups with work
   // K is shared by a power of two of workgroups, neighbours in the grid: with eight and more of them an XCD's L2 meets the same columns of all A.
+  // Where every workgroup of the second product adds the shares up again fewer of them are worth more: 300 rows of 8192 to 8192, rank 64, 18.3 us with 256 workgroups, 21.7 with 512.
+  const int wanted = p.many ? 512 : 256;
   int splits = 1;
-  while (splits < 32 && busy * p.chunks * splits < 512 && steps >= splits * 4) splits *= 2;
+  while (splits < 32 && busy * p.chunks * splits < wanted && steps >= splits * 4) splits *= 2;
   p.steps = (steps + splits - 1) / splits;
   p.splits = (steps + p.steps - 1) / p.steps;
   // Columns: in a multiple of eight parts, for the same reason
@@ -795,7 +802,7 @@ int launch_adapters(const ccq_adapter_set* set, int T, const int32_t* rows, cons
     if (p.rank_tiles == 1) return two ? down<1, 2>(a, n, s) : down<1, 1>(a, n, s);
     if (p.rank_tiles == 2) return two ? down<2, 2>(a, n, s) : down<2, 1>(a, n, s);
     if (p.rank_tiles == 4) return two ? down<4, 2>(a, n, s) : down<4, 1>(a, n, s);
-    return down<8, 1>(a, n, s);
+    return two ? down<8, 2>(a, n, s) : down<8, 1>(a, n, s);
   });
   a.chunks = p.column_chunks;
   if (p.many) {
