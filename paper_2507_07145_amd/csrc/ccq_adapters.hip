@@ -6,7 +6,7 @@
 //     One row of 8192 to 8192, rank 16: 3.6 + 4.4 us; 37 rows, 7184 to 5001, rank 24, 12 adapters: 5.0 + 6.1; 128 rows of 96 adapters, 4096 to 11008, rank 32: 7.2 + 15.8, of
 //     which B's 51 MB alone take 10.
 //   up to 511 rows, or rows x N up to 2^22: MFMA, B and the products through LDS (256 rows, 4096 to 4096, rank 16, four adapters: 4.1 + 6.4 us).
-//   more: v is joined by a kernel of its own, B stays in registers (2048 rows, 7168 to 18432, rank 64, four adapters: 11.6 + 4.8 + 35 us; 4.3 TB/s of y and out).
+//   more: v is joined by a kernel of its own, B stays in registers (2048 rows, 7168 to 18432, rank 64, four adapters: 12.6 + 4.8 + 35 us; 4.3 TB/s of y and out).
 // v is a sum of thousands of products and would lose in bf16 what the result's own rounding keeps: it enters matrix instructions as two bf16 numbers (within 2^-15 of it), which costs a
 // second one on operands that are there.
 // Bound by memory: A and B of the adapters in use where rows are few, x, y and out where they are many; short calls by a chain of four or five dependent loads in each kernel.
@@ -79,7 +79,7 @@ __device__ __forceinline__ uint32_t staged(int row, int piece) { return (uint32_
 // the card's address units take at a quarter of their rate.  Threads hold two stages more, or four, in registers; wavefront w multiplies columns 32 w .. of each
 // stage, the wavefronts' sums are added at the end.
 template <int RT, int TT>
-__global__ __launch_bounds__(256, RT * TT >= 8 ? 2 : 3) void ccq_adapter_down_kernel(AdapterArgs a) {
+__global__ __launch_bounds__(256, RT == 8 ? 2 : 3) void ccq_adapter_down_kernel(AdapterArgs a) {
   extern __shared__ __align__(256) uint8_t lds[];
   constexpr int kStage = (RT + TT) * 16 * kStageRow;
   uint32_t g = blockIdx.x;
@@ -132,7 +132,7 @@ __global__ __launch_bounds__(256, RT * TT >= 8 ? 2 : 3) void ccq_adapter_down_ke
     for (int u = 0; u < RT; ++u)
 #pragma unroll
       for (int w = 0; w < TT; ++w) acc[u][w] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    constexpr int kDepth = RT * TT <= 2 || RT * TT == 8 && RT < 8 ? 4 : 2;   // stages asked for ahead, as registers allow (2048 x 7168, rank 64: two 12.7 us, three 14.2, four 11.8)
+    constexpr int kDepth = RT * TT <= 2 ? 4 : 2;   // stages asked for ahead: three workgroups on a CU are worth more (2048 x 7168, rank 64: 12.6 us, with four stages and two of them 16.6)
     u32x4_t x[kDepth][TT], w[kDepth][RT];
     auto stage = [&](int s, int d) {
       uint8_t* const to_lds = lds + ((s - from) & 1) * kStage;
@@ -731,8 +731,9 @@ Plan plan_of(const ccq_adapter_set* s, int T) {
   const int steps = (s->K + kStageColumns - 1) / kStageColumns;
   const int64_t busy = p.blocks + begins < p.blocks * p.together ? p.blocks + begins : p.blocks * p.together;   // workgroups with work
   // K is shared by a power of two of workgroups, neighbours in the grid: with eight and more of them an XCD's L2 meets the same columns of all A.
-  // Where every workgroup of the second product adds the shares up again fewer of them are worth more: 300 rows of 8192 to 8192, rank 64, 18.3 us with 256 workgroups, 21.7 with 512.
-  const int wanted = p.many ? 512 : 256;
+  // Up to as many workgroups as the chip holds.  Where every workgroup of the second product adds the shares up again fewer are worth more: 300 rows of 8192 to 8192, rank 64, 18.3 us
+  // with 256, 21.7 with 512.  Of ranks above 64 a CU holds two: 2048 rows of 8192, rank 128, 22.1 us in x A^T with half as many, 23.7 otherwise; 256 rows 27.6 in all and 30.0.
+  const int wanted = (p.many ? 512 : 256) / (p.padded > 64 ? 2 : 1);
   int splits = 1;
   while (splits < 32 && busy * p.chunks * splits < wanted && steps >= splits * 4) splits *= 2;
   p.steps = (steps + splits - 1) / splits;
