@@ -738,12 +738,13 @@ Plan plan_of(const ccq_adapter_set* s, int T) {
   while (splits < 32 && busy * p.chunks * splits < wanted && steps >= splits * 4) splits *= 2;
   p.steps = (steps + splits - 1) / splits;
   p.splits = (steps + p.steps - 1) / p.steps;
-  // Columns: in a multiple of eight parts, for the same reason
   p.steps32 = p.padded <= 32 ? 1 : p.padded <= 64 ? 2 : p.padded <= 128 ? 4 : 8;
   const int width = p.few || p.many || p.padded <= 64 ? 256 : 128;
   const int64_t pieces = ((int64_t)s->N + width - 1) / width;
-  int64_t parts = ((p.blocks >= 64 ? 1024 : 512) + busy - 1) / busy;
-  parts = (parts + 7) / 8 * 8;
+  // Parts of the columns: runs of few rows in a multiple of eight, for the same reason.  The MFMA kernel's workgroups all at once (two on a CU, or one by the LDS that ranks near 256 need), since a second
+  // turn waits for the first one's end: 256 rows of 8192 to 8192, rank 64, in runs of any length 11.0 us with 480 workgroups, 14.5 with 640; 3000 rows to 1000 8.4 and 11.2.
+  const int64_t places = p.padded > 128 && 2 * up_lds<8>(s->rank) > 160 * 1024 ? 256 : 512;
+  int64_t parts = p.few ? ((512 + busy - 1) / busy + 7) / 8 * 8 : busy < places ? places / busy : 1;
   p.columns = (int)((pieces + parts - 1) / parts * width);
   p.column_chunks = (int)(((int64_t)s->N + p.columns - 1) / p.columns);
   if (p.many) p.columns = kRowsColumns, p.column_chunks = (s->N + kRowsColumns - 1) / kRowsColumns;
