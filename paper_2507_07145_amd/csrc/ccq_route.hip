@@ -89,10 +89,20 @@ __device__ __forceinline__ int lanes_of_group(int groups) {
   return q;
 }
 
+// Logits whose scores may be the same in 64 bits though they are not: both above 20 or 600 below (1 + e^-l is rounded, or e^l or e^(l - top) lost), or nearer to each other than
+// 2^-30, as logits of less than 2^-7 can be.  Of others the scores are some 2^-48 apart at least, of 1 or, below 0, of themselves.
+struct Meeting {
+  float lo, hi;
+  __device__ __forceinline__ Meeting(const RouteArgs& a, float top) : lo(a.sigmoid ? -600.f : top - 600.f), hi(a.sigmoid ? 20.f : INFINITY) {}
+  __device__ __forceinline__ bool may(float x) const { return x > -INFINITY && (x >= hi || x <= lo || fabsf(x) < 0x1p-6f); }   // (with one of which this holds too)
+  __device__ __forceinline__ bool operator()(float x, float y) const { return !(fabsf(fminf(fmaxf(x, lo), hi) - fminf(fmaxf(y, lo), hi)) >= 0x1p-30f); }
+};
+
 // Closes the experts of groups that are not kept (keys become -infinity).  by: the values that groups are compared by.  Returns by how much the last group kept is
-// ahead of the first that is not, less `off` and what 2^-21 of the largest numbers that were added comes to.
-template <int L, int V, typename Key, typename Value>
-__device__ __forceinline__ Value keep_groups(const RouteArgs& a, char* lds, int sub, const Value (&by)[V], Key (&key)[V], Value off) {
+// ahead of the first that is not, less `off` and what 2^-21 of the largest numbers that were added comes to.  Of logits (LOGITS) it is -1 in a lane that finds two groups
+// whose scores may be the same, else 1.
+template <int L, int V, bool LOGITS, typename Key, typename Value>
+__device__ __forceinline__ Value keep_groups(const RouteArgs& a, char* lds, int sub, const Value (&by)[V], Key (&key)[V], Value off, Meeting meet) {
   Value* const values = reinterpret_cast<Value*>(lds);
   Value* const sums = reinterpret_cast<Value*>(lds + padded(a.E) * 8);
   uint8_t* const kept = reinterpret_cast<uint8_t*>(lds + (padded(a.E) + a.groups) * 8);
@@ -132,10 +142,15 @@ __device__ __forceinline__ Value keep_groups(const RouteArgs& a, char* lds, int 
   }
   wave_lds();
   Value least = INFINITY, most = -INFINITY;   // of the groups that are kept, of the others
+  bool met = false;
   for (int g = sub; g < a.groups; g += L) {
     const Value own = sums[g];
     int ahead = 0;
     for (int o = 0; o < a.groups; ++o) ahead += sums[o] > own || (sums[o] == own && o < g);
+    if constexpr (LOGITS) {
+      if (meet.may(own))   // (as good as never: 0.2 us of 6.8 for 511 rows of eight groups, with all pairs looked at 0.8)
+        for (int o = 0; o < a.groups; ++o) met |= sums[o] != own && meet(sums[o], own);
+    }
     kept[g] = ahead < a.top_groups;
     if (ahead < a.top_groups) least = min_of(least, own);
     else most = max_of(most, own);
@@ -146,6 +161,7 @@ __device__ __forceinline__ Value keep_groups(const RouteArgs& a, char* lds, int 
     const int e = i * L + sub;
     if (e < a.E && !kept[e * a.inv_group >> 20]) key[i] = -INFINITY;
   }
+  if constexpr (LOGITS) return met ? -1.f : 1.f;
   least = over_lanes<L>(least, [](Value x, Value y) { return min_of(x, y); });
   most = over_lanes<L>(most, [](Value x, Value y) { return max_of(x, y); });
   size = over_lanes<L>(size, [](Value x, Value y) { return max_of(x, y); });
@@ -233,7 +249,7 @@ __host__ __device__ inline int row_bytes(int E, int groups) { return groups > 1 
 // The choice is the one that 64-bit scores make, or the logits themselves.  It is made on fewer bits first.  Where every winner is ahead of the next by more than
 // these may be off, it is that already; where not, kMore candidates further on the last one mostly is behind all by that much, and their numbers in 64 bits, one to a
 // lane, set them in order.  Equal numbers in a row (and groups that are as near, for their choice) have all values formed in 64 bits: a row in thousands, unless
-// logits and biases are the same.
+// logits and biases are the same.  Groups that are compared by their best logits need no scores, but where two of these may be equal although the logits are not.
 template <int L, int V, bool BIAS>
 __device__ __forceinline__ void choose(const RouteArgs& a, char* lds, int32_t (&chosen)[kPlaces], int64_t t, int sub) {
   const bool live = t < a.T;
@@ -271,6 +287,14 @@ __device__ __forceinline__ void choose(const RouteArgs& a, char* lds, int32_t (&
   };
 
   float key[V], off = 0.f;
+  const Meeting meet(a, top);
+  auto keep_groups_exactly = [&](const float (&k)[V]) {
+    double s64[V];
+    exact(s64);
+#pragma unroll
+    for (int i = 0; i < V; ++i) key[i] = k[i];
+    keep_groups<L, V, false>(a, lds, sub, s64, key, 0.0, meet);
+  };
   const bool by_sums = BIAS || (a.groups > 1 && a.two_best);
   if (by_sums) {
     float s[V], inverse = 1.f;
@@ -289,20 +313,17 @@ __device__ __forceinline__ void choose(const RouteArgs& a, char* lds, int32_t (&
     }
     off = 2.f * (a.sigmoid ? kSigmoidOff : kSoftmaxOff);   // two of them against each other
     if (a.groups > 1) {
-      const bool sure = keep_groups<L, V>(a, lds, sub, s, key, 2.f * off) > 0.f;
-      if (__ballot(live && !sure)) {
-        double s64[V];
-        exact(s64);
-#pragma unroll
-        for (int i = 0; i < V; ++i) key[i] = BIAS ? s[i] : l[i];
-        keep_groups<L, V>(a, lds, sub, s64, key, 0.0);
-      }
+      const bool groups_sure = keep_groups<L, V, false>(a, lds, sub, s, key, 2.f * off, meet) > 0.f;
+      if (__ballot(live && !groups_sure)) keep_groups_exactly(BIAS ? s : l);
     }
     if (!BIAS) off = 0.f;
-  } else {
+  } else {   // (a group's best logit has its best score, which another group may have too)
 #pragma unroll
     for (int i = 0; i < V; ++i) key[i] = l[i];
-    if (a.groups > 1) keep_groups<L, V>(a, lds, sub, l, key, 0.f);
+    if (a.groups > 1) {
+      const bool groups_sure = keep_groups<L, V, true>(a, lds, sub, l, key, 0.f, meet) > 0.f;
+      if (__ballot(live && !groups_sure)) keep_groups_exactly(l);
+    }
   }
 
   const bool check = BIAS || a.fp32;   // (bf16 has its lowest 16 bits zero: its keys are whole)
