@@ -57,6 +57,21 @@ __device__ __forceinline__ T over_lanes(T v, F f) {
   return v;
 }
 
+// The sum of a row's values, f(i) that of expert i L + sub: the same additions in the same order for 16 lanes and for 64, so that it does not depend on how many rows there are.
+template <int L, int V, typename F>
+__device__ __forceinline__ double row_sum(F f) {
+  double sum[4] = {0.0, 0.0, 0.0, 0.0};   // of 64 experts, those of sub % 16 + 16 j
+#pragma unroll
+  for (int i = 0; i < V; ++i) sum[L == 16 ? i % 4 : 0] += f(i);
+  if constexpr (L == 16) {
+    sum[0] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  } else {
+    sum[0] += moved(sum[0], [](uint32_t u) { return xor16(u); });
+    sum[0] += moved(sum[0], [](uint32_t u) { return xor32(u); });
+  }
+  return over_lanes<16>(sum[0], [](double x, double y) { return x + y; });
+}
+
 constexpr float kNone = -INFINITY;
 
 // Logits as fp32 (bf16's are exact); what is not open is -infinity.
@@ -273,17 +288,12 @@ __device__ __forceinline__ void choose(const RouteArgs& a, char* lds, int32_t (&
   top = over_lanes<L>(top, [](float x, float y) { return fmaxf(x, y); });
 
   double total = a.sigmoid ? 1.0 : 0.0;   // of the softmax, once it is asked for
-  auto form_total = [&]() {
-    double sum = 0.0;
-#pragma unroll
-    for (int i = 0; i < V; ++i) sum += part(a, l[i], top);
-    total = over_lanes<L>(sum, [](double x, double y) { return x + y; });
-  };
+  auto form_total = [&]() { total = row_sum<L, V>([&](int i) { return part(a, l[i], top); }); };
+  auto score = [&](float of) { return a.sigmoid ? part(a, of, top) : part(a, of, top) / total; };   // (one form wherever it is asked for: sums may differ by their last bit alone)
   auto exact = [&](double (&s)[V]) {   // scores plus biases
     if (!a.sigmoid && total == 0.0) form_total();
-    const double inverse = 1.0 / total;
 #pragma unroll
-    for (int i = 0; i < V; ++i) s[i] = l[i] > kNone && bias[i] > kNone ? part(a, l[i], top) * inverse + (double)bias[i] : -INFINITY;   // (a comparison with NaN is false)
+    for (int i = 0; i < V; ++i) s[i] = l[i] > kNone && bias[i] > kNone ? score(l[i]) + (double)bias[i] : -INFINITY;   // (a comparison with NaN is false)
   };
 
   float key[V], off = 0.f;
@@ -349,7 +359,7 @@ __device__ __forceinline__ void choose(const RouteArgs& a, char* lds, int32_t (&
       int id = -1;
       double n = -INFINITY;
       if (sub < candidates) id = chosen[sub];
-      if (live && id >= 0) n = BIAS ? part(a, logit(a, t * a.ld + id), top) / total + (double)a.bias[id] : (double)logit(a, t * a.ld + id);
+      if (live && id >= 0) n = BIAS ? score(logit(a, t * a.ld + id)) + (double)a.bias[id] : (double)logit(a, t * a.ld + id);
       double* const numbers = reinterpret_cast<double*>(lds);
       if (sub < candidates) numbers[sub] = n;
       wave_lds();
@@ -384,7 +394,7 @@ __device__ __forceinline__ void choose(const RouteArgs& a, char* lds, int32_t (&
     if (sub + L * j < a.k) id[j] = chosen[sub + L * j];
     if (live && id[j] >= 0) w[j] = part(a, logit(a, t * a.ld + id[j]), top);
   }
-  if (a.renormalize) total = over_lanes<L>(w[0] + w[1], [](double x, double y) { return x + y; });
+  if (a.renormalize) total = row_sum<L, 1>([&](int) { return w[0] + w[1]; });   // (places sub and sub + 16; with 64 lanes, one place each, these meet first)
   if (!live) return;
 #pragma unroll
   for (int j = 0; j < (L < kMostChosen ? 2 : 1); ++j) {
