@@ -81,7 +81,7 @@ class Mixture:
 class Sequences:
     """Page table and lengths of a batch of sequences, each with room for `room` tokens, and which adapter each has (-1: none)."""
 
-    def __init__(self, sequences: int, room: int, adapters: int = 0, device="cuda"):
+    def __init__(self, sequences: int, room: int, device="cuda", adapters: int = 0):
         self.count, width = sequences, -(-room // PAGE_TOKENS)
         self.pages, self.room = sequences * width, width * PAGE_TOKENS
         self.table = torch.arange(self.pages, dtype=torch.int32, device=device).view(sequences, width)
@@ -101,8 +101,8 @@ class Sequences:
 
 
 class DecoderLayer:
-    def __init__(self, hidden: int, heads: int, kv_heads: int, feed_forward: int, pages: int, rope: layer.Rope, head_dim: int = 128, experts: int = 0, top_k: int = 0,
-                 adapters: int = 0, rank: int = 0, device="cuda"):
+    def __init__(self, hidden: int, heads: int, kv_heads: int, feed_forward: int, pages: int, rope: layer.Rope, head_dim: int = 128, device="cuda", experts: int = 0,
+                 top_k: int = 0, adapters: int = 0, rank: int = 0):
         new = lambda n, k: torch.randn(n, k, device=device) * k**-0.5  # noqa: E731
 
         def low_rank(n: int, k: int):
@@ -134,9 +134,9 @@ class DecoderLayer:
 
 
 class Decoder:
-    def __init__(self, layers: int, hidden: int, heads: int, kv_heads: int, feed_forward: int, sequences: int, room: int, experts: int = 0, top_k: int = 0, adapters: int = 0,
-                 rank: int = 0, device="cuda"):
-        self.state = Sequences(sequences, room, adapters, device)
+    def __init__(self, layers: int, hidden: int, heads: int, kv_heads: int, feed_forward: int, sequences: int, room: int, device="cuda", experts: int = 0, top_k: int = 0,
+                 adapters: int = 0, rank: int = 0):
+        self.state = Sequences(sequences, room, device, adapters)
         rope = layer.Rope(layer.rope_table(self.state.room, 128, device=device))
         more = dict(experts=experts, top_k=top_k, adapters=adapters, rank=rank, device=device)
         self.layers = [DecoderLayer(hidden, heads, kv_heads, feed_forward, self.state.pages, rope, **more) for _ in range(layers)]
@@ -184,8 +184,8 @@ def main():
         ap.add_argument(f"--{name}", type=int, default=value)
     a = ap.parse_args()
     torch.manual_seed(0)
-    decoder = Decoder(a.layers, a.hidden, a.heads, a.kv_heads, a.feed_forward, a.sequences, a.prompt + 3 * a.steps, a.experts, a.top_k, a.adapters,
-                      a.rank)
+    decoder = Decoder(a.layers, a.hidden, a.heads, a.kv_heads, a.feed_forward, a.sequences, a.prompt + 3 * a.steps, experts=a.experts, top_k=a.top_k,
+                      adapters=a.adapters, rank=a.rank)
     x = torch.randn(a.sequences * a.prompt, a.hidden, device="cuda").bfloat16()
     decoder.prompt(x)
     decoder.state.lens.zero_()
