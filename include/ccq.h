@@ -500,7 +500,7 @@ typedef struct {
   const void *base;         /* DEVICE [T][ld_base] of base_type, or NULL (zeros)                         */
   int64_t ld_base;
   int32_t base_type;        /* ccq_type                                                                  */
-  void *y;                  /* DEVICE [T][ldy] of y_type; may be base (with the same type and stride)    */
+  void *y;                  /* DEVICE [T][ldy] of y_type; may be base (same type; stride, past one row)  */
   int64_t ldy;
   int32_t y_type;           /* ccq_type                                                                  */
 } ccq_combination;
@@ -521,7 +521,7 @@ typedef struct {
  * product as the sum of two bf16 numbers, within 2^-15 of it (an infinite number in b, in the ranks in use, may make NaN of what would be infinite).
  *   rows, experts DEVICE int32 [T]: the order of ids [T][1] (ccq_sort_rows with experts = count), one for all projections of a step.  Each t stands
  *   in `rows` once; any order is right, rows of one adapter side by side are fast.  An adapter outside 0 .. count - 1 is none.
- *   x DEVICE bf16 [T][ldx], y and out DEVICE bf16 [T][ldy], [T][ld_out]: strides in elements and free, rows may start at any element; out may be y (with the same stride).
+ *   x DEVICE bf16 [T][ldx], y and out DEVICE bf16 [T][ldy], [T][ld_out]: strides in elements and free, rows may start at any element; out may be y (with the same stride, past one row).
  *   T = 0 is a no-op.  workspace DEVICE, 16-byte aligned, at least ccq_adapters_workspace_bytes(set, T) bytes (-1: invalid arguments). */
 int64_t ccq_adapters_workspace_bytes(const ccq_adapter_set *set, int32_t T);
 int ccq_adapters(const ccq_adapter_set *set, int32_t T, const int32_t *rows, const int32_t *experts, const void *x, int64_t ldx, const void *y, int64_t ldy,

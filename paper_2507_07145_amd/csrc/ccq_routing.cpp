@@ -86,7 +86,7 @@ extern "C" int ccq_combine(const ccq_combination* c, void* hip_stream) {
   if (c->T == 0) return CCQ_OK;
   if (!c->places || !c->weights || !c->y || (c->P > 0 && !c->rows)) return CCQ_ERR_NULL;
   if (c->ld_rows < c->N || c->ld_places < c->k || c->ld_weights < c->k || c->ldy < c->N || (c->base && c->ld_base < c->N)) return CCQ_ERR_BAD_PARAM;
-  if (c->y == c->base && (c->ldy != c->ld_base || c->y_type != c->base_type)) return CCQ_ERR_BAD_PARAM;
+  if (c->y == c->base && ((c->T > 1 && c->ldy != c->ld_base) || c->y_type != c->base_type)) return CCQ_ERR_BAD_PARAM;
   if (off(c->rows, 2) || off(c->places, 4) || off(c->weights, 4) || off(c->base, bytes_of(c->base_type)) || off(c->y, bytes_of(c->y_type))) return CCQ_ERR_ALIGN;
   return launch_combine(c, hip_stream);
 }
@@ -100,7 +100,7 @@ extern "C" int ccq_adapters(const ccq_adapter_set* set, int32_t T, const int32_t
   if (ldx < set->K || ldy < set->N || ld_out < set->N) return CCQ_ERR_BAD_PARAM;
   if (T == 0) return CCQ_OK;
   if (!set->a || !set->b || !rows || !experts || !x || !y || !out) return CCQ_ERR_NULL;
-  if (y == out && ldy != ld_out) return CCQ_ERR_BAD_PARAM;
+  if (T > 1 && y == out && ldy != ld_out) return CCQ_ERR_BAD_PARAM;
   if (off(set->a, 16) || off(set->b, 16) || off(set->scales, 4) || off(set->ranks, 4) || off(rows, 4) || off(experts, 4) || off(x, 2) || off(y, 2) || off(out, 2))
     return CCQ_ERR_ALIGN;
   if ((rc = check_workspace(adapters_workspace(set, T), workspace, workspace_bytes)) != CCQ_OK) return rc;
