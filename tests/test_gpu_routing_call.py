@@ -82,19 +82,21 @@ def test_a_subclass_is_not_looked_into():
 
 
 def test_out_of_memory_is_the_allocators_exception():
-    """A result that does not fit raises torch.OutOfMemoryError, as torch.empty does (the limit is the allocator's own, set from here: nothing is launched)."""
+    """A result that does not fit raises torch.OutOfMemoryError, as torch.empty does (the limit is the allocator's own, set from here: nothing is launched).
+    On a stream of their own: what earlier work has left free in pieces of the current one's memory is not for it."""
     T = 1 << 23
     logits, ids = torch.zeros(T, 8, dtype=torch.bfloat16, device=DEV), torch.zeros(T, 8, dtype=torch.int32, device=DEV)
     weights, rows = torch.zeros(T, 8, device=DEV), torch.zeros(1, 64, dtype=torch.bfloat16, device=DEV)
     a = routing.Adapters(torch.zeros(1, 8, 64, dtype=torch.bfloat16, device=DEV), torch.zeros(1, 64, 8, dtype=torch.bfloat16, device=DEV))
     x = torch.zeros(T, 64, dtype=torch.bfloat16, device=DEV)
     order = routing.Order(ids[:, 0].contiguous(), ids[:, 0].contiguous(), None, None)
+    stream = torch.cuda.Stream()
     torch.cuda.synchronize()
     torch.cuda.empty_cache()
     torch.cuda.set_per_process_memory_fraction(0.0)
     try:
         for call in (lambda: routing.route(logits, 8), lambda: routing.sort_rows(ids, 4), lambda: routing.combine(rows, ids, weights), lambda: routing.adapters(x, x, a, order)):
-            with pytest.raises(torch.OutOfMemoryError):
+            with torch.cuda.stream(stream), pytest.raises(torch.OutOfMemoryError):
                 call()
     finally:
         torch.cuda.set_per_process_memory_fraction(1.0)
