@@ -3,10 +3,10 @@
 // The first product, v = x A^T, is one kernel (MFMA 16x16x32 bf16): rows come sorted by adapter, and a workgroup takes a block of 16 or 32 of them with one run of one adapter in it and a
 // share of K; the shares' sums are left to the second product.  That has three forms:
 //   runs of few rows (rank x rows up to 8192, no more than four rows an adapter): B is read along its memory and multiplied by v in fp32, no matrix instruction.
-//     One row of 8192 to 8192, rank 16: 3.6 + 4.4 us; 37 rows, 7184 to 5001, rank 24, 12 adapters: 5.0 + 6.1; 128 rows of 96 adapters, 4096 to 11008, rank 32: 7.2 + 15.8, of
+//     One row of 8192 to 8192, rank 16: 3.8 + 4.6 us; 37 rows, 7184 to 5001, rank 24, 12 adapters: 5.0 + 6.0; 128 rows of 96 adapters, 4096 to 11008, rank 32: 7.5 + 15.8, of
 //     which B's 51 MB alone take 10.
-//   up to 511 rows, or rows x N up to 2^22: MFMA, B and the products through LDS (256 rows, 4096 to 4096, rank 16, four adapters: 4.1 + 6.4 us).
-//   more: v is joined by a kernel of its own, B stays in registers (2048 rows, 7168 to 18432, rank 64, four adapters: 12.6 + 4.8 + 35 us; 4.3 TB/s of y and out).
+//   up to 511 rows, or rows x N up to 2^22: MFMA, B and the products through LDS (256 rows, 4096 to 4096, rank 16, four adapters: 4.3 + 7.2 us; to 18432 4.3 + 12.4).
+//   more: v is joined by a kernel of its own, B stays in registers (2048 rows, 7168 to 18432, rank 64, four adapters: 13 + 5 + 35 us; 4.3 TB/s of y and out).
 // v is a sum of thousands of products and would lose in bf16 what the result's own rounding keeps: it enters matrix instructions as two bf16 numbers (within 2^-15 of it), which costs a
 // second one on operands that are there.
 // Bound by memory: A and B of the adapters in use where rows are few, x, y and out where they are many; short calls by a chain of four or five dependent loads in each kernel.
@@ -709,13 +709,14 @@ struct Plan {
 
 Plan plan_of(const ccq_adapter_set* s, int T) {
   Plan p;
-  // Runs of four rows or so, as far as one can tell here: the second product of 512 rows with 128 adapters of rank 16 (4096 to 4096) takes 8.2 us and by MFMA, with v joined,
-  // 15.2, of 128 rows with 32 adapters 6.7 and 8.8; of 512 rows with 64 adapters 9.5 and 7.5, and with 128 adapters of rank 64 25.0 and 21.0.
+  // Runs of four rows or so, as far as one can tell here: the second product of 512 rows with 128 adapters of rank 16 (4096 to 4096) takes 13.6 us and by MFMA 15.7, of 128 rows
+  // with 32 adapters 8.1 and 7.8; of 512 rows with 64 adapters 12.5 and 12.6, of 128 with 32 adapters of rank 64 14.3 and 9.5, and of 512 with 128 adapters of rank 64 36 and 25.5.
   p.few = (int64_t)T * s->rank <= 8192 && T <= 4 * (int64_t)s->count;
-  // The launch that joins v costs 3 to 4 us: second products without and with it take 7.6 and 9.6 us at 512 rows to 4096, 11.8 and 9.5 at 1024 rows to 4096, 11.3 and 10.5 at 512
-  // rows to 8192, 7.4 and 7.8 at 2048 rows to 1024.  (T: its workgroups are one launch's.)
+  // The launch that joins v costs 3 to 4 us: second products without and with it take, of rank 64, 8.5 and 10.7 us at 512 rows to 4096, 12.4 and 12.5 at 1024 rows to 4096, 13.5 and 12.6 at
+  // 512 rows to 8192, 7.5 and 11.3 at 2048 rows to 1024; of rank 16 7.3 and 9.1 at 512 rows to 4096, 9.8 and 10.5 at 1024.  (T: its workgroups are one launch's.)
   p.many = !p.few && T >= 512 && (int64_t)T * s->N >= 4 << 20 && T <= 1 << 22;
-  // Blocks of 32 rows read A half as often but are half as many: 512 rows of 8192, rank 64, 6.5 us with 16 rows and 9.9 with 32; 4096 rows of 4096, rank 32, 14.3 and 11.3.
+  // Blocks of 32 rows read A half as often but are half as many: with 16 rows and with 32, all launches, four adapters,
+  // 512 rows of 8192 to 8192, rank 64, take 22.4 and 24.6 us, 1024 24.6 and 25.0, 1536 30.9 and 32.1, 2048 35.8 and 35.2; rank 32, 4096 to 4096, 1024 rows 16.8 and 17.5, 2048 21.2 and 21.1, 4096 31.5 and 30.9.
   p.tiles = p.many && T >= 2048 ? 2 : 1;
   const int rows = 16 * p.tiles;
   p.blocks = ((int64_t)T + rows - 1) / rows;
@@ -732,7 +733,8 @@ Plan plan_of(const ccq_adapter_set* s, int T) {
   const int64_t busy = p.blocks + begins < p.blocks * p.together ? p.blocks + begins : p.blocks * p.together;   // workgroups with work
   // K is shared by a power of two of workgroups, neighbours in the grid: with eight and more of them an XCD's L2 meets the same columns of all A.
   // Up to as many workgroups as the chip holds.  Where every workgroup of the second product adds the shares up again fewer are worth more: 300 rows of 8192 to 8192, rank 64, 18.3 us
-  // with 256, 21.7 with 512.  Of ranks above 64 a CU holds two: 2048 rows of 8192, rank 128, 22.1 us in x A^T with half as many, 23.7 otherwise; 256 rows 27.6 in all and 30.0.
+  // with 256, 21.7 with 512.  (Where many adapters make x A^T the larger part it is the other way: 512 rows of 4096 to 4096 with 128 adapters 54 and 47.5.)  Of ranks above 64 a CU holds two: 2048
+  // rows of 8192, rank 128, 22.0 us in x A^T with half as many, 23.8 otherwise; 256 rows 26.1 in all and 26.5.
   const int wanted = (p.many ? 512 : 256) / (p.padded > 64 ? 2 : 1);
   int splits = 1;
   while (splits < 32 && busy * p.chunks * splits < wanted && steps >= splits * 4) splits *= 2;

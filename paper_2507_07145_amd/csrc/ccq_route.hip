@@ -3,8 +3,8 @@
 // L lanes hold a row's logits, V each: expert i L + lane in value i.  The choice is top_k times the largest that is left: every lane keeps its own best, the lanes of a row
 // compare theirs with DPP moves, and the lane that held the largest looks for its next.  Scores next to each other have to be told apart as exact arithmetic has
 // them: the choice is made in 32 bits where these leave no doubt, and else in 64.
-// One row of 64, with its order: 5.0 us; 64 rows of 256 with groups 7.1, 511 of 160 6.7: the latency of k rounds that wait for each other.  16384 rows of 256 with groups 18.5 us: vector
-// instructions (3.8 for the bytes alone).
+// One row of 64, with its order: 4.8 us; 64 rows of 256 with groups 7.0, 511 of 160 6.9: the latency of k rounds that wait for each other.  16384 rows of 256 with groups 19.4 us: vector
+// instructions, 1680 a wavefront (3.8 for the bytes alone).
 #include <cmath>
 
 #include "ccq_order.h"
@@ -424,6 +424,8 @@ struct FromLds {
     return id >= 0 ? (uint32_t)id : (uint32_t)E;
   }
 };
+// Two launches and one, with the call's order in a graph: one row of 64 experts 6.7 and 5.6 us, eight of 64 7.3 and 6.3, of 256 8.6 and 7.0, of 512 9.0 and 8.1, eight with 32 of 1024 16.2
+// and 16.7.  (A workgroup has room for 16 rows' wavefronts; more than eight have not been measured.)
 constexpr int kFewRows = 8;
 template <int V, bool BIAS>
 __global__ __launch_bounds__(64 * kFewRows) void ccq_route_few_kernel(RouteArgs a, SortArgs sort) {
@@ -458,8 +460,8 @@ bool launch(const RouteArgs& all, hipStream_t s) {
 
 template <bool BIAS>
 bool launch_by_size(const RouteArgs& a, hipStream_t s) {
-  // Few rows: a wavefront each, so that its steps are short; many: 16 lanes each, which have less to exchange.  Eight of 256, 1024 / 4096 / 8192 rows: 5.4 / 7.9 / 12.3 us with 64
-  // lanes, 8.1 / 8.4 / 9.9 with 16; of 64 experts 4.6 / 6.3 / 9.5 and 4.9 / 5.0 / 5.5.
+  // Few rows: a wavefront each, so that its steps are short; many: 16 lanes each, which have less to exchange.  Eight of 256, 1024 / 4096 / 8192 rows: 5.5 / 7.9 / 12.3 us with 64
+  // lanes, 8.1 / 8.6 / 9.9 with 16; of 64 experts 4.6 / 6.3 / 9.5 and 4.9 / 5.0 / 5.5.
   if (a.T > 2048) {
     if (a.E <= 64) return launch<16, 4, BIAS>(a, s);
     if (a.E <= 128) return launch<16, 8, BIAS>(a, s);

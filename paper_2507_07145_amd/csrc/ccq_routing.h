@@ -1,5 +1,4 @@
-// What the kernels around rows that choose their weights share: reductions over the lanes of a row, and the launchers that the host checks
-// (ccq_routing.cpp) call.
+// What the kernels around rows that choose their weights share: their limits, and the launchers that the host checks (ccq_routing.cpp) call.
 #pragma once
 #include <hip/hip_runtime.h>
 

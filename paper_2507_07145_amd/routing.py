@@ -9,6 +9,9 @@ Argument marshalling only, as in layer.py (include/ccq.h says what each call com
 cases with little host time, ctypes the others, which are checked and reported here.  Tensors are on the current GPU; with stream= the work is enqueued
 there, and results that are made lie in that stream's memory.
 
+The results of one call of route or sort_rows may be pieces of one allocation (of six tensors one, without stream=): who keeps one of them alone, or
+saves it, takes a clone.
+
 A layer of experts, without a copy to the host:
 
     routes = route(logits, 8, scoring="sigmoid", bias=balance, groups=8, top_groups=4, renormalize=True, scale=2.5)
